@@ -51,7 +51,9 @@ EXPORTS = ("preba_query", "preba_pack", "preba_preprocess", "preba_preprocess_ex
            "preba_bucket_batcher_push", "preba_bucket_batcher_poll",
            "preba_audio_query", "preba_audio_pack", "preba_audio_logmel",
            "preba_audio_layout", "preba_audio_resample_query", "preba_audio_resample",
-           "preba_jpeg_query", "preba_jpeg_decode")
+           "preba_jpeg_query", "preba_jpeg_decode",
+           "preba_pages_plan", "preba_rope_positions", "preba_rope_append",
+           "preba_pages_attend_query", "preba_pages_attend")
 
 
 class PrebaImg(ctypes.Structure):
@@ -143,6 +145,47 @@ class PrebaAudioBatch(ctypes.Structure):
                 ("n", ctypes.c_uint32), ("t_max", ctypes.c_uint32),
                 ("out", ctypes.c_void_p), ("out_bytes", ctypes.c_uint64),
                 ("status", ctypes.c_void_p)]
+
+
+class PrebaPagesPlan(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_void_p) for f in (
+        "cached", "fresh", "block_table", "free_pages", "free_count", "cu_q", "kv_len", "slots",
+        "positions", "free_left", "status")] + [("table_stride", ctypes.c_uint64)] + [
+        (f, ctypes.c_uint32) for f in (
+            "table_width", "free_capacity", "n", "tokens", "page_size", "pages")]
+
+
+class PrebaRopePositions(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_void_p) for f in (
+        "spans", "span_begin", "cached", "cu_q", "positions", "status")] + [
+        ("axis_stride", ctypes.c_uint64)] + [
+        (f, ctypes.c_uint32) for f in ("n_spans", "n", "tokens", "reserved")]
+
+
+class PrebaRopeAppend(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_void_p) for f in (
+        "q", "k", "v", "q_out", "k_cache", "v_cache", "positions", "slots", "inv_freq", "status")] + [
+        ("q_stride", ctypes.c_uint64 * 2), ("k_stride", ctypes.c_uint64 * 2),
+        ("v_stride", ctypes.c_uint64 * 2), ("q_out_stride", ctypes.c_uint64 * 2),
+        ("cache_stride", ctypes.c_uint64 * 3), ("axis_stride", ctypes.c_uint64),
+        ("sections", ctypes.c_uint32 * 3)] + [
+        (f, ctypes.c_uint32) for f in (
+            "tokens", "heads_q", "heads_kv", "head_dim", "rotary_dim", "pages", "page_size")] + [
+        ("dtype", ctypes.c_int32), ("flags", ctypes.c_uint32)]
+
+
+class PrebaPagesAttend(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_void_p) for f in (
+        "q", "k_cache", "v_cache", "block_table", "cu_q", "kv_len", "out", "lse", "workspace")] + [
+        ("workspace_bytes", ctypes.c_uint64), ("status", ctypes.c_void_p),
+        ("q_stride", ctypes.c_uint64 * 2), ("out_stride", ctypes.c_uint64 * 2),
+        ("k_stride", ctypes.c_uint64 * 3), ("v_stride", ctypes.c_uint64 * 3),
+        ("table_stride", ctypes.c_uint64)] + [
+        (f, ctypes.c_uint32) for f in (
+            "table_width", "n", "tokens", "max_q", "heads_q", "heads_kv", "head_dim", "pages",
+            "page_size", "window")] + [
+        ("dtype", ctypes.c_int32), ("flags", ctypes.c_uint32), ("scale", ctypes.c_float),
+        ("reserved", ctypes.c_uint32)]
 
 
 UTT_DTYPE = np.dtype([("offset", "<u8"), ("length", "<u4"), ("frames", "<u4")])
@@ -250,6 +293,14 @@ def lib() -> ctypes.CDLL:
         L.preba_jpeg_query.restype = ctypes.c_int
         L.preba_jpeg_decode.argtypes = [ctypes.POINTER(PrebaJpegBatch), ctypes.c_void_p]
         L.preba_jpeg_decode.restype = ctypes.c_int
+        L.preba_pages_attend_query.argtypes = [ctypes.c_uint32] * 5 + [u64p]
+        L.preba_pages_attend_query.restype = ctypes.c_int
+        for name, struct in (("preba_pages_plan", PrebaPagesPlan),
+                             ("preba_rope_positions", PrebaRopePositions),
+                             ("preba_rope_append", PrebaRopeAppend),
+                             ("preba_pages_attend", PrebaPagesAttend)):
+            getattr(L, name).argtypes = [ctypes.POINTER(struct), ctypes.c_void_p]
+            getattr(L, name).restype = ctypes.c_int
         L.preba_strerror.argtypes = [ctypes.c_int]
         L.preba_strerror.restype = ctypes.c_char_p
         L.preba_last_cuda_error.argtypes = []
@@ -929,3 +980,243 @@ class PreparedJpeg:
         rc = lib().preba_jpeg_decode(*self._args)
         if rc != OK:
             raise PrebaError(rc, "preba_jpeg_decode")
+
+
+# ---- serving step: pages, positions, rotation, attention -------------------------------------------
+
+ROPE_INTERLEAVED, ROPE_AXES_IN_TURN = 1, 2
+ATTEND_CAUSAL = 1
+PAGES_MAX_REQUESTS = 16384
+
+
+def _stream(stream) -> ctypes.c_void_p:
+    """A torch stream, a raw cudaStream_t or None for torch's current stream."""
+    if stream is None:
+        import torch
+
+        stream = torch.cuda.current_stream()
+    return ctypes.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
+
+
+def _ints(t, name: str, dims: int = 1):
+    """A CUDA int32 tensor of `dims` dimensions whose innermost is contiguous."""
+    import torch
+
+    if t.dtype != torch.int32 or t.dim() != dims or not t.is_cuda:
+        raise ValueError(f"{name} must be an int32 CUDA tensor with {dims} dimension(s)")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name} must be contiguous along its last dimension")
+    return t
+
+
+def _heads(t, name: str, dims: int, dtype=None):
+    """A CUDA tensor of 16-bit floats whose innermost dimension (the head's elements) is contiguous."""
+    import torch
+
+    if t.dtype not in (torch.float16, torch.bfloat16) or (dtype is not None and t.dtype != dtype):
+        raise ValueError(f"{name} must be float16 or bfloat16, the same as the other operands")
+    if t.dim() != dims or not t.is_cuda or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{name} must be a CUDA tensor with {dims} dimensions, the last contiguous")
+    if any(s < 0 for s in t.stride()):
+        raise ValueError(f"{name} has a negative stride")
+    return t
+
+
+def _same(name: str, got, want) -> None:
+    if tuple(got) != tuple(want):
+        raise ValueError(f"{name} has shape {tuple(got)}, expected {tuple(want)}")
+
+
+def _ptr(t):
+    return t.data_ptr() if t is not None else None
+
+
+def _code(t) -> int:
+    import torch
+
+    return F16 if t.dtype == torch.float16 else BF16
+
+
+class _Prepared:
+    """The arguments of one call, marshalled once; calling it enqueues the work."""
+
+    def _bind(self, name: str, struct, stream, keep) -> None:
+        self._name, self._call = name, getattr(lib(), name)
+        self._keep = (struct, keep)
+        self._args = (ctypes.byref(struct), _stream(stream))
+
+    def __call__(self) -> None:
+        rc = self._call(*self._args)
+        if rc != OK:
+            raise PrebaError(rc, self._name)
+
+
+class PreparedPagesPlan(_Prepared):
+    """``preba_pages_plan``, marshalled once.  All tensors are int32 CUDA tensors: ``cached``,
+    ``fresh``, ``kv_len`` [n], ``block_table`` [n, width], ``free_pages`` (the stack), ``free_count``
+    and ``free_left`` [1], ``cu_q`` [n + 1], ``slots`` and ``positions`` (or None) [tokens].  ``pages``
+    is the cache's page count (None: whatever 31-bit slots can name)."""
+
+    def __init__(self, cached, fresh, block_table, free_pages, free_count, page_size: int, cu_q,
+                 kv_len, slots, positions, free_left, pages: int | None = None, status=None,
+                 stream=None):
+        n = cached.numel()
+        _same("block_table", _ints(block_table, "block_table", 2).shape[:1], (n,))
+        for t, name, want in ((cached, "cached", n), (fresh, "fresh", n), (cu_q, "cu_q", n + 1),
+                              (kv_len, "kv_len", n), (free_count, "free_count", 1),
+                              (free_left, "free_left", 1)):
+            _same(name, _ints(t, name).shape, (want,))
+        _ints(free_pages, "free_pages"), _ints(slots, "slots")
+        if positions is not None:
+            _same("positions", _ints(positions, "positions").shape, slots.shape)
+        s = PrebaPagesPlan()
+        s.cached, s.fresh, s.block_table = _ptr(cached), _ptr(fresh), _ptr(block_table)
+        s.free_pages, s.free_count, s.cu_q = _ptr(free_pages), _ptr(free_count), _ptr(cu_q)
+        s.kv_len, s.slots, s.positions = _ptr(kv_len), _ptr(slots), _ptr(positions)
+        s.free_left, s.status = _ptr(free_left), _ptr(status)
+        s.table_stride, s.table_width = block_table.stride(0), block_table.shape[1]
+        s.free_capacity, s.n, s.tokens = free_pages.numel(), n, slots.numel()
+        s.page_size = page_size
+        s.pages = (2**31 - 1) // max(1, page_size) if pages is None else pages
+        self._bind("preba_pages_plan", s, stream,
+                   (cached, fresh, block_table, free_pages, free_count, cu_q, kv_len, slots,
+                    positions, free_left, status))
+
+
+def preba_pages_plan(*args, **kwargs) -> None:
+    """One ``preba_pages_plan`` call; the arguments are those of ``PreparedPagesPlan``."""
+    PreparedPagesPlan(*args, **kwargs)()
+
+
+class PreparedRopePositions(_Prepared):
+    """``preba_rope_positions``, marshalled once: ``spans`` int32 [m, 4] = {t, h, w, step} (h = 0:
+    text), ``span_begin`` [n + 1], ``cached`` [n], ``cu_q`` [n + 1], ``positions`` [3, tokens]."""
+
+    def __init__(self, spans, span_begin, cached, cu_q, positions, status=None, stream=None):
+        n = cached.numel()
+        _ints(spans, "spans", 2), _ints(positions, "positions", 2)
+        _same("spans", spans.shape, (spans.shape[0], 4))
+        if spans.shape[0] > 1 and spans.stride(0) != 4:
+            raise ValueError("spans must be contiguous")
+        _same("span_begin", _ints(span_begin, "span_begin").shape, (n + 1,))
+        _same("cached", _ints(cached, "cached").shape, (n,))
+        _same("cu_q", _ints(cu_q, "cu_q").shape, (n + 1,))
+        _same("positions", positions.shape[:1], (3,))
+        s = PrebaRopePositions()
+        s.spans, s.span_begin, s.cached = _ptr(spans), _ptr(span_begin), _ptr(cached)
+        s.cu_q, s.positions, s.status = _ptr(cu_q), _ptr(positions), _ptr(status)
+        s.axis_stride, s.n_spans, s.n = positions.stride(0), spans.shape[0], n
+        s.tokens = positions.shape[1]
+        self._bind("preba_rope_positions", s, stream,
+                   (spans, span_begin, cached, cu_q, positions, status))
+
+
+def preba_rope_positions(*args, **kwargs) -> None:
+    """One ``preba_rope_positions`` call; the arguments are those of ``PreparedRopePositions``."""
+    PreparedRopePositions(*args, **kwargs)()
+
+
+class PreparedRopeAppend(_Prepared):
+    """``preba_rope_append``, marshalled once.  ``q``, ``q_out`` [tokens, heads_q, d], ``k``, ``v``
+    [tokens, heads_kv, d] (views of one projection's output will do), caches [pages, page_size,
+    heads_kv, d] with any strides over a contiguous last dimension, ``positions`` int32 [3, tokens]
+    (or an expanded row), ``slots`` int32 [tokens], ``inv_freq`` float64 [rotary_dim/2],
+    ``sections`` the pairs that turn with time, height and width."""
+
+    def __init__(self, q, k, v, positions, inv_freq, sections, slots, q_out, k_cache, v_cache,
+                 interleaved: bool = False, axes_in_turn: bool = False, status=None, stream=None):
+        import torch
+
+        _heads(q, "q", 3)
+        tokens, hq, d = q.shape
+        _heads(k, "k", 3, q.dtype), _heads(v, "v", 3, q.dtype), _heads(q_out, "q_out", 3, q.dtype)
+        _heads(k_cache, "k_cache", 4, q.dtype), _heads(v_cache, "v_cache", 4, q.dtype)
+        hk = k.shape[1]
+        _same("k", k.shape, (tokens, hk, d))
+        _same("v", v.shape, (tokens, hk, d))
+        _same("q_out", q_out.shape, (tokens, hq, d))
+        _same("k_cache", k_cache.shape[2:], (hk, d))
+        _same("v_cache", v_cache.shape, k_cache.shape)
+        if v_cache.stride() != k_cache.stride():
+            raise ValueError("k_cache and v_cache must have the same strides")
+        _same("positions", _ints(positions, "positions", 2).shape, (3, tokens))
+        _same("slots", _ints(slots, "slots").shape, (tokens,))
+        if inv_freq.dtype != torch.float64 or not inv_freq.is_cuda or not inv_freq.is_contiguous():
+            raise ValueError("inv_freq must be a contiguous float64 CUDA tensor")
+        if len(sections) != 3:
+            raise ValueError("sections must have 3 entries")
+        s = PrebaRopeAppend()
+        s.q, s.k, s.v, s.q_out = _ptr(q), _ptr(k), _ptr(v), _ptr(q_out)
+        s.k_cache, s.v_cache, s.positions = _ptr(k_cache), _ptr(v_cache), _ptr(positions)
+        s.slots, s.inv_freq, s.status = _ptr(slots), _ptr(inv_freq), _ptr(status)
+        s.q_stride[:], s.k_stride[:], s.v_stride[:] = q.stride()[:2], k.stride()[:2], v.stride()[:2]
+        s.q_out_stride[:], s.cache_stride[:] = q_out.stride()[:2], k_cache.stride()[:3]
+        s.axis_stride, s.sections[:] = positions.stride(0), sections
+        s.tokens, s.heads_q, s.heads_kv, s.head_dim = tokens, hq, hk, d
+        s.rotary_dim = 2 * inv_freq.numel()
+        s.pages, s.page_size = k_cache.shape[:2]
+        s.dtype = _code(q)
+        s.flags = (ROPE_INTERLEAVED if interleaved else 0) | (ROPE_AXES_IN_TURN if axes_in_turn else 0)
+        self._bind("preba_rope_append", s, stream,
+                   (q, k, v, positions, inv_freq, slots, q_out, k_cache, v_cache, status))
+
+
+def preba_rope_append(*args, **kwargs) -> None:
+    """One ``preba_rope_append`` call; the arguments are those of ``PreparedRopeAppend``."""
+    PreparedRopeAppend(*args, **kwargs)()
+
+
+def preba_pages_attend_query(n: int, tokens: int, heads_q: int, heads_kv: int, head_dim: int) -> int:
+    """Bytes of workspace that ``preba_pages_attend`` needs at these sizes (zeroed once)."""
+    out = ctypes.c_uint64()
+    rc = lib().preba_pages_attend_query(n, tokens, heads_q, heads_kv, head_dim, ctypes.byref(out))
+    if rc != OK:
+        raise PrebaError(rc, "preba_pages_attend_query")
+    return int(out.value)
+
+
+class PreparedPagesAttend(_Prepared):
+    """``preba_pages_attend``, marshalled once.  ``q``, ``out`` [tokens, heads_q, d], caches [pages,
+    page_size, heads_kv, d] with any strides over a contiguous last dimension, ``block_table`` int32
+    [n, width], ``cu_q`` [n + 1], ``kv_len`` [n], ``workspace`` a zeroed CUDA tensor of
+    ``preba_pages_attend_query`` bytes, ``lse`` float32 [tokens, heads_q] or None."""
+
+    def __init__(self, q, k_cache, v_cache, block_table, cu_q, kv_len, out, workspace, max_q: int,
+                 scale: float, causal: bool = True, window: int = 0, lse=None, status=None,
+                 stream=None):
+        import torch
+
+        _heads(q, "q", 3)
+        tokens, hq, d = q.shape
+        _heads(out, "out", 3, q.dtype)
+        _heads(k_cache, "k_cache", 4, q.dtype), _heads(v_cache, "v_cache", 4, q.dtype)
+        _same("out", out.shape, q.shape)
+        _same("k_cache", k_cache.shape[3:], (d,))
+        _same("v_cache", v_cache.shape, k_cache.shape)
+        n = kv_len.numel()
+        _same("block_table", _ints(block_table, "block_table", 2).shape[:1], (n,))
+        _same("cu_q", _ints(cu_q, "cu_q").shape, (n + 1,))
+        _same("kv_len", _ints(kv_len, "kv_len").shape, (n,))
+        if lse is not None:
+            _same("lse", lse.shape, (tokens, hq))
+            if lse.dtype != torch.float32 or not lse.is_contiguous():
+                raise ValueError("lse must be a contiguous float32 tensor")
+        s = PrebaPagesAttend()
+        s.q, s.k_cache, s.v_cache, s.out = _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(out)
+        s.block_table, s.cu_q, s.kv_len = _ptr(block_table), _ptr(cu_q), _ptr(kv_len)
+        s.lse, s.workspace, s.status = _ptr(lse), _ptr(workspace), _ptr(status)
+        s.workspace_bytes = workspace.numel() * workspace.element_size()
+        s.q_stride[:], s.out_stride[:] = q.stride()[:2], out.stride()[:2]
+        s.k_stride[:], s.v_stride[:] = k_cache.stride()[:3], v_cache.stride()[:3]
+        s.table_stride, s.table_width = block_table.stride(0), block_table.shape[1]
+        s.n, s.tokens, s.max_q, s.heads_q, s.heads_kv = n, tokens, max_q, hq, k_cache.shape[2]
+        s.head_dim, s.pages, s.page_size = d, k_cache.shape[0], k_cache.shape[1]
+        s.window, s.dtype, s.scale = window, _code(q), scale
+        s.flags = ATTEND_CAUSAL if causal else 0
+        self._bind("preba_pages_attend", s, stream,
+                   (q, k_cache, v_cache, block_table, cu_q, kv_len, out, lse, workspace, status))
+
+
+def preba_pages_attend(*args, **kwargs) -> None:
+    """One ``preba_pages_attend`` call; the arguments are those of ``PreparedPagesAttend``."""
+    PreparedPagesAttend(*args, **kwargs)()
