@@ -1,0 +1,109 @@
+// Shared by the two attention kernels (preba_attend.cu): requests, barriers, tensor copies.
+#ifndef PREBA_ATTEND_H_
+#define PREBA_ATTEND_H_
+
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include "preba_internal.h"
+#include "preba_tokens.h"
+
+namespace preba {
+namespace attend {
+
+constexpr uint32_t kFull = 0xffffffffu;
+constexpr uint32_t kSpinLimit = 1u << 20;  // polls of one wait
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kMaxSplitCtas = 2 * 160;  // CTAs that may share a request's keys (2 per SM)
+
+__device__ __forceinline__ void report(int32_t* status, int32_t code) {
+  if (status) atomicCAS(status, 0, code);
+}
+
+// What a request's rows and keys are, checked.  False: the request is skipped.
+struct request_t {
+  int32_t row, rows, keys;  // first row, rows, keys
+};
+__device__ __forceinline__ bool load_request(const preba_pages_attend_t& p, uint32_t r, request_t& q) {
+  const int32_t a = p.cu_q[r], b = p.cu_q[r + 1], kv = p.kv_len[r];
+  q.row = a;
+  q.rows = b - a;
+  q.keys = kv;
+  return !(a < 0 || b < a || static_cast<uint32_t>(b) > p.tokens || static_cast<uint32_t>(b - a) > p.max_q ||
+           kv < 0 || static_cast<uint64_t>(kv) > static_cast<uint64_t>(p.table_width) * p.page_size);
+}
+
+// Rows j0 .. j1-1 of a request see keys in [lo, hi) and no others (each row its own part of them).
+__device__ __forceinline__ void seen_by(const preba_pages_attend_t& p, const request_t& q, int32_t j0,
+                                        int32_t j1, int32_t& lo, int32_t& hi) {
+  const int32_t at0 = q.keys - q.rows;  // place of row 0; may be negative
+  hi = (p.flags & PREBA_ATTEND_CAUSAL) ? max(0, min(q.keys, at0 + j1)) : q.keys;
+  lo = p.window ? static_cast<int32_t>(max(static_cast<int64_t>(0),
+                                           static_cast<int64_t>(at0) + j0 + 1 - p.window)) : 0;
+}
+
+// ---- shared-memory barriers and tensor copies (PTX) ------------------------------------------
+
+__device__ __forceinline__ uint32_t smem_addr(const void* ptr) {
+  return static_cast<uint32_t>(__cvta_generic_to_shared(ptr));
+}
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive_expect_tx(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes)
+               : "memory");
+}
+__device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+// Waits for the phase with the given parity to complete; false if the limit ran out.
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
+  for (uint32_t it = 0; it < kSpinLimit; ++it)
+    if (mbar_try_wait(bar, parity)) return true;
+  return false;
+}
+
+// One box of a four-dimensional tensor into shared memory.
+__device__ __forceinline__ void tensor_copy(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y,
+                                            int32_t z, int32_t w, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes "
+      "[%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+      "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
+      : "memory");
+}
+
+__device__ __forceinline__ float exp2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+template <typename T> __device__ __forceinline__ uint32_t pack2(float a, float b);
+template <> __device__ __forceinline__ uint32_t pack2<__half>(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float a, float b) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+}  // namespace attend
+}  // namespace preba
+
+#endif  // PREBA_ATTEND_H_
