@@ -9,14 +9,6 @@ namespace {
 
 using namespace attend;
 
-template <typename T> __device__ __forceinline__ float2 open2(uint32_t v);
-template <> __device__ __forceinline__ float2 open2<__half>(uint32_t v) {
-  return __half22float2(*reinterpret_cast<const __half2*>(&v));
-}
-template <> __device__ __forceinline__ float2 open2<__nv_bfloat16>(uint32_t v) {
-  return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
-}
-
 // ---- few rows: at most 16 (token, head) rows on a key head -----------------------------------------
 //
 // Such a step has to read the keys and values once and does 4 flops per byte and row with them, far
@@ -28,6 +20,7 @@ template <> __device__ __forceinline__ float2 open2<__nv_bfloat16>(uint32_t v) {
 // timing does not change a bit.  Within a tile each of the four warps takes 16 keys with a running maximum
 // and sum of its own; the warps are joined once per (request, key head).
 
+constexpr uint64_t kCounterBytes = kMaxSplitCtas * 4;  // at the workspace's start
 constexpr int kRowsMax = 16;
 constexpr int kTileKeys = 64;
 constexpr int kWarps = 4;                      // of consumers; one more warp issues the copies
@@ -460,7 +453,7 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
         store_rows<T, DP / 8>(a, w.q, w.head, o, l, m, 0);
       } else {
         const uint32_t slot = w.tile == 0;
-        float* to = reinterpret_cast<float*>(static_cast<uint8_t*>(p.workspace) + kMaxSplitCtas * 4 +
+        float* to = reinterpret_cast<float*>(static_cast<uint8_t*>(p.workspace) + kCounterBytes +
                                              static_cast<uint64_t>(2 * blockIdx.x + slot) * L::kPartial);
 #pragma unroll
         for (int n = 0; n < DP / 8; ++n)
@@ -501,7 +494,7 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
   for (int i = 0; i < 2; ++i) {
     if (!ctl.joins[i]) continue;
     const piece_t x = ctl.pieces[i];
-    const uint8_t* partials = static_cast<const uint8_t*>(p.workspace) + kMaxSplitCtas * 4;
+    const uint8_t* partials = static_cast<const uint8_t*>(p.workspace) + kCounterBytes;
     // the first CTA's piece begins the (request, key head): slot 1; the others lie in slot 0
     auto at = [&](uint32_t cta) {
       return reinterpret_cast<const float*>(
@@ -536,92 +529,6 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
   }
 }
 
-// One warp per (request, row, query head): 32 keys at a time, one per lane, then the values with an
-// element per lane.
-template <typename T>
-__global__ void __launch_bounds__(128)
-attend_kernel(const preba_pages_attend_t p, const uint32_t page_shift) {
-  const uint32_t lane = threadIdx.x & 31;
-  const uint64_t unit = (static_cast<uint64_t>(blockIdx.x) * 128 + threadIdx.x) >> 5;
-  if (unit >= static_cast<uint64_t>(p.tokens) * p.heads_q) return;
-  const uint32_t token = static_cast<uint32_t>(unit / p.heads_q), head = unit % p.heads_q;
-  // the request that owns the token
-  uint32_t r = 0;
-  for (; r < p.n; ++r)
-    if (p.cu_q[r + 1] > static_cast<int64_t>(token)) break;
-  request_t q;
-  if (r == p.n) return;
-  if (!load_request(p, r, q)) {
-    report(p.status, PREBA_ERR_BAD_TABLE);
-    return;
-  }
-  if (static_cast<uint32_t>(q.row) > token) return;
-  const int64_t at = static_cast<int64_t>(q.keys) - q.rows + (token - q.row);
-  int64_t k1 = q.keys, k0 = 0;
-  if (p.flags & PREBA_ATTEND_CAUSAL) k1 = min(k1, at + 1);
-  if (p.window) k0 = max(k0, at - p.window + 1);
-  const uint32_t head_kv = head / (p.heads_q / p.heads_kv);
-  const T* qp = static_cast<const T*>(p.q) + token * p.q_stride[0] + head * p.q_stride[1];
-  float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int64_t k = k0; k < k1; k += 32) {
-    const int64_t mine = k + lane;
-    float s = -INFINITY;
-    uint64_t v_at = 0;
-    if (mine < k1) {
-      const int32_t page = p.block_table[r * p.table_stride + (mine >> page_shift)];
-      const uint32_t in = static_cast<uint32_t>(mine) & (p.page_size - 1);
-      if (page < 0 || static_cast<uint32_t>(page) >= p.pages) {
-        report(p.status, PREBA_ERR_BAD_TABLE);
-        v_at = ~0ull;
-        s = 0.f;
-      } else {
-        const T* kp = static_cast<const T*>(p.k_cache) + page * p.k_stride[0] + in * p.k_stride[1] +
-                      head_kv * p.k_stride[2];
-        v_at = page * p.v_stride[0] + in * p.v_stride[1] + head_kv * p.v_stride[2];
-        float sum = 0.f;
-        for (uint32_t e = 0; e < p.head_dim; e += 8) {
-          const uint4 x = *reinterpret_cast<const uint4*>(qp + e);
-          const uint4 y = *reinterpret_cast<const uint4*>(kp + e);
-          const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float2 a = open2<T>(xs[i]), b = open2<T>(ys[i]);
-            sum = fmaf(a.x, b.x, fmaf(a.y, b.y, sum));
-          }
-        }
-        s = sum * p.scale;
-      }
-    }
-    float top = s;
-#pragma unroll
-    for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, d));
-    top = fmaxf(top, m);
-    const float keep = expf(m - top), e = mine < k1 ? expf(s - top) : 0.f;
-    m = top;
-    float sum = e;
-#pragma unroll
-    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(kFull, sum, d);
-    l = l * keep + sum;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] *= keep;
-    for (int j = 0; j < 32 && k + j < k1; ++j) {
-      const float w = __shfl_sync(kFull, e, j);
-      const uint64_t base = __shfl_sync(kFull, v_at, j);
-      if (base == ~0ull) continue;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (lane + 32 * i < p.head_dim)
-          o[i] = fmaf(w, static_cast<float>(static_cast<const T*>(p.v_cache)[base + lane + 32 * i]), o[i]);
-    }
-  }
-  T* to = static_cast<T*>(p.out) + token * p.out_stride[0] + head * p.out_stride[1];
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (lane + 32 * i < p.head_dim) to[lane + 32 * i] = static_cast<T>(l > 0.f ? o[i] / l : 0.f);
-  if (p.lse && lane == 0)
-    p.lse[static_cast<uint64_t>(token) * p.heads_q + head] = l > 0.f ? m + logf(l) : -INFINITY;
-}
-
 int finish(cudaError_t err) {
   if (err == cudaSuccess) return PREBA_OK;
   g_last_cuda_error = static_cast<int>(err);
@@ -634,10 +541,12 @@ bool sizes_ok(uint32_t n, uint32_t tokens, uint32_t heads_q, uint32_t heads_kv, 
          head_dim >= 8 && head_dim % 8 == 0 && head_dim <= PREBA_PAGES_MAX_HEAD_DIM;
 }
 
-// The workspace: a counter per CTA, then two partial sums of the widest kind per CTA.
-uint64_t workspace_of(uint32_t head_dim) {
-  return kMaxSplitCtas * 4ull +
-         2ull * kMaxSplitCtas * (head_dim <= 64 ? few_layout<64>::kPartial : few_layout<128>::kPartial);
+// The workspace: a counter per CTA of the kernel for few rows, which every call leaves zeroed; then what
+// one call needs, partial sums of that kernel or the list and the partial sums of the other.
+uint64_t workspace_of(uint32_t n, uint32_t tokens, uint32_t group, uint32_t head_dim) {
+  const uint64_t few = 2ull * kMaxSplitCtas * (head_dim <= 64 ? few_layout<64>::kPartial
+                                                              : few_layout<128>::kPartial);
+  return kCounterBytes + std::max(few, tiles_workspace(n, tokens, group, head_dim));
 }
 
 // cuTensorMapEncodeTiled, found through the runtime so that the library needs no libcuda to load.
@@ -660,23 +569,38 @@ cudaError_t encoder(encode_fn* fn) {
   return cudaSuccess;
 }
 
-// Boxes of 64 elements x box_rows slots of one head of one page; elements past head_dim read as 0.
-cudaError_t cache_map(CUtensorMap* map, const preba_pages_attend_t& p, const void* cache,
-                      const uint64_t* strides, uint32_t box_rows) {
+}  // namespace
+
+namespace attend {
+
+cudaError_t tensor_map(CUtensorMap* map, int dtype, const void* base, const uint64_t* dims,
+                       const uint64_t* strides, const uint32_t* box) {
   encode_fn encode;
   const cudaError_t err = encoder(&encode);
   if (err != cudaSuccess) return err;
-  const cuuint64_t dims[4] = {p.head_dim, p.page_size, p.heads_kv, p.pages};
+  const cuuint64_t extent[4] = {dims[0], dims[1], dims[2], dims[3]};
+  cuuint64_t bytes[3];
   // the stride of an axis of one entry is never used: any valid one will do
-  const cuuint64_t bytes[3] = {2 * strides[1], 2 * (p.heads_kv > 1 ? strides[2] : strides[1]),
-                               2 * (p.pages > 1 ? strides[0] : strides[1])};
-  const cuuint32_t box[4] = {64, box_rows, 1, 1}, step[4] = {1, 1, 1, 1};
+  for (int i = 0; i < 3; ++i) bytes[i] = dims[i + 1] > 1 ? 2 * strides[i] : 16;
+  const cuuint32_t boxes[4] = {64, box[0], box[1], 1}, step[4] = {1, 1, 1, 1};
   const CUresult rc = encode(
-      map, p.dtype == PREBA_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4,
-      const_cast<void*>(cache), dims, bytes, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+      map, dtype == PREBA_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4,
+      const_cast<void*>(base), extent, bytes, boxes, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
       CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return rc == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
+
+cudaError_t cache_map(CUtensorMap* map, const preba_pages_attend_t& p, const void* cache,
+                      const uint64_t* strides, uint32_t box_rows) {
+  const uint64_t dims[4] = {p.head_dim, p.page_size, p.heads_kv, p.pages};
+  const uint64_t order[3] = {strides[1], strides[2], strides[0]};
+  const uint32_t box[2] = {box_rows, 1};
+  return tensor_map(map, p.dtype, cache, dims, order, box);
+}
+
+}  // namespace attend
+
+namespace {
 
 template <typename T, int DP>
 cudaError_t launch_few(const few_args& a, int sms, cudaStream_t stream) {
@@ -699,13 +623,14 @@ bool operand_ok(const void* base, const uint64_t* strides, int count) {
   return true;
 }
 
-// An axis of the caches with more than one entry has a stride (tensor copies know no other kind).
+// An axis of the queries and caches with more than one entry has a stride (tensor copies know no other kind).
 bool strides_used(const preba_pages_attend_t& p) {
   for (const uint64_t* s : {p.k_stride, p.v_stride})
     if (s[1] == 0 || (p.heads_kv > 1 && s[2] == 0) || (p.pages > 1 && s[0] == 0) ||
         std::max({s[0], s[1], s[2]}) >= (1ull << 38))
       return false;
-  return true;
+  return (p.heads_q == 1 || p.q_stride[1]) && (p.tokens == 1 || p.q_stride[0]) &&
+         std::max(p.q_stride[0], p.q_stride[1]) < (1ull << 38);
 }
 
 }  // namespace
@@ -715,7 +640,7 @@ extern "C" int preba_pages_attend_query(uint32_t n, uint32_t tokens, uint32_t he
                                         uint32_t head_dim, uint64_t* workspace_bytes) {
   using namespace preba;
   if (!workspace_bytes || !sizes_ok(n, tokens, heads_q, heads_kv, head_dim)) return PREBA_ERR_INVALID_ARG;
-  *workspace_bytes = workspace_of(head_dim);
+  *workspace_bytes = workspace_of(n, tokens, heads_q / heads_kv, head_dim);
   return PREBA_OK;
 }
 
@@ -734,12 +659,10 @@ extern "C" int preba_pages_attend(const preba_pages_attend_t* req, void* stream)
       !(p.scale > 0.f) || !(p.scale < INFINITY))
     return PREBA_ERR_INVALID_ARG;
   if (!p.workspace || (reinterpret_cast<uintptr_t>(p.workspace) & 15)) return PREBA_ERR_INVALID_ARG;
-  if (p.workspace_bytes < workspace_of(p.head_dim)) return PREBA_ERR_BUFFER_TOO_SMALL;
-  const uint64_t units = static_cast<uint64_t>(p.tokens) * p.heads_q;
-  const uint32_t shift = 31 - __builtin_clz(p.page_size);
-  const uint32_t grid = static_cast<uint32_t>((units + 3) / 4);
-  cudaStream_t s = static_cast<cudaStream_t>(stream);
   const uint32_t group = p.heads_q / p.heads_kv;
+  if (p.workspace_bytes < workspace_of(p.n, p.tokens, group, p.head_dim)) return PREBA_ERR_BUFFER_TOO_SMALL;
+  const uint32_t shift = 31 - __builtin_clz(p.page_size);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
   int device = 0, sms = 0;
   cudaError_t err = cudaGetDevice(&device);
   if (err == cudaSuccess) err = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
@@ -752,9 +675,5 @@ extern "C" int preba_pages_attend(const preba_pages_attend_t* req, void* stream)
     return finish(p.head_dim <= 64 ? launch_few<__nv_bfloat16, 64>(a, sms, s)
                                    : launch_few<__nv_bfloat16, 128>(a, sms, s));
   }
-  if (p.dtype == PREBA_F16)
-    attend_kernel<__half><<<grid, 128, 0, s>>>(p, shift);
-  else
-    attend_kernel<__nv_bfloat16><<<grid, 128, 0, s>>>(p, shift);
-  return finish(cudaGetLastError());
+  return finish(launch_tiles(p, shift, sms, static_cast<uint8_t*>(p.workspace) + kCounterBytes, s));
 }

@@ -16,7 +16,21 @@ namespace attend {
 constexpr uint32_t kFull = 0xffffffffu;
 constexpr uint32_t kSpinLimit = 1u << 20;  // polls of one wait
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int kMaxSplitCtas = 2 * 160;  // CTAs that may share a request's keys (2 per SM)
+constexpr int kMaxTileCtas = 160;                // of the kernel for many rows: one per SM
+constexpr int kMaxSplitCtas = 2 * kMaxTileCtas;  // of the kernel for few rows: two per SM
+
+// Tensor maps of four axes, 16-bit elements, boxes of 64 elements x box[0] x box[1] x 1 in the 128-byte
+// swizzle; what lies outside the tensor reads as 0.  Strides in elements, of axes 1 to 3.
+cudaError_t tensor_map(CUtensorMap* map, int dtype, const void* base, const uint64_t* dims,
+                       const uint64_t* strides, const uint32_t* box);
+// The cache: boxes of box_rows slots of one head of one page.
+cudaError_t cache_map(CUtensorMap* map, const preba_pages_attend_t& p, const void* cache,
+                      const uint64_t* strides, uint32_t box_rows);
+
+// The kernel for many rows (preba_attend_tiles.cu): its workspace and its launches.
+uint64_t tiles_workspace(uint32_t n, uint32_t tokens, uint32_t group, uint32_t head_dim);
+cudaError_t launch_tiles(const preba_pages_attend_t& p, uint32_t page_shift, int sms, void* workspace,
+                         cudaStream_t stream);
 
 __device__ __forceinline__ void report(int32_t* status, int32_t code) {
   if (status) atomicCAS(status, 0, code);

@@ -1,0 +1,867 @@
+// Attention of many rows over the paged cache on the 5th-generation tensor cores: the second kernel
+// of preba_pages_attend (the first, for few rows, is in preba_attend.cu).
+//
+// Rows are (token, query head) pairs of one key head: all heads of a group share the keys, so a tile of
+// 128 rows holds floor(128 / group) tokens.  A CTA works on two such tiles, A and B, and streams the
+// keys and values they see through a ring of 128-key slots:
+//   S = Q K^T  (tcgen05, both operands in shared memory, S in tensor memory)
+//   P = exp2(scale log2(e) S - m), written over S in the 16-bit type, row sums in fp32 registers
+//   O += P V   (tcgen05, P from tensor memory, V from shared memory as it lies: rows are keys)
+// Two groups of four warps, a thread per row, do the exponentials of A and B while the tensor cores work
+// on the other tile.  The accumulator O stays in tensor memory; it is multiplied only when a row's
+// maximum has grown by more than 2^8 since the last time (until then P is at most 2^8 and the sums
+// simply carry the old reference; the result is the same quotient).
+//
+// The work is a list of (request, pair of tiles, key head) with their numbers of key tiles.  If the
+// longest is short beside a CTA's share, CTAs claim them one by one, longest first.  Otherwise the
+// key tiles of all of them form one line, every CTA takes an equal run of it, and pieces that are not
+// whole leave partial sums which the last CTA to finish joins in the order of the keys.  Which, and
+// the list, is decided on the device by a planning kernel, as the lengths are there.
+#include <algorithm>
+
+#include <type_traits>
+
+#include "preba_attend.h"
+
+namespace preba {
+namespace {
+
+using namespace attend;
+
+constexpr int kTile = 128;             // rows of a tile, keys of a slot
+constexpr int kSoftWarps = 8;          // four per tile
+constexpr int kCopyWarp = 8, kMmaWarp = 9;
+constexpr int kThreads = 32 * 10;
+constexpr uint32_t kTmemColumns = 512;
+constexpr uint32_t kMinRun = 2;        // key tiles of a CTA's run in the line, at least
+constexpr float kGrowth = 8.f;         // log2 of what a row may outgrow its reference by
+
+template <int DP> struct layout {      // DP: head_dim rounded up to 64 or 128
+  static constexpr int kHalves = DP / 64;
+  static constexpr uint32_t kHalf = kTile * 128;            // 64 elements of 128 rows
+  static constexpr uint32_t kQ = kHalves * kHalf;           // a tile of queries
+  static constexpr uint32_t kSlot = kHalves * kHalf;        // a tile of keys, or of values
+  static constexpr int kSlots = DP == 128 ? 5 : 10;
+  static constexpr uint32_t kRing = 2 * kQ;
+  static constexpr uint32_t kBars = kRing + kSlots * kSlot;
+  static constexpr uint32_t kItems = kBars + 512;
+  static constexpr uint32_t kBytes = kItems + 512;
+  // tensor memory columns: S of A and B (P lies over them), O of A and B
+  static constexpr uint32_t kS = 0, kO = 256;
+};
+
+// A piece of work: key tiles [tile, tile + count) of a pair of row tiles on one key head.
+struct item_t {
+  int32_t count;                 // 0: no more
+  uint32_t request, head;
+  int32_t row, rows, keys;       // the request: first row, rows, keys
+  int32_t token;                 // first token of tile A within the request
+  int32_t lo, hi;                // keys that any row of the pair sees
+  int32_t tile;
+  int32_t first[2], last[2];     // key tiles of A and B within the piece: [first, last)
+  int32_t whole;                 // the piece is all of the pair's keys
+  uint32_t slot;                 // else: where its partial sums go
+};
+static_assert(sizeof(item_t) <= 128, "layout::kItems");
+
+// What the planning kernel leaves for the CTAs.
+struct tiles_head {
+  uint32_t next;      // claims
+  uint32_t n_pairs, units, claim, per;
+};
+
+struct tiles_args {
+  preba_pages_attend_t p;
+  uint32_t page_shift, group, tokens_per_tile, box_rows, box_shift, grid, max_pairs;
+  tiles_head* head;
+  uint32_t* joined;   // a counter per CTA: pieces finished of the pair that it holds the beginning of
+  uint4* pairs;       // request, pair within it, key tiles of the pairs before, key tiles
+  uint32_t* order;    // pairs, longest first
+  float* partials;    // two per CTA
+};
+
+struct pair_range {
+  int32_t lo, hi;                // keys
+  int32_t first[2], last[2];     // key tiles of A and B
+  int32_t begin, end;            // of both
+};
+__device__ __forceinline__ pair_range range_of(const tiles_args& a, const request_t& q, uint32_t pair) {
+  pair_range r;
+  r.lo = r.hi = 0;
+  r.begin = r.end = 0;
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    const int32_t j0 = (2 * pair + x) * a.tokens_per_tile;
+    const int32_t j1 = min(j0 + static_cast<int32_t>(a.tokens_per_tile), q.rows);
+    r.first[x] = r.last[x] = 0;
+    if (j0 >= j1) continue;  // only B
+    int32_t lo, hi;
+    seen_by(a.p, q, j0, j1, lo, hi);
+    lo = min(lo, max(0, q.keys - 1));  // rows behind all keys see nothing: one empty tile
+    r.first[x] = lo / kTile;
+    r.last[x] = max(r.first[x] + 1, (hi + kTile - 1) / kTile);
+    if (x == 0 || lo < r.lo) r.lo = lo;
+    r.hi = max(r.hi, hi);
+    if (x == 0 || r.first[x] < r.begin) r.begin = r.first[x];
+    r.end = max(r.end, r.last[x]);
+  }
+  return r;
+}
+
+// ---- the plan -------------------------------------------------------------------------------------
+
+constexpr int kPlanThreads = 1024;
+constexpr int kBins = 1024;
+
+__device__ __forceinline__ uint32_t block_exclusive(uint32_t v, uint32_t* warp_sums, uint32_t& total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint32_t incl = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t up = __shfl_up_sync(kFull, incl, o);
+    if (lane >= o) incl += up;
+  }
+  if (lane == 31) warp_sums[warp] = incl;
+  __syncthreads();
+  const uint32_t s = warp_sums[lane];
+  uint32_t up_to = s;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t up = __shfl_up_sync(kFull, up_to, o);
+    if (lane >= o) up_to += up;
+  }
+  total = __shfl_sync(kFull, up_to, 31);
+  const uint32_t before = __shfl_sync(kFull, up_to - s, warp);
+  __syncthreads();
+  return before + incl - v;
+}
+
+__global__ void __launch_bounds__(kPlanThreads) tiles_plan_kernel(const tiles_args a) {
+  extern __shared__ uint32_t pairs_before[];  // n + 1: pairs of the requests before
+  __shared__ uint32_t warp_sums[32], bins[kBins], longest;
+  const preba_pages_attend_t& p = a.p;
+  if (threadIdx.x == 0) longest = 0;
+  for (uint32_t b = threadIdx.x; b < kBins; b += kPlanThreads) bins[b] = 0;
+  for (uint32_t c = threadIdx.x; c < a.grid; c += kPlanThreads) a.joined[c] = 0;
+
+  const uint32_t per = (p.n + kPlanThreads - 1) / kPlanThreads;
+  const uint32_t r0 = min(threadIdx.x * per, p.n), r1 = min(r0 + per, p.n);
+  auto pairs_of = [&](uint32_t r) -> uint32_t {
+    request_t q;
+    if (!load_request(p, r, q)) {
+      report(p.status, PREBA_ERR_BAD_TABLE);
+      return 0;
+    }
+    return (q.rows + 2 * a.tokens_per_tile - 1) / (2 * a.tokens_per_tile);
+  };
+  uint32_t mine = 0;
+  for (uint32_t r = r0; r < r1; ++r) mine += pairs_of(r);
+  uint32_t n_pairs;
+  uint32_t at = block_exclusive(mine, warp_sums, n_pairs);
+  for (uint32_t r = r0; r < r1; ++r) {
+    pairs_before[r] = at;
+    at += pairs_of(r);
+  }
+  if (threadIdx.x == 0) pairs_before[p.n] = n_pairs;
+  __syncthreads();
+  // rows of different requests do not overlap in a valid step; if they do, the list ends early
+  if (n_pairs > a.max_pairs) {
+    if (threadIdx.x == 0) report(p.status, PREBA_ERR_BAD_TABLE);
+    n_pairs = a.max_pairs;
+  }
+  uint32_t total = 0;
+  for (uint32_t base = 0; base < n_pairs; base += kPlanThreads) {
+    const uint32_t i = base + threadIdx.x;
+    uint32_t tiles = 0, r = 0;
+    if (i < n_pairs) {
+      uint32_t lo = 0, hi = p.n;  // the last request with no more pairs before it than i
+      while (hi - lo > 1) {
+        const uint32_t mid = (lo + hi) / 2;
+        if (pairs_before[mid] <= i) lo = mid; else hi = mid;
+      }
+      r = lo;
+      request_t q;
+      load_request(p, r, q);
+      const pair_range range = range_of(a, q, i - pairs_before[r]);
+      tiles = range.end - range.begin;
+    }
+    uint32_t sum;
+    const uint32_t before = block_exclusive(tiles, warp_sums, sum);
+    if (i < n_pairs) {
+      a.pairs[i] = make_uint4(r, i - pairs_before[r], total + before, tiles);
+      atomicMax(&longest, tiles);
+    }
+    total += sum;
+  }
+  __syncthreads();
+  // claimed one by one if the longest is short beside a CTA's share of the line
+  const uint64_t units = static_cast<uint64_t>(total) * p.heads_kv;
+  const bool claim = 3ull * longest * a.grid <= units;
+  if (claim) {
+    const uint32_t top = max(longest, 1u);
+    auto bin_of = [&](uint32_t tiles) {  // longest first
+      return kBins - 1 - static_cast<uint32_t>(static_cast<uint64_t>(tiles) * (kBins - 1) / top);
+    };
+    for (uint32_t i = threadIdx.x; i < n_pairs; i += kPlanThreads) atomicAdd(&bins[bin_of(a.pairs[i].w)], 1);
+    __syncthreads();
+    uint32_t sum;
+    const uint32_t before = block_exclusive(bins[threadIdx.x], warp_sums, sum);
+    bins[threadIdx.x] = before;
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < n_pairs; i += kPlanThreads)
+      a.order[atomicAdd(&bins[bin_of(a.pairs[i].w)], 1)] = i;
+  }
+  if (threadIdx.x == 0) {
+    tiles_head h;
+    h.next = 0;
+    h.n_pairs = n_pairs;
+    h.units = static_cast<uint32_t>(units);
+    h.claim = claim;
+    h.per = max(kMinRun, static_cast<uint32_t>((units + a.grid - 1) / a.grid));
+    *a.head = h;
+  }
+}
+static_assert(kBins == kPlanThreads, "one bin per thread in the sum");
+
+// ---- tensor core instructions (PTX) ---------------------------------------------------------------
+
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+// Shared-memory operand: rows of 128 bytes in the 128-byte swizzle, eight rows to a group.  `leading`
+// is the distance between 64-element columns of an operand whose rows are not its contraction axis,
+// `stride` the one between groups of eight rows.
+__device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t leading, uint32_t stride) {
+  return static_cast<uint64_t>((addr & 0x3ffff) >> 4) | static_cast<uint64_t>(leading >> 4) << 16 |
+         static_cast<uint64_t>(stride >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+// fp32 accumulator, 128 rows, `columns` columns; values: the second operand's rows are contracted.
+template <typename T> __device__ __forceinline__ constexpr uint32_t shape(uint32_t columns, bool values) {
+  const uint32_t kind = sizeof(T) == 2 && !std::is_same<T, __half>::value ? 1 : 0;  // bfloat16 : binary16
+  return 1u << 4 | kind << 7 | kind << 10 | (values ? 1u << 16 : 0u) | (columns / 8) << 17 | (kTile / 16) << 24;
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc),
+      "r"(add)
+      : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc),
+      "r"(add)
+      : "memory");
+}
+// Arrives at the barrier when all matrix products issued before have finished.
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar)
+               : "memory");
+}
+
+#define PREBA_R8(v, i) "+r"(v[i]), "+r"(v[i + 1]), "+r"(v[i + 2]), "+r"(v[i + 3]), "+r"(v[i + 4]), \
+    "+r"(v[i + 5]), "+r"(v[i + 6]), "+r"(v[i + 7])
+#define PREBA_I8(v, i) "r"(v[i]), "r"(v[i + 1]), "r"(v[i + 2]), "r"(v[i + 3]), "r"(v[i + 4]), \
+    "r"(v[i + 5]), "r"(v[i + 6]), "r"(v[i + 7])
+#define PREBA_L32 "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24," \
+    "%25,%26,%27,%28,%29,%30,%31}"
+// 32 columns of the thread's row.  The registers hold them once tmem_loaded() has returned.
+__device__ __forceinline__ void tmem_load32(uint32_t* v, uint32_t addr) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 " PREBA_L32 ", [%32];"
+               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]),
+                 "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]),
+                 "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]),
+                 "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]),
+                 "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+               : "r"(addr)
+               : "memory");
+}
+// Nothing that uses the 32 registers moves above it.
+__device__ __forceinline__ void tmem_loaded(uint32_t* v) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : PREBA_R8(v, 0), PREBA_R8(v, 8), PREBA_R8(v, 16), PREBA_R8(v, 24)::"memory");
+}
+__device__ __forceinline__ void tmem_store32(uint32_t addr, const uint32_t* v) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], " PREBA_L32 ";" ::PREBA_I8(v, 0), PREBA_I8(v, 8),
+               PREBA_I8(v, 16), PREBA_I8(v, 24), "r"(addr)
+               : "memory");
+}
+__device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// ---- the kernel -----------------------------------------------------------------------------------
+
+// A counter of ring slots with the parity that a wait for its next use takes.
+template <int N> struct ring {
+  uint32_t slot = 0, phase = 0;
+  __device__ __forceinline__ void step() {
+    if (++slot == N) slot = 0, phase ^= 1;
+  }
+};
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(kThreads, 1)
+tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+             const __grid_constant__ CUtensorMap map_v, const __grid_constant__ tiles_args a) {
+  using L = layout<DP>;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const preba_pages_attend_t& p = a.p;
+  const int lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(kFull, threadIdx.x >> 5, 0);
+  const uint32_t base = smem_addr(smem);
+  const uint32_t kv_full = base + L::kBars, kv_empty = kv_full + 8 * L::kSlots;
+  const uint32_t q_full = kv_empty + 8 * L::kSlots, q_empty = q_full + 8;
+  const uint32_t s_full = q_empty + 8, p_full = s_full + 16, o_full = p_full + 16;  // A, B each
+  const uint32_t item_full = o_full + 16, item_empty = item_full + 16;             // two slots each
+  const uint32_t drained = item_empty + 16;
+  static_assert(8 * (2 * L::kSlots + 13) + 8 <= 512, "layout::kItems");
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + L::kBars + 504);
+  item_t* items = reinterpret_cast<item_t*>(smem + L::kItems);
+  uint32_t* joins = reinterpret_cast<uint32_t*>(smem + L::kItems + 2 * sizeof(item_t));  // 2 + 2 x 4 words
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < L::kSlots; ++s) {
+      mbar_init(kv_full + 8 * s, 1);
+      mbar_init(kv_empty + 8 * s, 1);
+    }
+    mbar_init(q_full, 1);
+    mbar_init(q_empty, 1);
+    for (int x = 0; x < 2; ++x) {
+      mbar_init(s_full + 8 * x, 1);
+      mbar_init(p_full + 8 * x, kTile);
+      mbar_init(o_full + 8 * x, 1);
+      mbar_init(item_full + 8 * x, 1);
+      mbar_init(item_empty + 8 * x, kSoftWarps + 1);
+    }
+    mbar_init(drained, 1);
+    for (int i = 0; i < 10; ++i) joins[i] = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == kMmaWarp) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(tmem_slot)),
+                 "n"(kTmemColumns)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = *tmem_slot;
+  bool ok = true;
+
+  if (warp == kCopyWarp) {
+    // ---- work and copies
+    const tiles_head plan = *a.head;
+    const uint32_t boxes = kTile >> a.box_shift;
+    const uint32_t chunk = lane & (boxes - 1), half = lane / boxes;
+    const bool mine = half < L::kHalves;
+    const uint32_t dst = half * L::kHalf + (chunk << a.box_shift) * 128;
+    ring<L::kSlots> kv;
+    ring<1> q_ring;
+    ring<2> out;
+    uint32_t issued = 0, q_issued = 0;
+    uint32_t unit = min(static_cast<uint64_t>(blockIdx.x) * plan.per, static_cast<uint64_t>(plan.units));
+    const uint32_t unit_end = min(unit + plan.per, plan.units);
+    uint32_t pair = 0;
+    if (!plan.claim && unit < unit_end) {  // the pair that the run begins in
+      uint32_t lo = 0, hi = plan.n_pairs;
+      while (hi - lo > 1) {
+        const uint32_t mid = (lo + hi) / 2;
+        if (a.pairs[mid].z * p.heads_kv <= unit) lo = mid; else hi = mid;
+      }
+      pair = lo;
+    }
+    while (ok) {
+      // the next piece
+      item_t item;
+      item.count = 0;
+      uint4 of;
+      if (plan.claim) {
+        uint32_t k = 0;
+        if (lane == 0) k = atomicAdd(&a.head->next, 1);
+        k = __shfl_sync(kFull, k, 0);
+        if (k < plan.n_pairs * p.heads_kv) {
+          of = a.pairs[a.order[k / p.heads_kv]];
+          item.head = k % p.heads_kv;
+          item.count = of.w;
+          item.tile = 0;
+          item.whole = 1;
+          item.slot = 0;
+        }
+      } else if (unit < unit_end) {
+        of = a.pairs[pair];
+        const uint32_t offset = unit - of.z * p.heads_kv;
+        item.head = offset / of.w;
+        item.tile = offset - item.head * of.w;
+        item.count = min(of.w - item.tile, unit_end - unit);
+        item.whole = item.count == static_cast<int32_t>(of.w);
+        item.slot = 2 * blockIdx.x + (item.tile == 0);
+        if (!item.whole && lane == 0) {  // to be joined at the end
+          const uint32_t start = unit - item.tile;
+          uint32_t* j = joins + 2 + 4 * (item.tile == 0);
+          j[0] = 1;
+          j[1] = pair * p.heads_kv + item.head;
+          j[2] = start / plan.per;
+          j[3] = (start + of.w - 1) / plan.per;
+        }
+        unit += item.count;
+        if (offset + item.count == of.w * p.heads_kv) ++pair;
+      }
+      const bool done = item.count == 0;
+      if (!done) {
+        request_t q;
+        load_request(p, of.x, q);
+        const pair_range range = range_of(a, q, of.y);
+        item.request = of.x;
+        item.row = q.row;
+        item.rows = q.rows;
+        item.keys = q.keys;
+        item.token = 2 * of.y * a.tokens_per_tile;
+        item.lo = range.lo;
+        item.hi = range.hi;
+        item.tile += range.begin;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          item.first[x] = max(range.first[x], item.tile);
+          item.last[x] = max(item.first[x], min(range.last[x], item.tile + item.count));
+        }
+      }
+      ok = mbar_wait(item_empty + 8 * out.slot, out.phase ^ 1);
+      if (!ok) break;
+      if (lane == 0) {
+        items[out.slot] = item;
+        mbar_arrive(item_full + 8 * out.slot);
+      }
+      out.step();
+      if (done) break;
+      // queries
+      ok = mbar_wait(q_empty, q_ring.phase ^ 1);
+      if (!ok) break;
+      if (lane == 0) {
+        const uint32_t bytes = a.tokens_per_tile * a.group * 128 * L::kHalves;
+        const bool two = item.token + static_cast<int32_t>(a.tokens_per_tile) < item.rows;
+        mbar_arrive_expect_tx(q_full, two ? 2 * bytes : bytes);
+        for (int x = 0; x < (two ? 2 : 1); ++x)
+          for (int h = 0; h < L::kHalves; ++h)
+            tensor_copy(base + x * L::kQ + h * L::kHalf, &map_q, 64 * h, item.head * a.group,
+                        item.row + item.token + x * a.tokens_per_tile, 0, q_full);
+      }
+      ++q_issued;
+      q_ring.step();
+      // keys and values, tile by tile
+      const int32_t* row = p.block_table + static_cast<uint64_t>(item.request) * p.table_stride;
+      int32_t key = item.tile * kTile + (chunk << a.box_shift);
+      auto wanted = [&](int32_t k) {
+        return mine && k < item.hi && k + static_cast<int32_t>(a.box_rows) > item.lo;
+      };
+      int32_t entry = wanted(key) ? row[key >> a.page_shift] : 0;
+      for (int32_t t = 0; t < item.count && ok; ++t, key += kTile) {
+        int32_t page = entry;
+        const bool want = wanted(key);
+        if (t + 1 < item.count) entry = wanted(key + kTile) ? row[(key + kTile) >> a.page_shift] : 0;
+        if (want && (page < 0 || static_cast<uint32_t>(page) >= p.pages)) {
+          report(p.status, PREBA_ERR_BAD_TABLE);
+          page = p.pages;  // beyond the tensor: the box is filled with zeros
+        }
+        const uint32_t bytes = __popc(__ballot_sync(kFull, want)) * a.box_rows * 128;
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+          ok = ok && mbar_wait(kv_empty + 8 * kv.slot, kv.phase ^ 1);
+          if (!ok) break;
+          if (lane == 0) mbar_arrive_expect_tx(kv_full + 8 * kv.slot, bytes);
+          __syncwarp();
+          if (want)
+            tensor_copy(base + L::kRing + kv.slot * L::kSlot + dst, v ? &map_v : &map_k, half * 64,
+                        key & (p.page_size - 1), item.head, page, kv_full + 8 * kv.slot);
+          ++issued;
+          kv.step();
+        }
+      }
+    }
+    if (!ok) {  // what is in flight lands before the memory goes to another
+      report(p.status, PREBA_ERR_TIMEOUT);
+      for (uint32_t i = issued - min(issued, static_cast<uint32_t>(L::kSlots)); i < issued; ++i)
+        mbar_wait(kv_full + 8 * (i % L::kSlots), (i / L::kSlots) & 1);
+      if (q_issued) mbar_wait(q_full, (q_issued - 1) & 1);
+    }
+  } else if (warp == kMmaWarp) {
+    // ---- matrix products: one lane issues, the warp clears values that nobody sees
+    constexpr uint32_t kQkShape = shape<T>(kTile, false), kPvShape = shape<T>(DP, true);
+    ring<L::kSlots> kv;  // next slot to be waited for
+    ring<1> q_ring, p_ring[2];
+    ring<2> in;
+    while (ok) {
+      ok = mbar_wait(item_full + 8 * in.slot, in.phase);
+      if (!ok) break;
+      const item_t item = items[in.slot];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(item_empty + 8 * in.slot);
+      in.step();
+      if (item.count == 0) break;
+      ok = mbar_wait(q_full, q_ring.phase);
+      if (!ok) break;
+      q_ring.step();
+      const int32_t end = item.tile + item.count;
+      uint32_t k_slot = 0, v_slot = 0;
+      auto qk = [&](int x) {
+        const uint64_t q_op = operand(base + x * L::kQ, 16, 1024);
+        const uint64_t k_op = operand(base + L::kRing + k_slot * L::kSlot, 16, 1024);
+        if (lane == 0) {
+#pragma unroll
+          for (int ks = 0; ks < DP / 16; ++ks) {
+            const uint32_t off = (ks / 4) * L::kHalf + (ks % 4) * 32;
+            mma_ss(tmem + L::kS + x * kTile, q_op + (off >> 4), k_op + (off >> 4), kQkShape, ks > 0);
+          }
+          mma_commit(s_full + 8 * x);
+        }
+      };
+      auto pv = [&](int x, bool add) {
+        const uint64_t v_op = operand(base + L::kRing + v_slot * L::kSlot, L::kHalf, 1024);
+        if (lane == 0) {
+#pragma unroll
+          for (int ks = 0; ks < kTile / 16; ++ks)
+            mma_ts(tmem + L::kO + x * DP, tmem + L::kS + x * kTile + 8 * ks, v_op + (ks * 2048 >> 4), kPvShape,
+                   add || ks > 0);
+        }
+      };
+      // keys of the first tile
+      ok = mbar_wait(kv_full + 8 * kv.slot, kv.phase);
+      if (!ok) break;
+      fence_after();
+      k_slot = kv.slot;
+      kv.step();
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+        if (item.first[x] == item.tile && item.first[x] < item.last[x]) qk(x);
+      if (lane == 0) {
+        mma_commit(kv_empty + 8 * k_slot);
+        if (item.count == 1) mma_commit(q_empty);
+      }
+      for (int32_t t = item.tile; t < end && ok; ++t) {
+        ok = mbar_wait(kv_full + 8 * kv.slot, kv.phase);
+        if (!ok) break;
+        v_slot = kv.slot;
+        kv.step();
+        const int32_t key = t * kTile;
+        if (key < item.lo || key + kTile > item.hi) {
+          // values outside the seen keys may be anything, and 0 times NaN is NaN: clear them
+          const int32_t c0 = min(max(item.lo - key, 0), kTile), c1 = min(max(item.hi - key, 0), kTile);
+          uint8_t* at = smem + L::kRing + v_slot * L::kSlot;
+          for (int32_t i = lane; i < kTile * 8; i += 32) {
+            const int32_t k = i >> 3;
+            if (k < c0 || k >= c1)
+#pragma unroll
+              for (int h = 0; h < L::kHalves; ++h)
+                *reinterpret_cast<uint4*>(at + h * L::kHalf + i * 16) = make_uint4(0, 0, 0, 0);
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+        }
+        bool k_waited = false;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          if (t >= item.first[x] && t < item.last[x]) {
+            ok = ok && mbar_wait(p_full + 8 * x, p_ring[x].phase);
+            if (!ok) break;
+            p_ring[x].step();
+            fence_after();
+            pv(x, t > item.first[x]);
+            if (t + 1 == item.last[x] && lane == 0) mma_commit(o_full + 8 * x);
+          }
+          if (t + 1 >= item.first[x] && t + 1 < item.last[x]) {
+            if (!k_waited) {
+              ok = ok && mbar_wait(kv_full + 8 * kv.slot, kv.phase);
+              if (!ok) break;
+              fence_after();
+              k_slot = kv.slot;
+              k_waited = true;
+            }
+            qk(x);
+          }
+        }
+        if (!ok) break;
+        if (lane == 0) mma_commit(kv_empty + 8 * v_slot);
+        if (t + 1 < end) {  // A or B sees every key tile of the piece, so its keys were waited for
+          kv.step();
+          if (lane == 0) {
+            mma_commit(kv_empty + 8 * k_slot);
+            if (t + 2 == end) mma_commit(q_empty);
+          }
+        }
+      }
+    }
+    if (!ok) {
+      report(p.status, PREBA_ERR_TIMEOUT);
+      if (lane == 0) mma_commit(drained);  // what was issued ends before the memory goes to another
+      mbar_wait(drained, 0);
+    }
+  } else {
+    // ---- softmax: group x has row tile x, a thread a row
+    const int x = warp >> 2, r = threadIdx.x & (kTile - 1);
+    const uint32_t lanes = static_cast<uint32_t>(warp & 3) << 21;  // 32 rows of tensor memory each
+    const uint32_t s_at = tmem + lanes + L::kS + x * kTile, o_at = tmem + lanes + L::kO + x * DP;
+    const float scale = p.scale * kLog2e;
+    const int32_t j = r / static_cast<int32_t>(a.group), g = r - j * static_cast<int32_t>(a.group);
+    ring<1> s_ring, o_ring;
+    ring<2> in;
+    while (ok) {
+      ok = mbar_wait(item_full + 8 * in.slot, in.phase);
+      if (!ok) break;
+      const item_t item = items[in.slot];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(item_empty + 8 * in.slot);
+      in.step();
+      if (item.count == 0) break;
+      const int32_t token = item.token + x * static_cast<int32_t>(a.tokens_per_tile);
+      if (token >= item.rows) continue;  // B has no rows
+      const int32_t tokens = min(static_cast<int32_t>(a.tokens_per_tile), item.rows - token);
+      const bool live = j < tokens;
+      request_t q{item.row, item.rows, item.keys};
+      int32_t row_lo = 0, row_hi = 0, low, high;
+      if (live) seen_by(p, q, token + j, token + j + 1, row_lo, row_hi);
+      int32_t all_lo, all_hi;  // keys that every row of the tile sees
+      seen_by(p, q, token, token + 1, low, all_hi);
+      seen_by(p, q, token + tokens - 1, token + tokens, all_lo, high);
+      float m = -INFINITY, l = 0.f;
+      for (int32_t t = item.first[x]; t < item.last[x] && ok; ++t) {
+        ok = mbar_wait(s_full + 8 * x, s_ring.phase);
+        if (!ok) break;
+        s_ring.step();
+        fence_after();
+        uint32_t s[kTile];
+#pragma unroll
+        for (int c = 0; c < kTile; c += 32) tmem_load32(s + c, s_at + c);
+#pragma unroll
+        for (int c = 0; c < kTile; c += 32) tmem_loaded(s + c);
+        const int32_t key = t * kTile;
+        if (key < all_lo || key + kTile > all_hi) {
+          const int32_t c0 = row_lo - key, c1 = row_hi - key;
+#pragma unroll
+          for (int c = 0; c < kTile; ++c)
+            if (c < c0 || c >= c1) s[c] = 0xff800000u;
+        }
+        float top = __uint_as_float(s[0]);
+#pragma unroll
+        for (int c = 1; c < kTile; ++c) top = fmaxf(top, __uint_as_float(s[c]));
+        top *= scale;
+        const bool grown = top > m + kGrowth;  // true for the first key seen: m is -inf
+        if (__any_sync(kFull, grown)) {
+          const float to = fmaxf(m, top);
+          const float keep = to == -INFINITY ? 0.f : exp2_approx(m - to);
+          m = to;
+          l *= keep;
+          if (t > item.first[x]) {  // the product before has finished: S could not be there otherwise
+            for (int c = 0; c < DP; c += 32) {
+              uint32_t o[32];
+              tmem_load32(o, o_at + c);
+              tmem_loaded(o);
+#pragma unroll
+              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * keep);
+              tmem_store32(o_at + c, o);
+            }
+          }
+        }
+        const float shift = m == -INFINITY ? 0.f : m;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < kTile; c += 2) {
+          const float e0 = exp2_approx(fmaf(__uint_as_float(s[c]), scale, -shift));
+          const float e1 = exp2_approx(fmaf(__uint_as_float(s[c + 1]), scale, -shift));
+          sum[(c / 2) & 3] += e0 + e1;
+          s[c / 2] = pack2<T>(e0, e1);
+        }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        tmem_store32(s_at, s);
+        tmem_store32(s_at + 32, s + 32);
+        tmem_stored();
+        fence_before();
+        mbar_arrive(p_full + 8 * x);
+      }
+      if (!ok) break;
+      const bool any = item.first[x] < item.last[x];
+      if (any) {
+        ok = mbar_wait(o_full + 8 * x, o_ring.phase);
+        if (!ok) break;
+        o_ring.step();
+        fence_after();
+      }
+      if (item.whole) {
+        const uint32_t h = item.head * a.group + g, tok = item.row + token + j;
+        const float inv = l > 0.f ? 1.f / l : 0.f;
+        T* to = static_cast<T*>(p.out) + tok * p.out_stride[0] + h * p.out_stride[1];
+#pragma unroll 1
+        for (int c = 0; c < DP; c += 32) {
+          uint32_t o[32];
+          tmem_load32(o, o_at + c);
+          tmem_loaded(o);
+          if (live) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 8)
+              if (c + i < static_cast<int32_t>(p.head_dim)) {
+                uint4 v;
+                v.x = pack2<T>(__uint_as_float(o[i]) * inv, __uint_as_float(o[i + 1]) * inv);
+                v.y = pack2<T>(__uint_as_float(o[i + 2]) * inv, __uint_as_float(o[i + 3]) * inv);
+                v.z = pack2<T>(__uint_as_float(o[i + 4]) * inv, __uint_as_float(o[i + 5]) * inv);
+                v.w = pack2<T>(__uint_as_float(o[i + 6]) * inv, __uint_as_float(o[i + 7]) * inv);
+                *reinterpret_cast<uint4*>(to + c + i) = v;
+              }
+          }
+        }
+        if (p.lse && live)
+          p.lse[static_cast<uint64_t>(tok) * p.heads_q + h] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+      } else {
+        // partial sums, a column of 256 rows after the other, then maxima and sums
+        float* to = a.partials + static_cast<uint64_t>(item.slot) * (2 * kTile * (DP + 2)) + x * kTile + r;
+        if (any)
+#pragma unroll 1
+          for (int c = 0; c < DP; c += 32) {
+            uint32_t o[32];
+            tmem_load32(o, o_at + c);
+            tmem_loaded(o);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) to[(c + i) * 2 * kTile] = __uint_as_float(o[i]);
+          }
+        to[DP * 2 * kTile] = m;
+        to[(DP + 1) * 2 * kTile] = l;
+      }
+      fence_before();
+    }
+    if (!ok) report(p.status, PREBA_ERR_TIMEOUT);
+  }
+
+  fence_before();
+  if (!a.head->claim) __threadfence();
+  __syncthreads();
+  fence_after();
+  if (warp == kMmaWarp)
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(kTmemColumns) : "memory");
+
+  // ---- join the CTAs' pieces: whoever finishes a pair on a key head last adds them up
+  if (a.head->claim) return;
+  if (threadIdx.x < 2) {
+    const uint32_t* j = joins + 2 + 4 * threadIdx.x;
+    uint32_t last = 0;
+    if (j[0]) last = atomicAdd(&a.joined[j[2]], 1) == j[3] - j[2];
+    __threadfence();
+    joins[threadIdx.x] = last;
+  }
+  __syncthreads();
+#pragma unroll 1
+  for (int i = 0; i < 2; ++i) {
+    if (!joins[i] || warp >= kSoftWarps) continue;
+    const uint32_t* of = joins + 2 + 4 * i;
+    const uint32_t pair = of[1] / p.heads_kv, head = of[1] - pair * p.heads_kv, c0 = of[2], c1 = of[3];
+    const uint4 info = a.pairs[pair];
+    request_t q;
+    load_request(p, info.x, q);
+    const int x = warp >> 2, r = threadIdx.x & (kTile - 1);
+    const int32_t j = r / static_cast<int32_t>(a.group), g = r - j * static_cast<int32_t>(a.group);
+    const int32_t token = (2 * info.y + x) * a.tokens_per_tile + j;
+    if (j >= static_cast<int32_t>(a.tokens_per_tile) || token >= q.rows) continue;
+    // the first CTA's piece begins the pair: its second slot; the others lie in their first
+    auto at = [&](uint32_t cta) {
+      return a.partials + static_cast<uint64_t>(2 * cta + (cta == c0)) * (2 * kTile * (DP + 2)) + x * kTile + r;
+    };
+    float m = -INFINITY, l = 0.f;
+    for (uint32_t c = c0; c <= c1; ++c) m = fmaxf(m, __ldcg(at(c) + DP * 2 * kTile));
+    for (uint32_t c = c0; c <= c1; ++c) {
+      const float mc = __ldcg(at(c) + DP * 2 * kTile);
+      if (mc != -INFINITY) l += exp2_approx(mc - m) * __ldcg(at(c) + (DP + 1) * 2 * kTile);
+    }
+    const uint32_t h = head * a.group + g, tok = q.row + token;
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    T* to = static_cast<T*>(p.out) + tok * p.out_stride[0] + h * p.out_stride[1];
+#pragma unroll 1
+    for (int e = 0; e < static_cast<int>(p.head_dim); e += 8) {
+      float acc[8] = {};
+      for (uint32_t c = c0; c <= c1; ++c) {
+        const float* from = at(c);
+        const float mc = __ldcg(from + DP * 2 * kTile);
+        if (mc == -INFINITY) continue;  // it saw nothing and left no sums
+        const float w = exp2_approx(mc - m) * inv;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) acc[k] = fmaf(w, __ldcg(from + (e + k) * 2 * kTile), acc[k]);
+      }
+      uint4 v;
+      v.x = pack2<T>(acc[0], acc[1]);
+      v.y = pack2<T>(acc[2], acc[3]);
+      v.z = pack2<T>(acc[4], acc[5]);
+      v.w = pack2<T>(acc[6], acc[7]);
+      *reinterpret_cast<uint4*>(to + e) = v;
+    }
+    if (p.lse) p.lse[static_cast<uint64_t>(tok) * p.heads_q + h] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+  }
+}
+
+template <typename T, int DP>
+cudaError_t launch(const tiles_args& a, cudaStream_t stream) {
+  using L = layout<DP>;
+  const preba_pages_attend_t& p = a.p;
+  CUtensorMap map_q, map_k, map_v;
+  const uint64_t dims_q[4] = {p.head_dim, p.heads_q, p.tokens, 1};
+  const uint64_t strides_q[3] = {p.q_stride[1], p.q_stride[0], 0};
+  const uint32_t box_q[2] = {a.group, a.tokens_per_tile};
+  cudaError_t err = tensor_map(&map_q, p.dtype, p.q, dims_q, strides_q, box_q);
+  if (err == cudaSuccess) err = cache_map(&map_k, p, p.k_cache, p.k_stride, a.box_rows);
+  if (err == cudaSuccess) err = cache_map(&map_v, p, p.v_cache, p.v_stride, a.box_rows);
+  if (err == cudaSuccess)
+    err = cudaFuncSetAttribute(tiles_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes);
+  if (err != cudaSuccess) return err;
+  tiles_kernel<T, DP><<<a.grid, kThreads, L::kBytes, stream>>>(map_q, map_k, map_v, a);
+  return cudaGetLastError();
+}
+
+uint64_t up16(uint64_t v) { return (v + 15) / 16 * 16; }
+
+uint64_t pairs_at_most(uint32_t n, uint32_t tokens, uint32_t group) {
+  return tokens / (2 * (kTile / group)) + n;
+}
+
+}  // namespace
+
+namespace attend {
+
+uint64_t tiles_workspace(uint32_t n, uint32_t tokens, uint32_t group, uint32_t head_dim) {
+  const uint64_t pairs = pairs_at_most(n, tokens, group);
+  return up16(sizeof(tiles_head)) + up16(4 * kMaxTileCtas) + 16 * pairs + up16(4 * pairs) +
+         2ull * kMaxTileCtas * 2 * kTile * ((head_dim <= 64 ? 64 : 128) + 2) * 4;
+}
+
+cudaError_t launch_tiles(const preba_pages_attend_t& p, uint32_t page_shift, int sms, void* workspace,
+                         cudaStream_t stream) {
+  tiles_args a{};
+  a.p = p;
+  a.page_shift = page_shift;
+  a.group = p.heads_q / p.heads_kv;
+  a.tokens_per_tile = kTile / a.group;
+  a.box_rows = std::min<uint32_t>(p.page_size, kTile);
+  a.box_shift = 31 - __builtin_clz(a.box_rows);
+  a.grid = std::min(sms, kMaxTileCtas);
+  const uint64_t pairs = pairs_at_most(p.n, p.tokens, a.group);
+  a.max_pairs = static_cast<uint32_t>(pairs);
+  uint8_t* at = static_cast<uint8_t*>(workspace);
+  a.head = reinterpret_cast<tiles_head*>(at);
+  at += up16(sizeof(tiles_head));
+  a.joined = reinterpret_cast<uint32_t*>(at);
+  at += up16(4 * kMaxTileCtas);
+  a.pairs = reinterpret_cast<uint4*>(at);
+  at += 16 * pairs;
+  a.order = reinterpret_cast<uint32_t*>(at);
+  at += up16(4 * pairs);
+  a.partials = reinterpret_cast<float*>(at);
+  const size_t smem = 4 * (static_cast<size_t>(p.n) + 1);
+  if (smem > 32 * 1024) {
+    const cudaError_t err = cudaFuncSetAttribute(tiles_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                 4 * (PREBA_PAGES_MAX_REQUESTS + 1));
+    if (err != cudaSuccess) return err;
+  }
+  tiles_plan_kernel<<<1, kPlanThreads, smem, stream>>>(a);
+  const cudaError_t err = cudaGetLastError();
+  if (err != cudaSuccess) return err;
+  if (p.dtype == PREBA_F16)
+    return p.head_dim <= 64 ? launch<__half, 64>(a, stream) : launch<__half, 128>(a, stream);
+  return p.head_dim <= 64 ? launch<__nv_bfloat16, 64>(a, stream) : launch<__nv_bfloat16, 128>(a, stream);
+}
+
+}  // namespace attend
+}  // namespace preba
