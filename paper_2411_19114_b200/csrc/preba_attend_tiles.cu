@@ -31,7 +31,10 @@ using namespace attend;
 constexpr int kTile = 128;             // rows of a tile, keys of a slot
 constexpr int kSoftWarps = 8;          // four per tile
 constexpr int kCopyWarp = 8, kMmaWarp = 9;
-constexpr int kThreads = 32 * 10;
+constexpr int kThreads = 32 * 12;       // the last two warps only complete the third warpgroup
+// Registers: launched with 168 a thread, 64512 in all; the softmax threads hold a row of S each.
+constexpr int kSoftRegisters = 208, kOtherRegisters = 88;
+static_assert(256 * kSoftRegisters + 128 * kOtherRegisters <= 168 * kThreads, "register split");
 constexpr uint32_t kTmemColumns = 512;
 constexpr uint32_t kMinRun = 2;        // key tiles of a CTA's run in the line, at least
 constexpr float kGrowth = 8.f;         // log2 of what a row may outgrow its reference by
@@ -228,36 +231,73 @@ static_assert(kBins == kPlanThreads, "one bin per thread in the sum");
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
-// Shared-memory operand: rows of 128 bytes in the 128-byte swizzle, eight rows to a group.  `leading`
-// is the distance between 64-element columns of an operand whose rows are not its contraction axis,
-// `stride` the one between groups of eight rows.
-__device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t leading, uint32_t stride) {
-  return static_cast<uint64_t>((addr & 0x3ffff) >> 4) | static_cast<uint64_t>(leading >> 4) << 16 |
-         static_cast<uint64_t>(stride >> 4) << 32 | 1ull << 46 | 2ull << 61;
+// Shared-memory operand: rows of 128 bytes in the 128-byte swizzle, eight rows (1024 bytes) to a group.
+// `leading` is the distance between 64-element columns of an operand whose rows are its contraction
+// axis.  The low word of the descriptor; the high one is the same for all.
+__device__ __forceinline__ uint32_t operand(uint32_t addr, uint32_t leading) {
+  return (addr & 0x3ffff) >> 4 | (leading >> 4) << 16;
 }
+constexpr uint32_t kOperandHigh = (1024 >> 4) | 1u << 14 | 2u << 29;
 // fp32 accumulator, 128 rows, `columns` columns; values: the second operand's rows are contracted.
 template <typename T> __device__ __forceinline__ constexpr uint32_t shape(uint32_t columns, bool values) {
   const uint32_t kind = sizeof(T) == 2 && !std::is_same<T, __half>::value ? 1 : 0;  // bfloat16 : binary16
   return 1u << 4 | kind << 7 | kind << 10 | (values ? 1u << 16 : 0u) | (columns / 8) << 17 | (kTile / 16) << 24;
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t add) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc),
-      "r"(add)
+      "{\n\t.reg .pred p;\n\t.reg .b64 x, y;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+      "mov.b64 x, {%1, %5};\n\tmov.b64 y, {%2, %5};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n\t}" ::"r"(d), "r"(a), "r"(b), "r"(idesc),
+      "r"(add), "n"(kOperandHigh)
       : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t add) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc),
-      "r"(add)
+      "{\n\t.reg .pred p;\n\t.reg .b64 y;\n\tsetp.ne.u32 p, %4, 0;\n\tmov.b64 y, {%2, %5};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n\t}" ::"r"(d), "r"(a), "r"(b), "r"(idesc),
+      "r"(add), "n"(kOperandHigh)
       : "memory");
 }
 // Arrives at the barrier when all matrix products issued before have finished.
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar)
                : "memory");
+}
+
+// Arithmetic on two fp32 numbers at once, and a maximum of three.
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+  uint64_t v;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b));
+  return v;
+}
+__device__ __forceinline__ uint64_t pair(uint32_t a, uint32_t b) {
+  uint64_t v;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "r"(a), "r"(b));
+  return v;
+}
+__device__ __forceinline__ void unpair(uint64_t v, float& a, float& b) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v));
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t v;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(a), "l"(b), "l"(c));
+  return v;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t v;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+  return v;
+}
+__device__ __forceinline__ float max3(float a, uint32_t b, uint32_t c) {
+  float v;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(v) : "f"(a), "f"(__uint_as_float(b)), "f"(__uint_as_float(c)));
+  return v;
+}
+__device__ __forceinline__ float max3(uint32_t a, uint32_t b, uint32_t c) {
+  return max3(__uint_as_float(a), b, c);
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  return max3(a, __float_as_uint(b), __float_as_uint(c));
 }
 
 #define PREBA_R8(v, i) "+r"(v[i]), "+r"(v[i + 1]), "+r"(v[i + 2]), "+r"(v[i + 3]), "+r"(v[i + 4]), \
@@ -286,6 +326,12 @@ __device__ __forceinline__ void tmem_store32(uint32_t addr, const uint32_t* v) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], " PREBA_L32 ";" ::PREBA_I8(v, 0), PREBA_I8(v, 8),
                PREBA_I8(v, 16), PREBA_I8(v, 24), "r"(addr)
                : "memory");
+}
+__device__ __forceinline__ void tmem_store16(uint32_t addr, const uint32_t* v) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::
+          PREBA_I8(v, 0), PREBA_I8(v, 8), "r"(addr)
+      : "memory");
 }
 __device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -349,253 +395,263 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
   const uint32_t tmem = *tmem_slot;
   bool ok = true;
 
-  if (warp == kCopyWarp) {
-    // ---- work and copies
-    const tiles_head plan = *a.head;
-    const uint32_t boxes = kTile >> a.box_shift;
-    const uint32_t chunk = lane & (boxes - 1), half = lane / boxes;
-    const bool mine = half < L::kHalves;
-    const uint32_t dst = half * L::kHalf + (chunk << a.box_shift) * 128;
-    ring<L::kSlots> kv;
-    ring<1> q_ring;
-    ring<2> out;
-    uint32_t issued = 0, q_issued = 0;
-    uint32_t unit = min(static_cast<uint64_t>(blockIdx.x) * plan.per, static_cast<uint64_t>(plan.units));
-    const uint32_t unit_end = min(unit + plan.per, plan.units);
-    uint32_t pair = 0;
-    if (!plan.claim && unit < unit_end) {  // the pair that the run begins in
-      uint32_t lo = 0, hi = plan.n_pairs;
-      while (hi - lo > 1) {
-        const uint32_t mid = (lo + hi) / 2;
-        if (a.pairs[mid].z * p.heads_kv <= unit) lo = mid; else hi = mid;
-      }
-      pair = lo;
-    }
-    while (ok) {
-      // the next piece
-      item_t item;
-      item.count = 0;
-      uint4 of;
-      if (plan.claim) {
-        uint32_t k = 0;
-        if (lane == 0) k = atomicAdd(&a.head->next, 1);
-        k = __shfl_sync(kFull, k, 0);
-        if (k < plan.n_pairs * p.heads_kv) {
-          of = a.pairs[a.order[k / p.heads_kv]];
-          item.head = k % p.heads_kv;
-          item.count = of.w;
-          item.tile = 0;
-          item.whole = 1;
-          item.slot = 0;
+  if (warp >= kSoftWarps) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegisters));
+    if (warp == kCopyWarp) {
+      // ---- work and copies
+      const tiles_head plan = *a.head;
+      const uint32_t boxes = kTile >> a.box_shift;
+      const uint32_t chunk = lane & (boxes - 1), half = lane / boxes;
+      const bool mine = half < L::kHalves;
+      const uint32_t dst = half * L::kHalf + (chunk << a.box_shift) * 128;
+      ring<L::kSlots> kv;
+      ring<1> q_ring;
+      ring<2> out;
+      uint32_t issued = 0, q_issued = 0;
+      uint32_t unit = min(static_cast<uint64_t>(blockIdx.x) * plan.per, static_cast<uint64_t>(plan.units));
+      const uint32_t unit_end = min(unit + plan.per, plan.units);
+      uint32_t pair = 0;
+      if (!plan.claim && unit < unit_end) {  // the pair that the run begins in
+        uint32_t lo = 0, hi = plan.n_pairs;
+        while (hi - lo > 1) {
+          const uint32_t mid = (lo + hi) / 2;
+          if (a.pairs[mid].z * p.heads_kv <= unit) lo = mid; else hi = mid;
         }
-      } else if (unit < unit_end) {
-        of = a.pairs[pair];
-        const uint32_t offset = unit - of.z * p.heads_kv;
-        item.head = offset / of.w;
-        item.tile = offset - item.head * of.w;
-        item.count = min(of.w - item.tile, unit_end - unit);
-        item.whole = item.count == static_cast<int32_t>(of.w);
-        item.slot = 2 * blockIdx.x + (item.tile == 0);
-        if (!item.whole && lane == 0) {  // to be joined at the end
-          const uint32_t start = unit - item.tile;
-          uint32_t* j = joins + 2 + 4 * (item.tile == 0);
-          j[0] = 1;
-          j[1] = pair * p.heads_kv + item.head;
-          j[2] = start / plan.per;
-          j[3] = (start + of.w - 1) / plan.per;
-        }
-        unit += item.count;
-        if (offset + item.count == of.w * p.heads_kv) ++pair;
+        pair = lo;
       }
-      const bool done = item.count == 0;
-      if (!done) {
-        request_t q;
-        load_request(p, of.x, q);
-        const pair_range range = range_of(a, q, of.y);
-        item.request = of.x;
-        item.row = q.row;
-        item.rows = q.rows;
-        item.keys = q.keys;
-        item.token = 2 * of.y * a.tokens_per_tile;
-        item.lo = range.lo;
-        item.hi = range.hi;
-        item.tile += range.begin;
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          item.first[x] = max(range.first[x], item.tile);
-          item.last[x] = max(item.first[x], min(range.last[x], item.tile + item.count));
-        }
-      }
-      ok = mbar_wait(item_empty + 8 * out.slot, out.phase ^ 1);
-      if (!ok) break;
-      if (lane == 0) {
-        items[out.slot] = item;
-        mbar_arrive(item_full + 8 * out.slot);
-      }
-      out.step();
-      if (done) break;
-      // queries
-      ok = mbar_wait(q_empty, q_ring.phase ^ 1);
-      if (!ok) break;
-      if (lane == 0) {
-        const uint32_t bytes = a.tokens_per_tile * a.group * 128 * L::kHalves;
-        const bool two = item.token + static_cast<int32_t>(a.tokens_per_tile) < item.rows;
-        mbar_arrive_expect_tx(q_full, two ? 2 * bytes : bytes);
-        for (int x = 0; x < (two ? 2 : 1); ++x)
-          for (int h = 0; h < L::kHalves; ++h)
-            tensor_copy(base + x * L::kQ + h * L::kHalf, &map_q, 64 * h, item.head * a.group,
-                        item.row + item.token + x * a.tokens_per_tile, 0, q_full);
-      }
-      ++q_issued;
-      q_ring.step();
-      // keys and values, tile by tile
-      const int32_t* row = p.block_table + static_cast<uint64_t>(item.request) * p.table_stride;
-      int32_t key = item.tile * kTile + (chunk << a.box_shift);
-      auto wanted = [&](int32_t k) {
-        return mine && k < item.hi && k + static_cast<int32_t>(a.box_rows) > item.lo;
-      };
-      int32_t entry = wanted(key) ? row[key >> a.page_shift] : 0;
-      for (int32_t t = 0; t < item.count && ok; ++t, key += kTile) {
-        int32_t page = entry;
-        const bool want = wanted(key);
-        if (t + 1 < item.count) entry = wanted(key + kTile) ? row[(key + kTile) >> a.page_shift] : 0;
-        if (want && (page < 0 || static_cast<uint32_t>(page) >= p.pages)) {
-          report(p.status, PREBA_ERR_BAD_TABLE);
-          page = p.pages;  // beyond the tensor: the box is filled with zeros
-        }
-        const uint32_t bytes = __popc(__ballot_sync(kFull, want)) * a.box_rows * 128;
-#pragma unroll
-        for (int v = 0; v < 2; ++v) {
-          ok = ok && mbar_wait(kv_empty + 8 * kv.slot, kv.phase ^ 1);
-          if (!ok) break;
-          if (lane == 0) mbar_arrive_expect_tx(kv_full + 8 * kv.slot, bytes);
-          __syncwarp();
-          if (want)
-            tensor_copy(base + L::kRing + kv.slot * L::kSlot + dst, v ? &map_v : &map_k, half * 64,
-                        key & (p.page_size - 1), item.head, page, kv_full + 8 * kv.slot);
-          ++issued;
-          kv.step();
-        }
-      }
-    }
-    if (!ok) {  // what is in flight lands before the memory goes to another
-      report(p.status, PREBA_ERR_TIMEOUT);
-      for (uint32_t i = issued - min(issued, static_cast<uint32_t>(L::kSlots)); i < issued; ++i)
-        mbar_wait(kv_full + 8 * (i % L::kSlots), (i / L::kSlots) & 1);
-      if (q_issued) mbar_wait(q_full, (q_issued - 1) & 1);
-    }
-  } else if (warp == kMmaWarp) {
-    // ---- matrix products: one lane issues, the warp clears values that nobody sees
-    constexpr uint32_t kQkShape = shape<T>(kTile, false), kPvShape = shape<T>(DP, true);
-    ring<L::kSlots> kv;  // next slot to be waited for
-    ring<1> q_ring, p_ring[2];
-    ring<2> in;
-    while (ok) {
-      ok = mbar_wait(item_full + 8 * in.slot, in.phase);
-      if (!ok) break;
-      const item_t item = items[in.slot];
-      __syncwarp();
-      if (lane == 0) mbar_arrive(item_empty + 8 * in.slot);
-      in.step();
-      if (item.count == 0) break;
-      ok = mbar_wait(q_full, q_ring.phase);
-      if (!ok) break;
-      q_ring.step();
-      const int32_t end = item.tile + item.count;
-      uint32_t k_slot = 0, v_slot = 0;
-      auto qk = [&](int x) {
-        const uint64_t q_op = operand(base + x * L::kQ, 16, 1024);
-        const uint64_t k_op = operand(base + L::kRing + k_slot * L::kSlot, 16, 1024);
-        if (lane == 0) {
-#pragma unroll
-          for (int ks = 0; ks < DP / 16; ++ks) {
-            const uint32_t off = (ks / 4) * L::kHalf + (ks % 4) * 32;
-            mma_ss(tmem + L::kS + x * kTile, q_op + (off >> 4), k_op + (off >> 4), kQkShape, ks > 0);
+      while (ok) {
+        // the next piece
+        item_t item;
+        item.count = 0;
+        uint4 of;
+        if (plan.claim) {
+          uint32_t k = 0;
+          if (lane == 0) k = atomicAdd(&a.head->next, 1);
+          k = __shfl_sync(kFull, k, 0);
+          if (k < plan.n_pairs * p.heads_kv) {
+            of = a.pairs[a.order[k / p.heads_kv]];
+            item.head = k % p.heads_kv;
+            item.count = of.w;
+            item.tile = 0;
+            item.whole = 1;
+            item.slot = 0;
           }
-          mma_commit(s_full + 8 * x);
+        } else if (unit < unit_end) {
+          of = a.pairs[pair];
+          const uint32_t offset = unit - of.z * p.heads_kv;
+          item.head = offset / of.w;
+          item.tile = offset - item.head * of.w;
+          item.count = min(of.w - item.tile, unit_end - unit);
+          item.whole = item.count == static_cast<int32_t>(of.w);
+          item.slot = 2 * blockIdx.x + (item.tile == 0);
+          if (!item.whole && lane == 0) {  // to be joined at the end
+            const uint32_t start = unit - item.tile;
+            uint32_t* j = joins + 2 + 4 * (item.tile == 0);
+            j[0] = 1;
+            j[1] = pair * p.heads_kv + item.head;
+            j[2] = start / plan.per;
+            j[3] = (start + of.w - 1) / plan.per;
+          }
+          unit += item.count;
+          if (offset + item.count == of.w * p.heads_kv) ++pair;
         }
-      };
-      auto pv = [&](int x, bool add) {
-        const uint64_t v_op = operand(base + L::kRing + v_slot * L::kSlot, L::kHalf, 1024);
+        const bool done = item.count == 0;
+        if (!done) {
+          request_t q;
+          load_request(p, of.x, q);
+          const pair_range range = range_of(a, q, of.y);
+          item.request = of.x;
+          item.row = q.row;
+          item.rows = q.rows;
+          item.keys = q.keys;
+          item.token = 2 * of.y * a.tokens_per_tile;
+          item.lo = range.lo;
+          item.hi = range.hi;
+          item.tile += range.begin;
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            item.first[x] = max(range.first[x], item.tile);
+            item.last[x] = max(item.first[x], min(range.last[x], item.tile + item.count));
+          }
+        }
+        ok = mbar_wait(item_empty + 8 * out.slot, out.phase ^ 1);
+        if (!ok) break;
         if (lane == 0) {
-#pragma unroll
-          for (int ks = 0; ks < kTile / 16; ++ks)
-            mma_ts(tmem + L::kO + x * DP, tmem + L::kS + x * kTile + 8 * ks, v_op + (ks * 2048 >> 4), kPvShape,
-                   add || ks > 0);
+          items[out.slot] = item;
+          mbar_arrive(item_full + 8 * out.slot);
         }
-      };
-      // keys of the first tile
-      ok = mbar_wait(kv_full + 8 * kv.slot, kv.phase);
-      if (!ok) break;
-      fence_after();
-      k_slot = kv.slot;
-      kv.step();
+        out.step();
+        if (done) break;
+        // queries
+        ok = mbar_wait(q_empty, q_ring.phase ^ 1);
+        if (!ok) break;
+        if (lane == 0) {
+          const uint32_t bytes = a.tokens_per_tile * a.group * 128 * L::kHalves;
+          const bool two = item.token + static_cast<int32_t>(a.tokens_per_tile) < item.rows;
+          mbar_arrive_expect_tx(q_full, two ? 2 * bytes : bytes);
+          for (int x = 0; x < (two ? 2 : 1); ++x)
+            for (int h = 0; h < L::kHalves; ++h)
+              tensor_copy(base + x * L::kQ + h * L::kHalf, &map_q, 64 * h, item.head * a.group,
+                          item.row + item.token + x * a.tokens_per_tile, 0, q_full);
+        }
+        ++q_issued;
+        q_ring.step();
+        // keys and values, tile by tile
+        const int32_t* row = p.block_table + static_cast<uint64_t>(item.request) * p.table_stride;
+        int32_t key = item.tile * kTile + (chunk << a.box_shift);
+        auto wanted = [&](int32_t k) {
+          return mine && k < item.hi && k + static_cast<int32_t>(a.box_rows) > item.lo;
+        };
+        int32_t entry = wanted(key) ? row[key >> a.page_shift] : 0;
+        for (int32_t t = 0; t < item.count && ok; ++t, key += kTile) {
+          int32_t page = entry;
+          const bool want = wanted(key);
+          if (t + 1 < item.count) entry = wanted(key + kTile) ? row[(key + kTile) >> a.page_shift] : 0;
+          if (want && (page < 0 || static_cast<uint32_t>(page) >= p.pages)) {
+            report(p.status, PREBA_ERR_BAD_TABLE);
+            page = p.pages;  // beyond the tensor: the box is filled with zeros
+          }
+          const uint32_t bytes = __popc(__ballot_sync(kFull, want)) * a.box_rows * 128;
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
-        if (item.first[x] == item.tile && item.first[x] < item.last[x]) qk(x);
-      if (lane == 0) {
-        mma_commit(kv_empty + 8 * k_slot);
-        if (item.count == 1) mma_commit(q_empty);
+          for (int v = 0; v < 2; ++v) {
+            ok = ok && mbar_wait(kv_empty + 8 * kv.slot, kv.phase ^ 1);
+            if (!ok) break;
+            if (lane == 0) mbar_arrive_expect_tx(kv_full + 8 * kv.slot, bytes);
+            __syncwarp();
+            if (want)
+              tensor_copy(base + L::kRing + kv.slot * L::kSlot + dst, v ? &map_v : &map_k, half * 64,
+                          key & (p.page_size - 1), item.head, page, kv_full + 8 * kv.slot);
+            ++issued;
+            kv.step();
+          }
+        }
       }
-      for (int32_t t = item.tile; t < end && ok; ++t) {
+      if (!ok) {  // what is in flight lands before the memory goes to another
+        report(p.status, PREBA_ERR_TIMEOUT);
+        for (uint32_t i = issued - min(issued, static_cast<uint32_t>(L::kSlots)); i < issued; ++i)
+          mbar_wait(kv_full + 8 * (i % L::kSlots), (i / L::kSlots) & 1);
+        if (q_issued) mbar_wait(q_full, (q_issued - 1) & 1);
+      }
+    } else if (warp == kMmaWarp) {
+      // ---- matrix products: one lane issues, the warp clears values that nobody sees
+      constexpr uint32_t kQkShape = shape<T>(kTile, false), kPvShape = shape<T>(DP, true);
+      ring<L::kSlots> kv;  // next slot to be waited for
+      ring<1> q_ring, p_ring[2];
+      ring<2> in;
+      while (ok) {
+        ok = mbar_wait(item_full + 8 * in.slot, in.phase);
+        if (!ok) break;
+        const item_t item = items[in.slot];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(item_empty + 8 * in.slot);
+        in.step();
+        if (item.count == 0) break;
+        ok = mbar_wait(q_full, q_ring.phase);
+        if (!ok) break;
+        q_ring.step();
+        const int32_t end = item.tile + item.count;
+        uint32_t k_slot = 0, v_slot = 0;
+        auto qk = [&](int x) {
+          const uint32_t q_op = operand(base + x * L::kQ, 16);
+          const uint32_t k_op = operand(base + L::kRing + k_slot * L::kSlot, 16);
+          if (lane == 0) {
+#pragma unroll
+            for (int ks = 0; ks < DP / 16; ++ks) {
+              const uint32_t off = (ks / 4) * L::kHalf + (ks % 4) * 32;
+              mma_ss(tmem + L::kS + x * kTile, q_op + (off >> 4), k_op + (off >> 4), kQkShape, ks > 0);
+            }
+            mma_commit(s_full + 8 * x);
+          }
+        };
+        auto pv = [&](int x, bool add) {
+          const uint32_t v_op = operand(base + L::kRing + v_slot * L::kSlot, L::kHalf);
+          if (lane == 0) {
+#pragma unroll
+            for (int ks = 0; ks < kTile / 16; ++ks)
+              mma_ts(tmem + L::kO + x * DP, tmem + L::kS + x * kTile + 8 * ks, v_op + (ks * 2048 >> 4), kPvShape,
+                     add || ks > 0);
+          }
+        };
+        // keys of the first tile
         ok = mbar_wait(kv_full + 8 * kv.slot, kv.phase);
         if (!ok) break;
-        v_slot = kv.slot;
+        fence_after();
+        k_slot = kv.slot;
         kv.step();
-        const int32_t key = t * kTile;
-        if (key < item.lo || key + kTile > item.hi) {
-          // values outside the seen keys may be anything, and 0 times NaN is NaN: clear them
-          const int32_t c0 = min(max(item.lo - key, 0), kTile), c1 = min(max(item.hi - key, 0), kTile);
-          uint8_t* at = smem + L::kRing + v_slot * L::kSlot;
-          for (int32_t i = lane; i < kTile * 8; i += 32) {
-            const int32_t k = i >> 3;
-            if (k < c0 || k >= c1)
 #pragma unroll
-              for (int h = 0; h < L::kHalves; ++h)
-                *reinterpret_cast<uint4*>(at + h * L::kHalf + i * 16) = make_uint4(0, 0, 0, 0);
-          }
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          __syncwarp();
+        for (int x = 0; x < 2; ++x)
+          if (item.first[x] == item.tile && item.first[x] < item.last[x]) qk(x);
+        if (lane == 0) {
+          mma_commit(kv_empty + 8 * k_slot);
+          if (item.count == 1) mma_commit(q_empty);
         }
-        bool k_waited = false;
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          if (t >= item.first[x] && t < item.last[x]) {
-            ok = ok && mbar_wait(p_full + 8 * x, p_ring[x].phase);
-            if (!ok) break;
-            p_ring[x].step();
-            fence_after();
-            pv(x, t > item.first[x]);
-            if (t + 1 == item.last[x] && lane == 0) mma_commit(o_full + 8 * x);
-          }
-          if (t + 1 >= item.first[x] && t + 1 < item.last[x]) {
-            if (!k_waited) {
-              ok = ok && mbar_wait(kv_full + 8 * kv.slot, kv.phase);
-              if (!ok) break;
-              fence_after();
-              k_slot = kv.slot;
-              k_waited = true;
-            }
-            qk(x);
-          }
-        }
-        if (!ok) break;
-        if (lane == 0) mma_commit(kv_empty + 8 * v_slot);
-        if (t + 1 < end) {  // A or B sees every key tile of the piece, so its keys were waited for
+        for (int32_t t = item.tile; t < end && ok; ++t) {
+          ok = mbar_wait(kv_full + 8 * kv.slot, kv.phase);
+          if (!ok) break;
+          v_slot = kv.slot;
           kv.step();
-          if (lane == 0) {
-            mma_commit(kv_empty + 8 * k_slot);
-            if (t + 2 == end) mma_commit(q_empty);
+          const int32_t key = t * kTile;
+          if (key < item.lo || key + kTile > item.hi) {
+            // values outside the seen keys may be anything, and 0 times NaN is NaN: clear them
+            const int32_t c0 = min(max(item.lo - key, 0), kTile), c1 = min(max(item.hi - key, 0), kTile);
+            uint8_t* at = smem + L::kRing + v_slot * L::kSlot;
+            for (int32_t i = lane; i < kTile * 8; i += 32) {
+              const int32_t k = i >> 3;
+              if (k < c0 || k >= c1)
+#pragma unroll
+                for (int h = 0; h < L::kHalves; ++h)
+                  *reinterpret_cast<uint4*>(at + h * L::kHalf + i * 16) = make_uint4(0, 0, 0, 0);
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+          }
+          bool k_waited = false;
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            if (t >= item.first[x] && t < item.last[x]) {
+              ok = ok && mbar_wait(p_full + 8 * x, p_ring[x].phase);
+              if (!ok) break;
+              p_ring[x].step();
+              fence_after();
+              pv(x, t > item.first[x]);
+              if (t + 1 == item.last[x] && lane == 0) mma_commit(o_full + 8 * x);
+            }
+            if (t + 1 >= item.first[x] && t + 1 < item.last[x]) {
+              if (!k_waited) {
+                ok = ok && mbar_wait(kv_full + 8 * kv.slot, kv.phase);
+                if (!ok) break;
+                fence_after();
+                k_slot = kv.slot;
+                k_waited = true;
+              }
+              qk(x);
+            }
+          }
+          if (!ok) break;
+          if (lane == 0) mma_commit(kv_empty + 8 * v_slot);
+          if (t + 1 < end) {  // A or B sees every key tile of the piece, so its keys were waited for
+            kv.step();
+            if (lane == 0) {
+              mma_commit(kv_empty + 8 * k_slot);
+              if (t + 2 == end) mma_commit(q_empty);
+            }
           }
         }
       }
+      if (!ok) {
+        report(p.status, PREBA_ERR_TIMEOUT);
+        if (lane == 0) mma_commit(drained);  // what was issued ends before the memory goes to another
+        mbar_wait(drained, 0);
+      }
     }
-    if (!ok) {
-      report(p.status, PREBA_ERR_TIMEOUT);
-      if (lane == 0) mma_commit(drained);  // what was issued ends before the memory goes to another
-      mbar_wait(drained, 0);
-    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    if (warp == kMmaWarp)
+      asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(kTmemColumns)
+                   : "memory");
   } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegisters));
     // ---- softmax: group x has row tile x, a thread a row
     const int x = warp >> 2, r = threadIdx.x & (kTile - 1);
     const uint32_t lanes = static_cast<uint32_t>(warp & 3) << 21;  // 32 rows of tensor memory each
@@ -608,6 +664,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
       ok = mbar_wait(item_full + 8 * in.slot, in.phase);
       if (!ok) break;
       const item_t item = items[in.slot];
+      const int32_t first = items[in.slot].first[x], last = items[in.slot].last[x];
       __syncwarp();
       if (lane == 0) mbar_arrive(item_empty + 8 * in.slot);
       in.step();
@@ -623,7 +680,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
       seen_by(p, q, token, token + 1, low, all_hi);
       seen_by(p, q, token + tokens - 1, token + tokens, all_lo, high);
       float m = -INFINITY, l = 0.f;
-      for (int32_t t = item.first[x]; t < item.last[x] && ok; ++t) {
+      for (int32_t t = first; t < last && ok; ++t) {
         ok = mbar_wait(s_full + 8 * x, s_ring.phase);
         if (!ok) break;
         s_ring.step();
@@ -640,9 +697,15 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
           for (int c = 0; c < kTile; ++c)
             if (c < c0 || c >= c1) s[c] = 0xff800000u;
         }
-        float top = __uint_as_float(s[0]);
+        float tops[4];
 #pragma unroll
-        for (int c = 1; c < kTile; ++c) top = fmaxf(top, __uint_as_float(s[c]));
+        for (int c = 0; c < 4; ++c) tops[c] = max3(s[3 * c], s[3 * c + 1], s[3 * c + 2]);
+#pragma unroll
+        for (int c = 12; c < 124; c += 8)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) tops[k] = max3(tops[k], s[c + 2 * k], s[c + 2 * k + 1]);
+        float top = fmaxf(max3(tops[0], s[124], s[125]), max3(tops[1], s[126], s[127]));
+        top = max3(top, tops[2], tops[3]);
         top *= scale;
         const bool grown = top > m + kGrowth;  // true for the first key seen: m is -inf
         if (__any_sync(kFull, grown)) {
@@ -650,7 +713,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
           const float keep = to == -INFINITY ? 0.f : exp2_approx(m - to);
           m = to;
           l *= keep;
-          if (t > item.first[x]) {  // the product before has finished: S could not be there otherwise
+          if (t > first) {  // the product before has finished: S could not be there otherwise
             for (int c = 0; c < DP; c += 32) {
               uint32_t o[32];
               tmem_load32(o, o_at + c);
@@ -662,23 +725,31 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
           }
         }
         const float shift = m == -INFINITY ? 0.f : m;
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        const uint64_t scale2 = pair(scale, scale), shift2 = pair(-shift, -shift);
+        uint64_t sums[2] = {0, 0};
 #pragma unroll
-        for (int c = 0; c < kTile; c += 2) {
-          const float e0 = exp2_approx(fmaf(__uint_as_float(s[c]), scale, -shift));
-          const float e1 = exp2_approx(fmaf(__uint_as_float(s[c + 1]), scale, -shift));
-          sum[(c / 2) & 3] += e0 + e1;
-          s[c / 2] = pack2<T>(e0, e1);
+        for (int c = 0; c < kTile; c += 32) {
+          uint32_t e[16];
+#pragma unroll
+          for (int i = 0; i < 32; i += 2) {
+            float z0, z1;
+            unpair(fma2(pair(s[c + i], s[c + i + 1]), scale2, shift2), z0, z1);
+            z0 = exp2_approx(z0);
+            z1 = exp2_approx(z1);
+            sums[(i / 2) & 1] = add2(sums[(i / 2) & 1], pair(z0, z1));
+            e[i / 2] = pack2<T>(z0, z1);
+          }
+          tmem_store16(s_at + c / 2, e);
         }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-        tmem_store32(s_at, s);
-        tmem_store32(s_at + 32, s + 32);
+        float l0, l1;
+        unpair(add2(sums[0], sums[1]), l0, l1);
+        l += l0 + l1;
         tmem_stored();
         fence_before();
         mbar_arrive(p_full + 8 * x);
       }
       if (!ok) break;
-      const bool any = item.first[x] < item.last[x];
+      const bool any = first < last;
       if (any) {
         ok = mbar_wait(o_full + 8 * x, o_ring.phase);
         if (!ok) break;
@@ -727,69 +798,71 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
       fence_before();
     }
     if (!ok) report(p.status, PREBA_ERR_TIMEOUT);
-  }
 
-  fence_before();
-  if (!a.head->claim) __threadfence();
-  __syncthreads();
-  fence_after();
-  if (warp == kMmaWarp)
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(kTmemColumns) : "memory");
-
-  // ---- join the CTAs' pieces: whoever finishes a pair on a key head last adds them up
-  if (a.head->claim) return;
-  if (threadIdx.x < 2) {
-    const uint32_t* j = joins + 2 + 4 * threadIdx.x;
-    uint32_t last = 0;
-    if (j[0]) last = atomicAdd(&a.joined[j[2]], 1) == j[3] - j[2];
-    __threadfence();
-    joins[threadIdx.x] = last;
-  }
-  __syncthreads();
-#pragma unroll 1
-  for (int i = 0; i < 2; ++i) {
-    if (!joins[i] || warp >= kSoftWarps) continue;
-    const uint32_t* of = joins + 2 + 4 * i;
-    const uint32_t pair = of[1] / p.heads_kv, head = of[1] - pair * p.heads_kv, c0 = of[2], c1 = of[3];
-    const uint4 info = a.pairs[pair];
-    request_t q;
-    load_request(p, info.x, q);
-    const int x = warp >> 2, r = threadIdx.x & (kTile - 1);
-    const int32_t j = r / static_cast<int32_t>(a.group), g = r - j * static_cast<int32_t>(a.group);
-    const int32_t token = (2 * info.y + x) * a.tokens_per_tile + j;
-    if (j >= static_cast<int32_t>(a.tokens_per_tile) || token >= q.rows) continue;
-    // the first CTA's piece begins the pair: its second slot; the others lie in their first
-    auto at = [&](uint32_t cta) {
-      return a.partials + static_cast<uint64_t>(2 * cta + (cta == c0)) * (2 * kTile * (DP + 2)) + x * kTile + r;
-    };
-    float m = -INFINITY, l = 0.f;
-    for (uint32_t c = c0; c <= c1; ++c) m = fmaxf(m, __ldcg(at(c) + DP * 2 * kTile));
-    for (uint32_t c = c0; c <= c1; ++c) {
-      const float mc = __ldcg(at(c) + DP * 2 * kTile);
-      if (mc != -INFINITY) l += exp2_approx(mc - m) * __ldcg(at(c) + (DP + 1) * 2 * kTile);
+    // ---- join the CTAs' pieces: whoever finishes a pair on a key head last adds them up
+    fence_before();
+    const bool claimed = a.head->claim;
+    if (!claimed) __threadfence();
+    __syncthreads();
+    if (claimed) return;
+    if (threadIdx.x < 2) {
+      const uint32_t* j = joins + 2 + 4 * threadIdx.x;
+      uint32_t last = 0;
+      if (j[0]) last = atomicAdd(&a.joined[j[2]], 1) == j[3] - j[2];
+      __threadfence();
+      joins[threadIdx.x] = last;
     }
-    const uint32_t h = head * a.group + g, tok = q.row + token;
-    const float inv = l > 0.f ? 1.f / l : 0.f;
-    T* to = static_cast<T*>(p.out) + tok * p.out_stride[0] + h * p.out_stride[1];
+    asm volatile("bar.sync 1, 256;" ::: "memory");
 #pragma unroll 1
-    for (int e = 0; e < static_cast<int>(p.head_dim); e += 8) {
-      float acc[8] = {};
+    for (int i = 0; i < 2; ++i) {
+      if (!joins[i]) continue;
+      const uint32_t* of = joins + 2 + 4 * i;
+      const uint32_t pair = of[1] / p.heads_kv, head = of[1] - pair * p.heads_kv, c0 = of[2], c1 = of[3];
+      const uint4 info = a.pairs[pair];
+      request_t q;
+      load_request(p, info.x, q);
+      const int32_t token = (2 * info.y + x) * a.tokens_per_tile + j;
+      if (j >= static_cast<int32_t>(a.tokens_per_tile) || token >= q.rows) continue;
+      // the first CTA's piece begins the pair: its second slot; the others lie in their first
+      auto at = [&](uint32_t cta) {
+        return a.partials + static_cast<uint64_t>(2 * cta + (cta == c0)) * (2 * kTile * (DP + 2)) + x * kTile + r;
+      };
+      float m = -INFINITY, l = 0.f;
+      for (uint32_t c = c0; c <= c1; ++c) m = fmaxf(m, __ldcg(at(c) + DP * 2 * kTile));
       for (uint32_t c = c0; c <= c1; ++c) {
-        const float* from = at(c);
-        const float mc = __ldcg(from + DP * 2 * kTile);
-        if (mc == -INFINITY) continue;  // it saw nothing and left no sums
-        const float w = exp2_approx(mc - m) * inv;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) acc[k] = fmaf(w, __ldcg(from + (e + k) * 2 * kTile), acc[k]);
+        const float mc = __ldcg(at(c) + DP * 2 * kTile);
+        if (mc != -INFINITY) l += exp2_approx(mc - m) * __ldcg(at(c) + (DP + 1) * 2 * kTile);
       }
-      uint4 v;
-      v.x = pack2<T>(acc[0], acc[1]);
-      v.y = pack2<T>(acc[2], acc[3]);
-      v.z = pack2<T>(acc[4], acc[5]);
-      v.w = pack2<T>(acc[6], acc[7]);
-      *reinterpret_cast<uint4*>(to + e) = v;
+      const uint32_t h = head * a.group + g, tok = q.row + token;
+      const float inv = l > 0.f ? 1.f / l : 0.f;
+      T* to = static_cast<T*>(p.out) + tok * p.out_stride[0] + h * p.out_stride[1];
+#pragma unroll 1
+      for (int e = 0; e < static_cast<int>(p.head_dim); e += 64) {
+        float acc[64] = {};
+        for (uint32_t c = c0; c <= c1; ++c) {
+          const float* from = at(c);
+          const float mc = __ldcg(from + DP * 2 * kTile);
+          float part[64];
+#pragma unroll
+          for (int k = 0; k < 64; ++k) part[k] = __ldcg(from + (e + k) * 2 * kTile);
+          // a piece that saw nothing left no sums: what lies there may be anything
+          const float w = mc == -INFINITY ? 0.f : exp2_approx(mc - m) * inv;
+#pragma unroll
+          for (int k = 0; k < 64; ++k) acc[k] = fmaf(w, mc == -INFINITY ? 0.f : part[k], acc[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < 64; k += 8)
+          if (e + k < static_cast<int>(p.head_dim)) {
+            uint4 v;
+            v.x = pack2<T>(acc[k], acc[k + 1]);
+            v.y = pack2<T>(acc[k + 2], acc[k + 3]);
+            v.z = pack2<T>(acc[k + 4], acc[k + 5]);
+            v.w = pack2<T>(acc[k + 6], acc[k + 7]);
+            *reinterpret_cast<uint4*>(to + e + k) = v;
+          }
+      }
+      if (p.lse) p.lse[static_cast<uint64_t>(tok) * p.heads_q + h] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
     }
-    if (p.lse) p.lse[static_cast<uint64_t>(tok) * p.heads_q + h] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
   }
 }
 
