@@ -53,6 +53,9 @@ template <int DP> struct layout {      // DP: head_dim rounded up to 64 or 128
   static constexpr uint32_t kS = 0, kO = 256;
 };
 
+// Partial sums of a piece in groups of four floats: 256 rows of O, then a maximum and a sum for each.
+template <int DP> constexpr uint32_t kPartial = 2 * kTile * DP / 4 + kTile;
+
 // A piece of work: key tiles [tile, tile + count) of a pair of row tiles on one key head.
 struct item_t {
   int32_t count;                 // 0: no more
@@ -80,7 +83,7 @@ struct tiles_args {
   uint32_t* joined;   // a counter per CTA: pieces finished of the pair that it holds the beginning of
   uint4* pairs;       // request, pair within it, key tiles of the pairs before, key tiles
   uint32_t* order;    // pairs, longest first
-  float* partials;    // two per CTA
+  float4* partials;   // two per CTA
 };
 
 struct pair_range {
@@ -258,6 +261,12 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint3
       "r"(add), "n"(kOperandHigh)
       : "memory");
 }
+// One lane of the (converged) warp, always the same.
+__device__ __forceinline__ bool elected() {
+  uint32_t yes;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
+  return yes != 0;
+}
 // Arrives at the barrier when all matrix products issued before have finished.
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar)
@@ -359,8 +368,8 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
   const uint32_t q_full = kv_empty + 8 * L::kSlots, q_empty = q_full + 8;
   const uint32_t s_full = q_empty + 8, p_full = s_full + 16, o_full = p_full + 16;  // A, B each
   const uint32_t item_full = o_full + 16, item_empty = item_full + 16;             // two slots each
-  const uint32_t drained = item_empty + 16;
-  static_assert(8 * (2 * L::kSlots + 13) + 8 <= 512, "layout::kItems");
+  const uint32_t drained = item_empty + 16, h_full = drained + 8;
+  static_assert(8 * (2 * L::kSlots + 15) + 8 <= 504, "layout::kItems");
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + L::kBars + 504);
   item_t* items = reinterpret_cast<item_t*>(smem + L::kItems);
   uint32_t* joins = reinterpret_cast<uint32_t*>(smem + L::kItems + 2 * sizeof(item_t));  // 2 + 2 x 4 words
@@ -374,7 +383,8 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
     mbar_init(q_empty, 1);
     for (int x = 0; x < 2; ++x) {
       mbar_init(s_full + 8 * x, 1);
-      mbar_init(p_full + 8 * x, kTile);
+      mbar_init(p_full + 8 * x, kSoftWarps / 2);
+      mbar_init(h_full + 8 * x, kSoftWarps / 2);
       mbar_init(o_full + 8 * x, 1);
       mbar_init(item_full + 8 * x, 1);
       mbar_init(item_empty + 8 * x, kSoftWarps + 1);
@@ -552,25 +562,29 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
         const int32_t end = item.tile + item.count;
         uint32_t k_slot = 0, v_slot = 0;
         auto qk = [&](int x) {
-          const uint32_t q_op = operand(base + x * L::kQ, 16);
-          const uint32_t k_op = operand(base + L::kRing + k_slot * L::kSlot, 16);
-          if (lane == 0) {
+          const uint32_t q_op = __shfl_sync(kFull, operand(base + x * L::kQ, 16), 0);
+          const uint32_t k_op = __shfl_sync(kFull, operand(base + L::kRing + k_slot * L::kSlot, 16), 0);
+          const uint32_t d = __shfl_sync(kFull, tmem + L::kS + x * kTile, 0);
+          if (elected()) {
 #pragma unroll
             for (int ks = 0; ks < DP / 16; ++ks) {
               const uint32_t off = (ks / 4) * L::kHalf + (ks % 4) * 32;
-              mma_ss(tmem + L::kS + x * kTile, q_op + (off >> 4), k_op + (off >> 4), kQkShape, ks > 0);
+              mma_ss(d, q_op + (off >> 4), k_op + (off >> 4), kQkShape, ks > 0);
             }
             mma_commit(s_full + 8 * x);
           }
+          __syncwarp();
         };
-        auto pv = [&](int x, bool add) {
-          const uint32_t v_op = operand(base + L::kRing + v_slot * L::kSlot, L::kHalf);
-          if (lane == 0) {
+        auto pv = [&](int x, bool add, int from, int to) {
+          const uint32_t v_op = __shfl_sync(kFull, operand(base + L::kRing + v_slot * L::kSlot, L::kHalf), 0);
+          const uint32_t d = __shfl_sync(kFull, tmem + L::kO + x * DP, 0);
+          const uint32_t a_op = __shfl_sync(kFull, tmem + L::kS + x * kTile, 0);
+          if (elected()) {
 #pragma unroll
-            for (int ks = 0; ks < kTile / 16; ++ks)
-              mma_ts(tmem + L::kO + x * DP, tmem + L::kS + x * kTile + 8 * ks, v_op + (ks * 2048 >> 4), kPvShape,
-                     add || ks > 0);
+            for (int ks = from; ks < to; ++ks)
+              mma_ts(d, a_op + 8 * ks, v_op + (ks * 2048 >> 4), kPvShape, add || ks > 0);
           }
+          __syncwarp();
         };
         // keys of the first tile
         ok = mbar_wait(kv_full + 8 * kv.slot, kv.phase);
@@ -581,7 +595,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
 #pragma unroll
         for (int x = 0; x < 2; ++x)
           if (item.first[x] == item.tile && item.first[x] < item.last[x]) qk(x);
-        if (lane == 0) {
+        if (elected()) {
           mma_commit(kv_empty + 8 * k_slot);
           if (item.count == 1) mma_commit(q_empty);
         }
@@ -609,12 +623,17 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
             if (t >= item.first[x] && t < item.last[x]) {
+              // the product with the first half of P while the second is being made
+              ok = ok && mbar_wait(h_full + 8 * x, p_ring[x].phase);
+              if (!ok) break;
+              fence_after();
+              pv(x, t > item.first[x], 0, kTile / 32);
               ok = ok && mbar_wait(p_full + 8 * x, p_ring[x].phase);
               if (!ok) break;
               p_ring[x].step();
               fence_after();
-              pv(x, t > item.first[x]);
-              if (t + 1 == item.last[x] && lane == 0) mma_commit(o_full + 8 * x);
+              pv(x, true, kTile / 32, kTile / 16);
+              if (t + 1 == item.last[x] && elected()) mma_commit(o_full + 8 * x);
             }
             if (t + 1 >= item.first[x] && t + 1 < item.last[x]) {
               if (!k_waited) {
@@ -628,10 +647,10 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
             }
           }
           if (!ok) break;
-          if (lane == 0) mma_commit(kv_empty + 8 * v_slot);
+          if (elected()) mma_commit(kv_empty + 8 * v_slot);
           if (t + 1 < end) {  // A or B sees every key tile of the piece, so its keys were waited for
             kv.step();
-            if (lane == 0) {
+            if (elected()) {
               mma_commit(kv_empty + 8 * k_slot);
               if (t + 2 == end) mma_commit(q_empty);
             }
@@ -740,13 +759,20 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
             e[i / 2] = pack2<T>(z0, z1);
           }
           tmem_store16(s_at + c / 2, e);
+          if (c == 32) {  // the first half is there: its product may start
+            tmem_stored();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(h_full + 8 * x);
+          }
         }
         float l0, l1;
         unpair(add2(sums[0], sums[1]), l0, l1);
         l += l0 + l1;
         tmem_stored();
         fence_before();
-        mbar_arrive(p_full + 8 * x);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full + 8 * x);
       }
       if (!ok) break;
       const bool any = first < last;
@@ -781,8 +807,8 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
         if (p.lse && live)
           p.lse[static_cast<uint64_t>(tok) * p.heads_q + h] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
       } else {
-        // partial sums, a column of 256 rows after the other, then maxima and sums
-        float* to = a.partials + static_cast<uint64_t>(item.slot) * (2 * kTile * (DP + 2)) + x * kTile + r;
+        // partial sums, four columns of 256 rows after the other, then maxima and sums
+        float4* to = a.partials + static_cast<uint64_t>(item.slot) * kPartial<DP> + x * kTile + r;
         if (any)
 #pragma unroll 1
           for (int c = 0; c < DP; c += 32) {
@@ -790,10 +816,11 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
             tmem_load32(o, o_at + c);
             tmem_loaded(o);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) to[(c + i) * 2 * kTile] = __uint_as_float(o[i]);
+            for (int i = 0; i < 32; i += 4)
+              to[(c + i) / 4 * 2 * kTile] = make_float4(__uint_as_float(o[i]), __uint_as_float(o[i + 1]),
+                                                        __uint_as_float(o[i + 2]), __uint_as_float(o[i + 3]));
           }
-        to[DP * 2 * kTile] = m;
-        to[(DP + 1) * 2 * kTile] = l;
+        reinterpret_cast<float2*>(to - (x * kTile + r) + DP / 4 * 2 * kTile)[x * kTile + r] = make_float2(m, l);
       }
       fence_before();
     }
@@ -825,40 +852,62 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
       if (j >= static_cast<int32_t>(a.tokens_per_tile) || token >= q.rows) continue;
       // the first CTA's piece begins the pair: its second slot; the others lie in their first
       auto at = [&](uint32_t cta) {
-        return a.partials + static_cast<uint64_t>(2 * cta + (cta == c0)) * (2 * kTile * (DP + 2)) + x * kTile + r;
+        return a.partials + static_cast<uint64_t>(2 * cta + (cta == c0)) * kPartial<DP>;
       };
+      auto stats = [&](uint32_t cta) {
+        return __ldcg(reinterpret_cast<const float2*>(at(cta) + DP / 4 * 2 * kTile) + x * kTile + r);
+      };
+      // A few pieces at a time, so that their loads are on the way together; a piece that saw nothing
+      // (or is none) has the weight 0, and what lies in its place may be anything.
       float m = -INFINITY, l = 0.f;
-      for (uint32_t c = c0; c <= c1; ++c) m = fmaxf(m, __ldcg(at(c) + DP * 2 * kTile));
-      for (uint32_t c = c0; c <= c1; ++c) {
-        const float mc = __ldcg(at(c) + DP * 2 * kTile);
-        if (mc != -INFINITY) l += exp2_approx(mc - m) * __ldcg(at(c) + (DP + 1) * 2 * kTile);
+#pragma unroll 1
+      for (uint32_t c = c0; c <= c1; c += 4) {
+        float2 v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = stats(min(c + k, c1));  // the last one again: no matter
+        m = fmaxf(m, fmaxf(fmaxf(v[0].x, v[1].x), fmaxf(v[2].x, v[3].x)));
       }
       const uint32_t h = head * a.group + g, tok = q.row + token;
-      const float inv = l > 0.f ? 1.f / l : 0.f;
       T* to = static_cast<T*>(p.out) + tok * p.out_stride[0] + h * p.out_stride[1];
 #pragma unroll 1
-      for (int e = 0; e < static_cast<int>(p.head_dim); e += 64) {
-        float acc[64] = {};
-        for (uint32_t c = c0; c <= c1; ++c) {
-          const float* from = at(c);
-          const float mc = __ldcg(from + DP * 2 * kTile);
-          float part[64];
+      for (int e = 0; e < static_cast<int>(p.head_dim); e += 32) {
+        float acc[32] = {};
+        l = 0.f;
+#pragma unroll 1
+        for (uint32_t c = c0; c <= c1; c += 3) {
+          float2 v[3];
+          float4 part[3][8];
 #pragma unroll
-          for (int k = 0; k < 64; ++k) part[k] = __ldcg(from + (e + k) * 2 * kTile);
-          // a piece that saw nothing left no sums: what lies there may be anything
-          const float w = mc == -INFINITY ? 0.f : exp2_approx(mc - m) * inv;
+          for (int k = 0; k < 3; ++k) {
+            v[k] = stats(min(c + k, c1));
 #pragma unroll
-          for (int k = 0; k < 64; ++k) acc[k] = fmaf(w, mc == -INFINITY ? 0.f : part[k], acc[k]);
+            for (int i = 0; i < 8; ++i)
+              if (c + k <= c1) part[k][i] = __ldcg(at(c + k) + (e / 4 + i) * 2 * kTile + x * kTile + r);
+          }
+#pragma unroll
+          for (int k = 0; k < 3; ++k)
+            if (c + k <= c1 && v[k].x != -INFINITY) {
+              const float w = exp2_approx(v[k].x - m);
+              l = fmaf(w, v[k].y, l);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                acc[4 * i] = fmaf(w, part[k][i].x, acc[4 * i]);
+                acc[4 * i + 1] = fmaf(w, part[k][i].y, acc[4 * i + 1]);
+                acc[4 * i + 2] = fmaf(w, part[k][i].z, acc[4 * i + 2]);
+                acc[4 * i + 3] = fmaf(w, part[k][i].w, acc[4 * i + 3]);
+              }
+            }
         }
+        const float inv = l > 0.f ? 1.f / l : 0.f;
 #pragma unroll
-        for (int k = 0; k < 64; k += 8)
-          if (e + k < static_cast<int>(p.head_dim)) {
+        for (int i = 0; i < 32; i += 8)
+          if (e + i < static_cast<int>(p.head_dim)) {
             uint4 v;
-            v.x = pack2<T>(acc[k], acc[k + 1]);
-            v.y = pack2<T>(acc[k + 2], acc[k + 3]);
-            v.z = pack2<T>(acc[k + 4], acc[k + 5]);
-            v.w = pack2<T>(acc[k + 6], acc[k + 7]);
-            *reinterpret_cast<uint4*>(to + e + k) = v;
+            v.x = pack2<T>(acc[i] * inv, acc[i + 1] * inv);
+            v.y = pack2<T>(acc[i + 2] * inv, acc[i + 3] * inv);
+            v.z = pack2<T>(acc[i + 4] * inv, acc[i + 5] * inv);
+            v.w = pack2<T>(acc[i + 6] * inv, acc[i + 7] * inv);
+            *reinterpret_cast<uint4*>(to + e + i) = v;
           }
       }
       if (p.lse) p.lse[static_cast<uint64_t>(tok) * p.heads_q + h] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
@@ -897,7 +946,7 @@ namespace attend {
 uint64_t tiles_workspace(uint32_t n, uint32_t tokens, uint32_t group, uint32_t head_dim) {
   const uint64_t pairs = pairs_at_most(n, tokens, group);
   return up16(sizeof(tiles_head)) + up16(4 * kMaxTileCtas) + 16 * pairs + up16(4 * pairs) +
-         2ull * kMaxTileCtas * 2 * kTile * ((head_dim <= 64 ? 64 : 128) + 2) * 4;
+         2ull * kMaxTileCtas * (head_dim <= 64 ? kPartial<64> : kPartial<128>) * sizeof(float4);
 }
 
 cudaError_t launch_tiles(const preba_pages_attend_t& p, uint32_t page_shift, int sms, void* workspace,
@@ -921,7 +970,7 @@ cudaError_t launch_tiles(const preba_pages_attend_t& p, uint32_t page_shift, int
   at += 16 * pairs;
   a.order = reinterpret_cast<uint32_t*>(at);
   at += up16(4 * pairs);
-  a.partials = reinterpret_cast<float*>(at);
+  a.partials = reinterpret_cast<float4*>(at);
   const size_t smem = 4 * (static_cast<size_t>(p.n) + 1);
   if (smem > 32 * 1024) {
     const cudaError_t err = cudaFuncSetAttribute(tiles_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
