@@ -15,8 +15,8 @@
 // The work is a list of (request, pair of tiles, key head) with their numbers of key tiles.  If the
 // longest is short beside a CTA's share, CTAs claim them one by one, longest first.  Otherwise the
 // key tiles of all of them form one line, every CTA takes an equal run of it, and pieces that are not
-// whole leave partial sums which the last CTA to finish joins in the order of the keys.  Which, and
-// the list, is decided on the device by a planning kernel, as the lengths are there.
+// whole leave partial sums which a last kernel joins in the order of the keys.  Which, and the list, is
+// decided on the device by a planning kernel, as the lengths are there.
 #include <algorithm>
 
 #include <type_traits>
@@ -48,7 +48,7 @@ template <int DP> struct layout {      // DP: head_dim rounded up to 64 or 128
   static constexpr uint32_t kRing = 2 * kQ;
   static constexpr uint32_t kBars = kRing + kSlots * kSlot;
   static constexpr uint32_t kItems = kBars + 512;
-  static constexpr uint32_t kBytes = kItems + 512;
+  static constexpr uint32_t kBytes = kItems + 256;
   // tensor memory columns: S of A and B (P lies over them), O of A and B
   static constexpr uint32_t kS = 0, kO = 256;
 };
@@ -68,7 +68,7 @@ struct item_t {
   int32_t whole;                 // the piece is all of the pair's keys
   uint32_t slot;                 // else: where its partial sums go
 };
-static_assert(sizeof(item_t) <= 128, "layout::kItems");
+static_assert(2 * sizeof(item_t) <= 256, "layout::kBytes");
 
 // What the planning kernel leaves for the CTAs.
 struct tiles_head {
@@ -80,7 +80,6 @@ struct tiles_args {
   preba_pages_attend_t p;
   uint32_t page_shift, group, tokens_per_tile, box_rows, box_shift, grid, max_pairs;
   tiles_head* head;
-  uint32_t* joined;   // a counter per CTA: pieces finished of the pair that it holds the beginning of
   uint4* pairs;       // request, pair within it, key tiles of the pairs before, key tiles
   uint32_t* order;    // pairs, longest first
   float4* partials;   // two per CTA
@@ -146,9 +145,9 @@ __global__ void __launch_bounds__(kPlanThreads) tiles_plan_kernel(const tiles_ar
   extern __shared__ uint32_t pairs_before[];  // n + 1: pairs of the requests before
   __shared__ uint32_t warp_sums[32], bins[kBins], longest;
   const preba_pages_attend_t& p = a.p;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (threadIdx.x == 0) longest = 0;
   for (uint32_t b = threadIdx.x; b < kBins; b += kPlanThreads) bins[b] = 0;
-  for (uint32_t c = threadIdx.x; c < a.grid; c += kPlanThreads) a.joined[c] = 0;
 
   const uint32_t per = (p.n + kPlanThreads - 1) / kPlanThreads;
   const uint32_t r0 = min(threadIdx.x * per, p.n), r1 = min(r0 + per, p.n);
@@ -372,7 +371,6 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
   static_assert(8 * (2 * L::kSlots + 15) + 8 <= 504, "layout::kItems");
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + L::kBars + 504);
   item_t* items = reinterpret_cast<item_t*>(smem + L::kItems);
-  uint32_t* joins = reinterpret_cast<uint32_t*>(smem + L::kItems + 2 * sizeof(item_t));  // 2 + 2 x 4 words
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < L::kSlots; ++s) {
@@ -390,7 +388,6 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
       mbar_init(item_empty + 8 * x, kSoftWarps + 1);
     }
     mbar_init(drained, 1);
-    for (int i = 0; i < 10; ++i) joins[i] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == kMmaWarp) {
@@ -403,6 +400,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
   __syncthreads();
   fence_after();
   const uint32_t tmem = *tmem_slot;
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // for the plan
   bool ok = true;
 
   if (warp >= kSoftWarps) {
@@ -454,14 +452,6 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
           item.count = min(of.w - item.tile, unit_end - unit);
           item.whole = item.count == static_cast<int32_t>(of.w);
           item.slot = 2 * blockIdx.x + (item.tile == 0);
-          if (!item.whole && lane == 0) {  // to be joined at the end
-            const uint32_t start = unit - item.tile;
-            uint32_t* j = joins + 2 + 4 * (item.tile == 0);
-            j[0] = 1;
-            j[1] = pair * p.heads_kv + item.head;
-            j[2] = start / plan.per;
-            j[3] = (start + of.w - 1) / plan.per;
-          }
           unit += item.count;
           if (offset + item.count == of.w * p.heads_kv) ++pair;
         }
@@ -826,92 +816,97 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
     }
     if (!ok) report(p.status, PREBA_ERR_TIMEOUT);
 
-    // ---- join the CTAs' pieces: whoever finishes a pair on a key head last adds them up
     fence_before();
-    const bool claimed = a.head->claim;
-    if (!claimed) __threadfence();
     __syncthreads();
-    if (claimed) return;
-    if (threadIdx.x < 2) {
-      const uint32_t* j = joins + 2 + 4 * threadIdx.x;
-      uint32_t last = 0;
-      if (j[0]) last = atomicAdd(&a.joined[j[2]], 1) == j[3] - j[2];
-      __threadfence();
-      joins[threadIdx.x] = last;
+  }
+}
+
+// ---- joining ----------------------------------------------------------------------------------------
+//
+// Pairs of which several CTAs had a piece: a block adds up 32 columns of one, a thread a row.  All SMs
+// take part, which is why this is a kernel of its own (the last CTA of each pair doing it by itself kept
+// a third of the SMs busy for 10 to 20 us).
+
+constexpr int kJoinColumns = 32;
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(2 * kTile) tiles_join_kernel(const __grid_constant__ tiles_args a) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const tiles_head plan = *a.head;
+  if (plan.claim) return;
+  const preba_pages_attend_t& p = a.p;
+  const int x = threadIdx.x / kTile, r = threadIdx.x % kTile;
+  const int32_t j = r / static_cast<int32_t>(a.group), g = r - j * static_cast<int32_t>(a.group);
+  const uint32_t n = plan.n_pairs * p.heads_kv * (DP / kJoinColumns);
+  for (uint32_t unit = blockIdx.x; unit < n; unit += gridDim.x) {
+    const uint32_t e = unit % (DP / kJoinColumns) * kJoinColumns, of = unit / (DP / kJoinColumns);
+    const uint32_t which = of / p.heads_kv, head = of - which * p.heads_kv;
+    const uint4 info = a.pairs[which];
+    const uint32_t start = info.z * p.heads_kv + head * info.w;
+    const uint32_t first = start / plan.per, last = (start + info.w - 1) / plan.per;
+    if (first == last || e >= p.head_dim) continue;
+    request_t q;
+    load_request(p, info.x, q);
+    const int32_t token = (2 * info.y + x) * a.tokens_per_tile + j;
+    if (j >= static_cast<int32_t>(a.tokens_per_tile) || token >= q.rows) continue;
+    // the first CTA's piece begins the pair: its second slot; the others lie in their first
+    auto at = [&](uint32_t cta) {
+      return a.partials + static_cast<uint64_t>(2 * cta + (cta == first)) * kPartial<DP>;
+    };
+    auto stats = [&](uint32_t cta) {
+      return __ldcg(reinterpret_cast<const float2*>(at(cta) + DP / 4 * 2 * kTile) + threadIdx.x);
+    };
+    // a few pieces at a time, so that their loads are on the way together
+    float m = -INFINITY, l = 0.f;
+#pragma unroll 1
+    for (uint32_t c = first; c <= last; c += 4) {
+      float2 v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = stats(min(c + k, last));  // the last one again: no matter
+      m = fmaxf(m, fmaxf(fmaxf(v[0].x, v[1].x), fmaxf(v[2].x, v[3].x)));
     }
-    asm volatile("bar.sync 1, 256;" ::: "memory");
+    float acc[kJoinColumns] = {};
 #pragma unroll 1
-    for (int i = 0; i < 2; ++i) {
-      if (!joins[i]) continue;
-      const uint32_t* of = joins + 2 + 4 * i;
-      const uint32_t pair = of[1] / p.heads_kv, head = of[1] - pair * p.heads_kv, c0 = of[2], c1 = of[3];
-      const uint4 info = a.pairs[pair];
-      request_t q;
-      load_request(p, info.x, q);
-      const int32_t token = (2 * info.y + x) * a.tokens_per_tile + j;
-      if (j >= static_cast<int32_t>(a.tokens_per_tile) || token >= q.rows) continue;
-      // the first CTA's piece begins the pair: its second slot; the others lie in their first
-      auto at = [&](uint32_t cta) {
-        return a.partials + static_cast<uint64_t>(2 * cta + (cta == c0)) * kPartial<DP>;
-      };
-      auto stats = [&](uint32_t cta) {
-        return __ldcg(reinterpret_cast<const float2*>(at(cta) + DP / 4 * 2 * kTile) + x * kTile + r);
-      };
-      // A few pieces at a time, so that their loads are on the way together; a piece that saw nothing
-      // (or is none) has the weight 0, and what lies in its place may be anything.
-      float m = -INFINITY, l = 0.f;
-#pragma unroll 1
-      for (uint32_t c = c0; c <= c1; c += 4) {
-        float2 v[4];
+    for (uint32_t c = first; c <= last; c += 4) {
+      float2 v[4];
+      float4 part[4][kJoinColumns / 4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = stats(min(c + k, c1));  // the last one again: no matter
-        m = fmaxf(m, fmaxf(fmaxf(v[0].x, v[1].x), fmaxf(v[2].x, v[3].x)));
+      for (int k = 0; k < 4; ++k) {
+        v[k] = stats(min(c + k, last));
+#pragma unroll
+        for (int i = 0; i < kJoinColumns / 4; ++i)
+          part[k][i] = __ldcg(at(min(c + k, last)) + (e / 4 + i) * 2 * kTile + threadIdx.x);
       }
-      const uint32_t h = head * a.group + g, tok = q.row + token;
-      T* to = static_cast<T*>(p.out) + tok * p.out_stride[0] + h * p.out_stride[1];
-#pragma unroll 1
-      for (int e = 0; e < static_cast<int>(p.head_dim); e += 32) {
-        float acc[32] = {};
-        l = 0.f;
-#pragma unroll 1
-        for (uint32_t c = c0; c <= c1; c += 3) {
-          float2 v[3];
-          float4 part[3][8];
 #pragma unroll
-          for (int k = 0; k < 3; ++k) {
-            v[k] = stats(min(c + k, c1));
+      for (int k = 0; k < 4; ++k) {
+        // a piece that saw nothing left no sums: what lies in their place may be anything
+        if (c + k > last || v[k].x == -INFINITY) continue;
+        const float w = exp2_approx(v[k].x - m);
+        l = fmaf(w, v[k].y, l);
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-              if (c + k <= c1) part[k][i] = __ldcg(at(c + k) + (e / 4 + i) * 2 * kTile + x * kTile + r);
-          }
-#pragma unroll
-          for (int k = 0; k < 3; ++k)
-            if (c + k <= c1 && v[k].x != -INFINITY) {
-              const float w = exp2_approx(v[k].x - m);
-              l = fmaf(w, v[k].y, l);
-#pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                acc[4 * i] = fmaf(w, part[k][i].x, acc[4 * i]);
-                acc[4 * i + 1] = fmaf(w, part[k][i].y, acc[4 * i + 1]);
-                acc[4 * i + 2] = fmaf(w, part[k][i].z, acc[4 * i + 2]);
-                acc[4 * i + 3] = fmaf(w, part[k][i].w, acc[4 * i + 3]);
-              }
-            }
+        for (int i = 0; i < kJoinColumns / 4; ++i) {
+          acc[4 * i] = fmaf(w, part[k][i].x, acc[4 * i]);
+          acc[4 * i + 1] = fmaf(w, part[k][i].y, acc[4 * i + 1]);
+          acc[4 * i + 2] = fmaf(w, part[k][i].z, acc[4 * i + 2]);
+          acc[4 * i + 3] = fmaf(w, part[k][i].w, acc[4 * i + 3]);
         }
-        const float inv = l > 0.f ? 1.f / l : 0.f;
-#pragma unroll
-        for (int i = 0; i < 32; i += 8)
-          if (e + i < static_cast<int>(p.head_dim)) {
-            uint4 v;
-            v.x = pack2<T>(acc[i] * inv, acc[i + 1] * inv);
-            v.y = pack2<T>(acc[i + 2] * inv, acc[i + 3] * inv);
-            v.z = pack2<T>(acc[i + 4] * inv, acc[i + 5] * inv);
-            v.w = pack2<T>(acc[i + 6] * inv, acc[i + 7] * inv);
-            *reinterpret_cast<uint4*>(to + e + i) = v;
-          }
       }
-      if (p.lse) p.lse[static_cast<uint64_t>(tok) * p.heads_q + h] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
     }
+    const uint32_t h = head * a.group + g, tok = q.row + token;
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    T* to = static_cast<T*>(p.out) + tok * p.out_stride[0] + h * p.out_stride[1] + e;
+#pragma unroll
+    for (int i = 0; i < kJoinColumns; i += 8)
+      if (e + i < p.head_dim) {
+        uint4 v;
+        v.x = pack2<T>(acc[i] * inv, acc[i + 1] * inv);
+        v.y = pack2<T>(acc[i + 2] * inv, acc[i + 3] * inv);
+        v.z = pack2<T>(acc[i + 4] * inv, acc[i + 5] * inv);
+        v.w = pack2<T>(acc[i + 6] * inv, acc[i + 7] * inv);
+        *reinterpret_cast<uint4*>(to + i) = v;
+      }
+    if (p.lse && e == 0)
+      p.lse[static_cast<uint64_t>(tok) * p.heads_q + h] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
   }
 }
 
@@ -929,8 +924,23 @@ cudaError_t launch(const tiles_args& a, cudaStream_t stream) {
   if (err == cudaSuccess)
     err = cudaFuncSetAttribute(tiles_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes);
   if (err != cudaSuccess) return err;
-  tiles_kernel<T, DP><<<a.grid, kThreads, L::kBytes, stream>>>(map_q, map_k, map_v, a);
-  return cudaGetLastError();
+  // each kernel may be set up while the one before it runs; it waits for its results itself
+  cudaLaunchAttribute early;
+  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = a.grid;
+  cfg.blockDim = kThreads;
+  cfg.dynamicSmemBytes = L::kBytes;
+  cfg.stream = stream;
+  cfg.attrs = &early;
+  cfg.numAttrs = 1;
+  err = cudaLaunchKernelEx(&cfg, tiles_kernel<T, DP>, map_q, map_k, map_v, a);
+  if (err != cudaSuccess) return err;
+  cfg.gridDim = 2 * a.grid;
+  cfg.blockDim = 2 * kTile;
+  cfg.dynamicSmemBytes = 0;
+  return cudaLaunchKernelEx(&cfg, tiles_join_kernel<T, DP>, a);
 }
 
 uint64_t up16(uint64_t v) { return (v + 15) / 16 * 16; }
@@ -945,7 +955,7 @@ namespace attend {
 
 uint64_t tiles_workspace(uint32_t n, uint32_t tokens, uint32_t group, uint32_t head_dim) {
   const uint64_t pairs = pairs_at_most(n, tokens, group);
-  return up16(sizeof(tiles_head)) + up16(4 * kMaxTileCtas) + 16 * pairs + up16(4 * pairs) +
+  return up16(sizeof(tiles_head)) + 16 * pairs + up16(4 * pairs) +
          2ull * kMaxTileCtas * (head_dim <= 64 ? kPartial<64> : kPartial<128>) * sizeof(float4);
 }
 
@@ -964,8 +974,6 @@ cudaError_t launch_tiles(const preba_pages_attend_t& p, uint32_t page_shift, int
   uint8_t* at = static_cast<uint8_t*>(workspace);
   a.head = reinterpret_cast<tiles_head*>(at);
   at += up16(sizeof(tiles_head));
-  a.joined = reinterpret_cast<uint32_t*>(at);
-  at += up16(4 * kMaxTileCtas);
   a.pairs = reinterpret_cast<uint4*>(at);
   at += 16 * pairs;
   a.order = reinterpret_cast<uint32_t*>(at);
