@@ -823,14 +823,14 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
 
 // ---- joining ----------------------------------------------------------------------------------------
 //
-// Pairs of which several CTAs had a piece: a block adds up 32 columns of one, a thread a row.  All SMs
+// Pairs of which several CTAs had a piece: a block adds up 16 columns of one, a thread a row.  All SMs
 // take part, which is why this is a kernel of its own (the last CTA of each pair doing it by itself kept
 // a third of the SMs busy for 10 to 20 us).
 
-constexpr int kJoinColumns = 32;
+constexpr int kJoinColumns = 16;
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(2 * kTile) tiles_join_kernel(const __grid_constant__ tiles_args a) {
+__global__ void __launch_bounds__(2 * kTile, 2) tiles_join_kernel(const __grid_constant__ tiles_args a) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const tiles_head plan = *a.head;
   if (plan.claim) return;
@@ -847,36 +847,28 @@ __global__ void __launch_bounds__(2 * kTile) tiles_join_kernel(const __grid_cons
     if (first == last || e >= p.head_dim) continue;
     request_t q;
     load_request(p, info.x, q);
-    const int32_t token = (2 * info.y + x) * a.tokens_per_tile + j;
-    if (j >= static_cast<int32_t>(a.tokens_per_tile) || token >= q.rows) continue;
-    // the first CTA's piece begins the pair: its second slot; the others lie in their first
-    auto at = [&](uint32_t cta) {
-      return a.partials + static_cast<uint64_t>(2 * cta + (cta == first)) * kPartial<DP>;
-    };
-    auto stats = [&](uint32_t cta) {
-      return __ldcg(reinterpret_cast<const float2*>(at(cta) + DP / 4 * 2 * kTile) + threadIdx.x);
-    };
-    // a few pieces at a time, so that their loads are on the way together
-    float m = -INFINITY, l = 0.f;
-#pragma unroll 1
-    for (uint32_t c = first; c <= last; c += 4) {
-      float2 v[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] = stats(min(c + k, last));  // the last one again: no matter
-      m = fmaxf(m, fmaxf(fmaxf(v[0].x, v[1].x), fmaxf(v[2].x, v[3].x)));
-    }
-    float acc[kJoinColumns] = {};
+    // Pieces in the order of the keys, four at a time so that their loads are on the way together; the
+    // first CTA's piece begins the pair and lies in its second slot, the others in their first.
+    float m = -INFINITY, l = 0.f, acc[kJoinColumns] = {};
 #pragma unroll 1
     for (uint32_t c = first; c <= last; c += 4) {
       float2 v[4];
       float4 part[4][kJoinColumns / 4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        v[k] = stats(min(c + k, last));
+        const uint32_t cta = min(c + k, last);  // the last one again: it is not counted
+        const float4* from = a.partials + static_cast<uint64_t>(2 * cta + (cta == first)) * kPartial<DP>;
+        v[k] = __ldcg(reinterpret_cast<const float2*>(from + DP / 4 * 2 * kTile) + threadIdx.x);
 #pragma unroll
         for (int i = 0; i < kJoinColumns / 4; ++i)
-          part[k][i] = __ldcg(at(min(c + k, last)) + (e / 4 + i) * 2 * kTile + threadIdx.x);
+          part[k][i] = __ldcg(from + (e / 4 + i) * 2 * kTile + threadIdx.x);
       }
+      const float to = fmaxf(m, fmaxf(fmaxf(v[0].x, v[1].x), fmaxf(v[2].x, v[3].x)));
+      const float keep = to == -INFINITY ? 0.f : exp2_approx(m - to);
+      m = to;
+      l *= keep;
+#pragma unroll
+      for (int i = 0; i < kJoinColumns; ++i) acc[i] *= keep;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         // a piece that saw nothing left no sums: what lies in their place may be anything
@@ -892,6 +884,8 @@ __global__ void __launch_bounds__(2 * kTile) tiles_join_kernel(const __grid_cons
         }
       }
     }
+    const int32_t token = (2 * info.y + x) * a.tokens_per_tile + j;
+    if (j >= static_cast<int32_t>(a.tokens_per_tile) || token >= q.rows) continue;
     const uint32_t h = head * a.group + g, tok = q.row + token;
     const float inv = l > 0.f ? 1.f / l : 0.f;
     T* to = static_cast<T*>(p.out) + tok * p.out_stride[0] + h * p.out_stride[1] + e;
@@ -937,7 +931,7 @@ cudaError_t launch(const tiles_args& a, cudaStream_t stream) {
   cfg.numAttrs = 1;
   err = cudaLaunchKernelEx(&cfg, tiles_kernel<T, DP>, map_q, map_k, map_v, a);
   if (err != cudaSuccess) return err;
-  cfg.gridDim = 2 * a.grid;
+  cfg.gridDim = 4 * a.grid;
   cfg.blockDim = 2 * kTile;
   cfg.dynamicSmemBytes = 0;
   return cudaLaunchKernelEx(&cfg, tiles_join_kernel<T, DP>, a);
