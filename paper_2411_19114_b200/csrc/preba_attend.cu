@@ -1,6 +1,7 @@
 // Attention of a step's tokens over the paged cache (preba_tokens.h): preba_pages_attend.
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "preba_attend.h"
 
@@ -25,16 +26,16 @@ constexpr int kRowsMax = 16;
 constexpr int kTileKeys = 64;
 constexpr int kWarps = 4;                      // of consumers; one more warp issues the copies
 constexpr int kFewThreads = 32 * (kWarps + 1);
-constexpr uint32_t kMinTiles = 4;              // a CTA's run is not shorter than this
+constexpr uint32_t kMinTiles = 2;              // a CTA's run is not shorter than this
 
 template <int DP> struct few_layout {          // DP: head_dim rounded up to 64 or 128
   static constexpr int kHalves = DP / 64;
   static constexpr uint32_t kOperand = kTileKeys * DP * 2;  // bytes of a tile's keys (or values)
   static constexpr uint32_t kStage = 2 * kOperand;
   static constexpr int kStages = 3 * 128 / DP;
-  static constexpr uint32_t kJoin = kStages * kStage;            // two slots of 16 x DP floats
-  static constexpr uint32_t kStats = kJoin + 2 * kRowsMax * DP * 4;  // their maxima and sums
-  static constexpr uint32_t kBars = kStats + 2 * 2 * kRowsMax * 4;
+  static constexpr uint32_t kJoin = kStages * kStage;             // eight rows of each warp's sums
+  static constexpr uint32_t kStats = kJoin + kWarps * 8 * DP * 4;  // the warps' maxima and sums
+  static constexpr uint32_t kBars = kStats + kWarps * 2 * kRowsMax * 4;
   static constexpr uint32_t kControl = kBars + 2 * kStages * 8;
   static constexpr uint32_t kBytes = kControl + 128;
   static constexpr uint32_t kPartial = kRowsMax * DP * 4 + 2 * kRowsMax * 4;  // of one partial sum
@@ -209,11 +210,19 @@ __device__ __forceinline__ void store_rows(const few_args& a, const request_t& q
   }
 }
 
+// Partial sums of a CTA's first (slot 0) or last piece: pairs of columns in the fragment layout, rows 0 to
+// 7, then rows 8 to 15, then a maximum and a sum for each row.
+template <int DP> __device__ __forceinline__ float2* partial_of(const preba_pages_attend_t& p, uint32_t cta, uint32_t slot) {
+  return reinterpret_cast<float2*>(static_cast<uint8_t*>(p.workspace) + kCounterBytes +
+                                   static_cast<uint64_t>(2 * cta + slot) * few_layout<DP>::kPartial);
+}
+
 template <typename T, int DP>
 __global__ void __launch_bounds__(kFewThreads, 2)
 few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                 const __grid_constant__ few_args a) {
   using L = few_layout<DP>;
+  constexpr int kTiles = DP / 8 / kWarps;  // column groups of a warp where the work is split by columns
   extern __shared__ __align__(1024) uint8_t smem[];
   const preba_pages_attend_t& p = a.p;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -226,8 +235,11 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
       mbar_init(empty + 8 * s, kWarps);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
     ctl.pieces[0].live = ctl.pieces[1].live = 0;
   }
+  chained_begin();
   find_run(a, &ctl.run, ctl.warp_sums);  // synchronises
   const run_t run = ctl.run;
   if (run.begin >= run.end) return;
@@ -405,78 +417,77 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
       l[i] += __shfl_xor_sync(kFull, l[i], 1);
       l[i] += __shfl_xor_sync(kFull, l[i], 2);
     }
-    // ---- join the warps: 2 and 3 hand their sums to 0 and 1, then 1 to 0
+    // ---- join the warps: every warp lays its sums down, scaled to the common maximum, eight rows at a
+    // time, and adds up a quarter of the columns of all four
     float* join = reinterpret_cast<float*>(smem + L::kJoin);
     float* stats = reinterpret_cast<float*>(smem + L::kStats);
-    auto give = [&](int slot) {
-      float* to = join + slot * (kRowsMax * DP);
-#pragma unroll
-      for (int n = 0; n < DP / 8; ++n)
-#pragma unroll
-        for (int c = 0; c < 4; ++c) to[(4 * n + c) * 32 + lane] = o[n][c];
-      if ((lane & 3) == 0)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          stats[(slot * 2 + 0) * kRowsMax + (lane >> 2) + 8 * i] = m[i];
-          stats[(slot * 2 + 1) * kRowsMax + (lane >> 2) + 8 * i] = l[i];
-        }
-    };
-    auto take = [&](int slot) {
-      const float* from = join + slot * (kRowsMax * DP);
+    if ((lane & 3) == 0)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const float mo = stats[(slot * 2 + 0) * kRowsMax + (lane >> 2) + 8 * i];
-        const float lo = stats[(slot * 2 + 1) * kRowsMax + (lane >> 2) + 8 * i];
-        const float both = fmaxf(m[i], mo);
-        const float x = both == -INFINITY ? 0.f : exp2_approx(m[i] - both);
-        const float y = both == -INFINITY ? 0.f : exp2_approx(mo - both);
-        m[i] = both;
-        l[i] = l[i] * x + lo * y;
-#pragma unroll
-        for (int n = 0; n < DP / 8; ++n)
-#pragma unroll
-          for (int c = 2 * i; c < 2 * i + 2; ++c) o[n][c] = o[n][c] * x + from[(4 * n + c) * 32 + lane] * y;
+        stats[(2 * warp + 0) * kRowsMax + (lane >> 2) + 8 * i] = m[i];
+        stats[(2 * warp + 1) * kRowsMax + (lane >> 2) + 8 * i] = l[i];
       }
-    };
-    consumers_sync();  // the slots of the piece before have been read
-    if (warp >= 2) give(warp - 2);
     consumers_sync();
-    if (warp < 2) take(warp);
-    if (warp == 1) {
-      __syncwarp();
-      give(1);
+    float mine[2] = {m[0], m[1]};
+    float r[kTiles][4];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      float part[kWarps];
+#pragma unroll
+      for (int k = 0; k < kWarps; ++k) part[k] = stats[2 * k * kRowsMax + (lane >> 2) + 8 * i];
+      m[i] = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+      l[i] = 0.f;
+#pragma unroll
+      for (int k = 0; k < kWarps; ++k)
+        if (part[k] != -INFINITY)
+          l[i] += exp2_approx(part[k] - m[i]) * stats[(2 * k + 1) * kRowsMax + (lane >> 2) + 8 * i];
     }
-    consumers_sync();
-    if (warp == 0) {
-      take(1);
-      if (w.count == w.tiles) {
-        store_rows<T, DP / 8>(a, w.q, w.head, o, l, m, 0);
-      } else {
-        const uint32_t slot = w.tile == 0;
-        float* to = reinterpret_cast<float*>(static_cast<uint8_t*>(p.workspace) + kCounterBytes +
-                                             static_cast<uint64_t>(2 * blockIdx.x + slot) * L::kPartial);
 #pragma unroll
-        for (int n = 0; n < DP / 8; ++n)
+    for (int i = 0; i < 2; ++i) {
 #pragma unroll
-          for (int c = 0; c < 4; ++c)
-            if (c < 2 || rows > 8) to[(4 * n + c) * 32 + lane] = o[n][c];
-        if ((lane & 3) == 0)
+      for (int n = 0; n < kTiles; ++n) r[n][2 * i] = r[n][2 * i + 1] = 0.f;
+      if (i == 1 && rows <= 8) break;
+      const float keep = mine[i] == -INFINITY ? 0.f : exp2_approx(mine[i] - m[i]);
+      float2* to = reinterpret_cast<float2*>(join) + warp * (DP / 8) * 32 + lane;
+      if (i) consumers_sync();  // the first eight rows have been added up
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            to[kRowsMax * DP + (lane >> 2) + 8 * i] = m[i];
-            to[kRowsMax * DP + kRowsMax + (lane >> 2) + 8 * i] = l[i];
-          }
-        if (lane == 0) {
-          const uint32_t start = w.unit - w.count - w.tile;  // of the (request, key head)
-          ctl.pieces[slot] = {1, w.request, w.head, start / run.per, (start + w.tiles - 1) / run.per};
+      for (int n = 0; n < DP / 8; ++n) to[n * 32] = make_float2(o[n][2 * i] * keep, o[n][2 * i + 1] * keep);
+      consumers_sync();
+#pragma unroll
+      for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+        for (int k = 0; k < kWarps; ++k) {
+          const float2 v = (reinterpret_cast<const float2*>(join) + lane)[(k * (DP / 8) + kTiles * warp + n) * 32];
+          r[n][2 * i] += v.x;
+          r[n][2 * i + 1] += v.y;
         }
+    }
+    if (w.count == w.tiles) {
+      store_rows<T, kTiles>(a, w.q, w.head, r, l, m, kTiles * warp);
+    } else {
+      const uint32_t slot = w.tile == 0;
+      float2* to = partial_of<DP>(p, blockIdx.x, slot) + lane;
+#pragma unroll
+      for (int n = 0; n < kTiles; ++n) {
+        to[(kTiles * warp + n) * 32] = make_float2(r[n][0], r[n][1]);
+        if (rows > 8) to[(DP / 8 + kTiles * warp + n) * 32] = make_float2(r[n][2], r[n][3]);
+      }
+      if (warp == 0 && (lane & 3) == 0)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          (to - lane)[kRowsMax * DP / 2 + (lane >> 2) + 8 * i] = make_float2(m[i], l[i]);
+      if (threadIdx.x == 0) {
+        const uint32_t start = w.unit - w.count - w.tile;  // of the (request, key head)
+        ctl.pieces[slot] = {1, w.request, w.head, start / run.per, (start + w.tiles - 1) / run.per};
       }
     }
+    consumers_sync();  // what the warps laid down has been read
   }
   if (!ok) report(p.status, PREBA_ERR_TIMEOUT);
 
   // ---- join the CTAs: whoever finishes a (request, key head) last adds its pieces up
-  if (warp == 0) __threadfence();
+  if (!ctl.pieces[0].live && !ctl.pieces[1].live) return;
+  __threadfence();
   consumers_sync();
   uint32_t* counters = static_cast<uint32_t*>(p.workspace);
   if (threadIdx.x < 2) {
@@ -494,37 +505,47 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
   for (int i = 0; i < 2; ++i) {
     if (!ctl.joins[i]) continue;
     const piece_t x = ctl.pieces[i];
-    const uint8_t* partials = static_cast<const uint8_t*>(p.workspace) + kCounterBytes;
-    // the first CTA's piece begins the (request, key head): slot 1; the others lie in slot 0
-    auto at = [&](uint32_t cta) {
-      return reinterpret_cast<const float*>(
-          partials + static_cast<uint64_t>(2 * cta + (cta == x.first)) * L::kPartial);
-    };
     request_t q;
     load_request(p, x.request, q);
-    const bool tall = q.rows * a.group > 8;
-    float top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
-    for (uint32_t cta = x.first; cta <= x.last; ++cta)
+    float top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f}, acc[kTiles][4] = {};
+    // in the order of the keys, a few pieces at a time so that their loads are on the way together
+    auto add = [&](auto count, auto first_row) {
+      constexpr int N = decltype(count)::value, h = decltype(first_row)::value;
+#pragma unroll 1
+      for (uint32_t c = x.first; c <= x.last; c += N) {
+        float2 stat[N], part[N][kTiles];
 #pragma unroll
-      for (int k = 0; k < 2; ++k) top[k] = fmaxf(top[k], __ldcg(at(cta) + kRowsMax * DP + (lane >> 2) + 8 * k));
-    constexpr int kTiles = DP / 8 / kWarps;  // column groups of a warp
-    float acc[kTiles][4] = {};
-#pragma unroll 2
-    for (uint32_t cta = x.first; cta <= x.last; ++cta) {
-      const float* from = at(cta);
-      float e[2];
+        for (int k = 0; k < N; ++k) {
+          const uint32_t cta = min(c + k, x.last);  // the last one again: it is not counted
+          // the first CTA's piece begins the (request, key head): slot 1; the others lie in slot 0
+          const float2* from = partial_of<DP>(p, cta, cta == x.first);
+          stat[k] = __ldcg(from + kRowsMax * DP / 2 + (lane >> 2) + 8 * h);
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const float mk = __ldcg(from + kRowsMax * DP + (lane >> 2) + 8 * k);
-        e[k] = mk == -INFINITY ? 0.f : exp2_approx(mk - top[k]);
-        sum[k] += e[k] * __ldcg(from + kRowsMax * DP + kRowsMax + (lane >> 2) + 8 * k);
+          for (int n = 0; n < kTiles; ++n) part[k][n] = __ldcg(from + (h * (DP / 8) + kTiles * warp + n) * 32 + lane);
+        }
+        float to = top[h];
+#pragma unroll
+        for (int k = 0; k < N; ++k) to = fmaxf(to, stat[k].x);
+        const float keep = to == -INFINITY ? 0.f : exp2_approx(top[h] - to);
+        top[h] = to;
+        sum[h] *= keep;
+#pragma unroll
+        for (int n = 0; n < kTiles; ++n) acc[n][2 * h] *= keep, acc[n][2 * h + 1] *= keep;
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+          const float e = c + k > x.last || stat[k].x == -INFINITY ? 0.f : exp2_approx(stat[k].x - to);
+          sum[h] = fmaf(e, stat[k].y, sum[h]);
+#pragma unroll
+          for (int n = 0; n < kTiles; ++n) {
+            acc[n][2 * h] = fmaf(e, part[k][n].x, acc[n][2 * h]);
+            acc[n][2 * h + 1] = fmaf(e, part[k][n].y, acc[n][2 * h + 1]);
+          }
+        }
       }
-#pragma unroll
-      for (int n = 0; n < kTiles; ++n)
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-          if (c < 2 || tall) acc[n][c] += e[c >> 1] * __ldcg(from + (4 * (kTiles * warp + n) + c) * 32 + lane);
-    }
+    };
+    using std::integral_constant;
+    add(integral_constant<int, 8>(), integral_constant<int, 0>());
+    if (q.rows * a.group > 8) add(integral_constant<int, 8>(), integral_constant<int, 1>());
     store_rows<T, kTiles>(a, q, x.head, acc, sum, top, kTiles * warp);
   }
 }
@@ -612,8 +633,7 @@ cudaError_t launch_few(const few_args& a, int sms, cudaStream_t stream) {
                                few_layout<DP>::kBytes);
   if (err != cudaSuccess) return err;
   const int grid = std::min(2 * sms, kMaxSplitCtas);
-  few_rows_kernel<T, DP><<<grid, kFewThreads, few_layout<DP>::kBytes, stream>>>(map_k, map_v, a);
-  return cudaGetLastError();
+  return launch_chained(few_rows_kernel<T, DP>, grid, kFewThreads, few_layout<DP>::kBytes, stream, map_k, map_v, a);
 }
 
 bool operand_ok(const void* base, const uint64_t* strides, int count) {

@@ -145,9 +145,9 @@ __global__ void __launch_bounds__(kPlanThreads) tiles_plan_kernel(const tiles_ar
   extern __shared__ uint32_t pairs_before[];  // n + 1: pairs of the requests before
   __shared__ uint32_t warp_sums[32], bins[kBins], longest;
   const preba_pages_attend_t& p = a.p;
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (threadIdx.x == 0) longest = 0;
   for (uint32_t b = threadIdx.x; b < kBins; b += kPlanThreads) bins[b] = 0;
+  chained_begin();
 
   const uint32_t per = (p.n + kPlanThreads - 1) / kPlanThreads;
   const uint32_t r0 = min(threadIdx.x * per, p.n), r1 = min(r0 + per, p.n);
@@ -400,7 +400,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
   __syncthreads();
   fence_after();
   const uint32_t tmem = *tmem_slot;
-  asm volatile("griddepcontrol.wait;" ::: "memory");  // for the plan
+  chained_begin();
   bool ok = true;
 
   if (warp >= kSoftWarps) {
@@ -831,7 +831,7 @@ constexpr int kJoinColumns = 16;
 
 template <typename T, int DP>
 __global__ void __launch_bounds__(2 * kTile, 2) tiles_join_kernel(const __grid_constant__ tiles_args a) {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  chained_begin();
   const tiles_head plan = *a.head;
   if (plan.claim) return;
   const preba_pages_attend_t& p = a.p;
@@ -918,23 +918,9 @@ cudaError_t launch(const tiles_args& a, cudaStream_t stream) {
   if (err == cudaSuccess)
     err = cudaFuncSetAttribute(tiles_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes);
   if (err != cudaSuccess) return err;
-  // each kernel may be set up while the one before it runs; it waits for its results itself
-  cudaLaunchAttribute early;
-  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  early.val.programmaticStreamSerializationAllowed = 1;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = a.grid;
-  cfg.blockDim = kThreads;
-  cfg.dynamicSmemBytes = L::kBytes;
-  cfg.stream = stream;
-  cfg.attrs = &early;
-  cfg.numAttrs = 1;
-  err = cudaLaunchKernelEx(&cfg, tiles_kernel<T, DP>, map_q, map_k, map_v, a);
+  err = launch_chained(tiles_kernel<T, DP>, a.grid, kThreads, L::kBytes, stream, map_q, map_k, map_v, a);
   if (err != cudaSuccess) return err;
-  cfg.gridDim = 4 * a.grid;
-  cfg.blockDim = 2 * kTile;
-  cfg.dynamicSmemBytes = 0;
-  return cudaLaunchKernelEx(&cfg, tiles_join_kernel<T, DP>, a);
+  return launch_chained(tiles_join_kernel<T, DP>, 4 * a.grid, 2 * kTile, 0, stream, a);
 }
 
 uint64_t up16(uint64_t v) { return (v + 15) / 16 * 16; }
@@ -979,8 +965,7 @@ cudaError_t launch_tiles(const preba_pages_attend_t& p, uint32_t page_shift, int
                                                  4 * (PREBA_PAGES_MAX_REQUESTS + 1));
     if (err != cudaSuccess) return err;
   }
-  tiles_plan_kernel<<<1, kPlanThreads, smem, stream>>>(a);
-  const cudaError_t err = cudaGetLastError();
+  const cudaError_t err = launch_chained(tiles_plan_kernel, 1, kPlanThreads, smem, stream, a);
   if (err != cudaSuccess) return err;
   if (p.dtype == PREBA_F16)
     return p.head_dim <= 64 ? launch<__half, 64>(a, stream) : launch<__half, 128>(a, stream);

@@ -35,4 +35,36 @@ __device__ __forceinline__ bool range_violation(int32_t* status) {
 #define PREBA_IN_RANGE(status, cond) true
 #endif
 
+#if defined(__CUDACC__)
+#include <cuda_runtime.h>
+
+// Kernels of the serving step follow one another within microseconds.  Each is launched so that its
+// thread blocks may be set up while the kernel before it on the stream still runs; chained_begin() waits
+// for everything before it to be complete and then lets the kernel behind it be set up likewise.  No block
+// touches memory that another kernel may write or read before it has passed, and every block has to
+// pass, even one with nothing to do: so stream order holds as for any launch, whatever the neighbours are.
+namespace preba {
+__device__ __forceinline__ void chained_begin() {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
+template <typename... Params, typename... Args>
+cudaError_t launch_chained(void (*kernel)(Params...), uint32_t grid, uint32_t block, size_t smem,
+                           cudaStream_t stream, const Args&... args) {
+  cudaLaunchAttribute early;
+  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cfg.attrs = &early;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+}  // namespace preba
+#endif
+
 #endif  // PREBA_INTERNAL_H_

@@ -64,6 +64,7 @@ __device__ __forceinline__ uint32_t last_not_above(const int32_t* a, uint32_t n,
 __global__ void __launch_bounds__(kPlanThreads)
 plan_kernel(const preba_pages_plan_t p, const uint32_t page_shift) {
   extern __shared__ int32_t plan_smem[];
+  chained_begin();
   int32_t* cu = plan_smem;               // n + 1: first row of each request
   int32_t* first = plan_smem + p.n + 1;  // n: new pages before the request's, or -1: refused
   __shared__ int64_t warp_sums[kPlanThreads / 32];
@@ -237,6 +238,7 @@ __device__ __forceinline__ span_t load_span(const int32_t* spans, uint32_t i, in
 
 __global__ void __launch_bounds__(kPosThreads)
 positions_kernel(const preba_rope_positions_t p, const uint32_t run) {
+  chained_begin();
   const uint32_t lane = threadIdx.x & 31;
   const uint64_t warp = (static_cast<uint64_t>(blockIdx.x) * kPosThreads + threadIdx.x) >> 5;
   const uint64_t first = warp * run;
@@ -362,6 +364,7 @@ __device__ __forceinline__ uint32_t axis_of(uint32_t j, const uint32_t (&section
 template <typename T>
 __global__ void __launch_bounds__(kRopeThreads)
 append_kernel(const preba_rope_append_t p, const uint32_t page_shift) {
+  chained_begin();
   __shared__ float2 turn[kRopeTokens][PREBA_PAGES_MAX_HEAD_DIM / 2];
   const uint32_t t0 = blockIdx.x * kRopeTokens;
   const uint32_t n_tok = min(kRopeTokens, p.tokens - t0);
@@ -488,8 +491,8 @@ extern "C" int preba_pages_plan(const preba_pages_plan_t* plan, void* stream) {
     if (rc != PREBA_OK) return rc;
   }
   const uint32_t grid = std::max(1u, (p.tokens + kPlanTokensPerCta - 1) / kPlanTokensPerCta);
-  plan_kernel<<<grid, kPlanThreads, smem, static_cast<cudaStream_t>(stream)>>>(p, log2_of(p.page_size));
-  return finish(cudaGetLastError());
+  return finish(launch_chained(plan_kernel, grid, kPlanThreads, smem, static_cast<cudaStream_t>(stream), p,
+                               log2_of(p.page_size)));
 }
 
 extern "C" int preba_rope_positions(const preba_rope_positions_t* req, void* stream) {
@@ -504,8 +507,7 @@ extern "C" int preba_rope_positions(const preba_rope_positions_t* req, void* str
   const uint32_t run = std::min(256u, (p.tokens + 2367) / 2368);
   const uint64_t warps = (p.tokens + run - 1) / run;
   const uint32_t grid = static_cast<uint32_t>((warps * 32 + kPosThreads - 1) / kPosThreads);
-  positions_kernel<<<grid, kPosThreads, 0, static_cast<cudaStream_t>(stream)>>>(p, run);
-  return finish(cudaGetLastError());
+  return finish(launch_chained(positions_kernel, grid, kPosThreads, 0, static_cast<cudaStream_t>(stream), p, run));
 }
 
 extern "C" int preba_rope_append(const preba_rope_append_t* req, void* stream) {
@@ -543,9 +545,6 @@ extern "C" int preba_rope_append(const preba_rope_append_t* req, void* stream) {
   const uint32_t grid = (p.tokens + kRopeTokens - 1) / kRopeTokens;
   const uint32_t shift = p.heads_kv ? log2_of(p.page_size) : 3;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (p.dtype == PREBA_F16)
-    append_kernel<__half><<<grid, kRopeThreads, 0, s>>>(p, shift);
-  else
-    append_kernel<__nv_bfloat16><<<grid, kRopeThreads, 0, s>>>(p, shift);
-  return finish(cudaGetLastError());
+  return finish(launch_chained(p.dtype == PREBA_F16 ? append_kernel<__half> : append_kernel<__nv_bfloat16>, grid,
+                               kRopeThreads, 0, s, p, shift));
 }
