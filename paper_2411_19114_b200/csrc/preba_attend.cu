@@ -675,7 +675,7 @@ extern "C" int preba_pages_attend(const preba_pages_attend_t* req, void* stream)
       (p.page_size & (p.page_size - 1)) || p.table_stride < p.table_width ||
       (p.dtype != PREBA_F16 && p.dtype != PREBA_BF16) || (p.flags & ~PREBA_ATTEND_CAUSAL) ||
       p.window > INT32_MAX || p.pages > INT32_MAX / p.page_size || !strides_used(p) ||
-      static_cast<double>(p.n) * p.heads_kv * (static_cast<double>(p.table_width) * p.page_size / 64 + 2) > 4e9 ||
+      static_cast<double>(p.n) * p.heads_kv * (static_cast<double>(p.table_width) * p.page_size / 64 + 2) > 2e9 ||
       !(p.scale > 0.f) || !(p.scale < INFINITY))
     return PREBA_ERR_INVALID_ARG;
   if (!p.workspace || (reinterpret_cast<uintptr_t>(p.workspace) & 15)) return PREBA_ERR_INVALID_ARG;

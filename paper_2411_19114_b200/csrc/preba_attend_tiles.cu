@@ -76,11 +76,21 @@ struct tiles_head {
   uint32_t n_pairs, units, claim, per;
 };
 
+// Two row tiles of a request.
+struct pair_t {
+  uint32_t request, pair;   // and which pair of it
+  uint32_t before, tiles;   // key tiles of the pairs before, key tiles
+  int32_t row, rows, keys;  // the request
+  uint32_t reserved;
+};
+static_assert(sizeof(pair_t) == 32, "two vector loads");
+
 struct tiles_args {
   preba_pages_attend_t p;
   uint32_t page_shift, group, tokens_per_tile, box_rows, box_shift, grid, max_pairs;
   tiles_head* head;
-  uint4* pairs;       // request, pair within it, key tiles of the pairs before, key tiles
+  pair_t* pairs;
+  uint32_t* begin;    // of every CTA's run in the line: the pair
   uint32_t* order;    // pairs, longest first
   float4* partials;   // two per CTA
 };
@@ -149,8 +159,8 @@ __global__ void __launch_bounds__(kPlanThreads) tiles_plan_kernel(const tiles_ar
   for (uint32_t b = threadIdx.x; b < kBins; b += kPlanThreads) bins[b] = 0;
   chained_begin();
 
-  const uint32_t per = (p.n + kPlanThreads - 1) / kPlanThreads;
-  const uint32_t r0 = min(threadIdx.x * per, p.n), r1 = min(r0 + per, p.n);
+  const uint32_t share = (p.n + kPlanThreads - 1) / kPlanThreads;
+  const uint32_t r0 = min(threadIdx.x * share, p.n), r1 = min(r0 + share, p.n);
   auto pairs_of = [&](uint32_t r) -> uint32_t {
     request_t q;
     if (!load_request(p, r, q)) {
@@ -178,6 +188,7 @@ __global__ void __launch_bounds__(kPlanThreads) tiles_plan_kernel(const tiles_ar
   for (uint32_t base = 0; base < n_pairs; base += kPlanThreads) {
     const uint32_t i = base + threadIdx.x;
     uint32_t tiles = 0, r = 0;
+    request_t q;
     if (i < n_pairs) {
       uint32_t lo = 0, hi = p.n;  // the last request with no more pairs before it than i
       while (hi - lo > 1) {
@@ -185,7 +196,6 @@ __global__ void __launch_bounds__(kPlanThreads) tiles_plan_kernel(const tiles_ar
         if (pairs_before[mid] <= i) lo = mid; else hi = mid;
       }
       r = lo;
-      request_t q;
       load_request(p, r, q);
       const pair_range range = range_of(a, q, i - pairs_before[r]);
       tiles = range.end - range.begin;
@@ -193,7 +203,7 @@ __global__ void __launch_bounds__(kPlanThreads) tiles_plan_kernel(const tiles_ar
     uint32_t sum;
     const uint32_t before = block_exclusive(tiles, warp_sums, sum);
     if (i < n_pairs) {
-      a.pairs[i] = make_uint4(r, i - pairs_before[r], total + before, tiles);
+      a.pairs[i] = {r, i - pairs_before[r], total + before, tiles, q.row, q.rows, q.keys, 0};
       atomicMax(&longest, tiles);
     }
     total += sum;
@@ -202,19 +212,26 @@ __global__ void __launch_bounds__(kPlanThreads) tiles_plan_kernel(const tiles_ar
   // claimed one by one if the longest is short beside a CTA's share of the line
   const uint64_t units = static_cast<uint64_t>(total) * p.heads_kv;
   const bool claim = 3ull * longest * a.grid <= units;
-  if (claim) {
+  const uint32_t per = max(kMinRun, static_cast<uint32_t>((units + a.grid - 1) / a.grid));
+  if (!claim) {
+    // every run's first pair: a pair writes down the runs that begin in it
+    for (uint32_t i = threadIdx.x; i < n_pairs; i += kPlanThreads) {
+      const uint32_t from = a.pairs[i].before * p.heads_kv, to = from + a.pairs[i].tiles * p.heads_kv;
+      for (uint32_t c = (from + per - 1) / per; c * per < to && c < a.grid; ++c) a.begin[c] = i;
+    }
+  } else {
     const uint32_t top = max(longest, 1u);
     auto bin_of = [&](uint32_t tiles) {  // longest first
       return kBins - 1 - static_cast<uint32_t>(static_cast<uint64_t>(tiles) * (kBins - 1) / top);
     };
-    for (uint32_t i = threadIdx.x; i < n_pairs; i += kPlanThreads) atomicAdd(&bins[bin_of(a.pairs[i].w)], 1);
+    for (uint32_t i = threadIdx.x; i < n_pairs; i += kPlanThreads) atomicAdd(&bins[bin_of(a.pairs[i].tiles)], 1);
     __syncthreads();
     uint32_t sum;
     const uint32_t before = block_exclusive(bins[threadIdx.x], warp_sums, sum);
     bins[threadIdx.x] = before;
     __syncthreads();
     for (uint32_t i = threadIdx.x; i < n_pairs; i += kPlanThreads)
-      a.order[atomicAdd(&bins[bin_of(a.pairs[i].w)], 1)] = i;
+      a.order[atomicAdd(&bins[bin_of(a.pairs[i].tiles)], 1)] = i;
   }
   if (threadIdx.x == 0) {
     tiles_head h;
@@ -222,7 +239,7 @@ __global__ void __launch_bounds__(kPlanThreads) tiles_plan_kernel(const tiles_ar
     h.n_pairs = n_pairs;
     h.units = static_cast<uint32_t>(units);
     h.claim = claim;
-    h.per = max(kMinRun, static_cast<uint32_t>((units + a.grid - 1) / a.grid));
+    h.per = per;
     *a.head = h;
   }
 }
@@ -345,6 +362,11 @@ __device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.s
 
 // ---- the kernel -----------------------------------------------------------------------------------
 
+// The lowest n bits, of 32.
+__device__ __forceinline__ uint32_t below(int32_t n) {
+  return n <= 0 ? 0u : n >= 32 ? kFull : (1u << n) - 1;
+}
+
 // A counter of ring slots with the parity that a wait for its next use takes.
 template <int N> struct ring {
   uint32_t slot = 0, phase = 0;
@@ -418,20 +440,12 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
       uint32_t issued = 0, q_issued = 0;
       uint32_t unit = min(static_cast<uint64_t>(blockIdx.x) * plan.per, static_cast<uint64_t>(plan.units));
       const uint32_t unit_end = min(unit + plan.per, plan.units);
-      uint32_t pair = 0;
-      if (!plan.claim && unit < unit_end) {  // the pair that the run begins in
-        uint32_t lo = 0, hi = plan.n_pairs;
-        while (hi - lo > 1) {
-          const uint32_t mid = (lo + hi) / 2;
-          if (a.pairs[mid].z * p.heads_kv <= unit) lo = mid; else hi = mid;
-        }
-        pair = lo;
-      }
+      uint32_t pair = !plan.claim && unit < unit_end ? a.begin[blockIdx.x] : 0;
       while (ok) {
         // the next piece
         item_t item;
         item.count = 0;
-        uint4 of;
+        pair_t of;
         if (plan.claim) {
           uint32_t k = 0;
           if (lane == 0) k = atomicAdd(&a.head->next, 1);
@@ -439,32 +453,31 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
           if (k < plan.n_pairs * p.heads_kv) {
             of = a.pairs[a.order[k / p.heads_kv]];
             item.head = k % p.heads_kv;
-            item.count = of.w;
+            item.count = of.tiles;
             item.tile = 0;
             item.whole = 1;
             item.slot = 0;
           }
         } else if (unit < unit_end) {
           of = a.pairs[pair];
-          const uint32_t offset = unit - of.z * p.heads_kv;
-          item.head = offset / of.w;
-          item.tile = offset - item.head * of.w;
-          item.count = min(of.w - item.tile, unit_end - unit);
-          item.whole = item.count == static_cast<int32_t>(of.w);
+          const uint32_t offset = unit - of.before * p.heads_kv;
+          item.head = offset / of.tiles;
+          item.tile = offset - item.head * of.tiles;
+          item.count = min(of.tiles - item.tile, unit_end - unit);
+          item.whole = item.count == static_cast<int32_t>(of.tiles);
           item.slot = 2 * blockIdx.x + (item.tile == 0);
           unit += item.count;
-          if (offset + item.count == of.w * p.heads_kv) ++pair;
+          if (offset + item.count == of.tiles * p.heads_kv) ++pair;
         }
         const bool done = item.count == 0;
         if (!done) {
-          request_t q;
-          load_request(p, of.x, q);
-          const pair_range range = range_of(a, q, of.y);
-          item.request = of.x;
+          const request_t q{of.row, of.rows, of.keys};
+          const pair_range range = range_of(a, q, of.pair);
+          item.request = of.request;
           item.row = q.row;
           item.rows = q.rows;
           item.keys = q.keys;
-          item.token = 2 * of.y * a.tokens_per_tile;
+          item.token = 2 * of.pair * a.tokens_per_tile;
           item.lo = range.lo;
           item.hi = range.hi;
           item.tile += range.begin;
@@ -701,10 +714,14 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
         for (int c = 0; c < kTile; c += 32) tmem_loaded(s + c);
         const int32_t key = t * kTile;
         if (key < all_lo || key + kTile > all_hi) {
-          const int32_t c0 = row_lo - key, c1 = row_hi - key;
+          // a bit per key of 32: constant bit tests come out as predicates, eight at a time
 #pragma unroll
-          for (int c = 0; c < kTile; ++c)
-            if (c < c0 || c >= c1) s[c] = 0xff800000u;
+          for (int c = 0; c < kTile; c += 32) {
+            const uint32_t seen = below(row_hi - key - c) & ~below(row_lo - key - c);
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (!(seen >> i & 1)) s[c + i] = 0xff800000u;
+          }
         }
         float tops[4];
 #pragma unroll
@@ -841,12 +858,10 @@ __global__ void __launch_bounds__(2 * kTile, 2) tiles_join_kernel(const __grid_c
   for (uint32_t unit = blockIdx.x; unit < n; unit += gridDim.x) {
     const uint32_t e = unit % (DP / kJoinColumns) * kJoinColumns, of = unit / (DP / kJoinColumns);
     const uint32_t which = of / p.heads_kv, head = of - which * p.heads_kv;
-    const uint4 info = a.pairs[which];
-    const uint32_t start = info.z * p.heads_kv + head * info.w;
-    const uint32_t first = start / plan.per, last = (start + info.w - 1) / plan.per;
+    const pair_t info = a.pairs[which];
+    const uint32_t start = info.before * p.heads_kv + head * info.tiles;
+    const uint32_t first = start / plan.per, last = (start + info.tiles - 1) / plan.per;
     if (first == last || e >= p.head_dim) continue;
-    request_t q;
-    load_request(p, info.x, q);
     // Pieces in the order of the keys, four at a time so that their loads are on the way together; the
     // first CTA's piece begins the pair and lies in its second slot, the others in their first.
     float m = -INFINITY, l = 0.f, acc[kJoinColumns] = {};
@@ -884,9 +899,9 @@ __global__ void __launch_bounds__(2 * kTile, 2) tiles_join_kernel(const __grid_c
         }
       }
     }
-    const int32_t token = (2 * info.y + x) * a.tokens_per_tile + j;
-    if (j >= static_cast<int32_t>(a.tokens_per_tile) || token >= q.rows) continue;
-    const uint32_t h = head * a.group + g, tok = q.row + token;
+    const int32_t token = (2 * info.pair + x) * a.tokens_per_tile + j;
+    if (j >= static_cast<int32_t>(a.tokens_per_tile) || token >= info.rows) continue;
+    const uint32_t h = head * a.group + g, tok = info.row + token;
     const float inv = l > 0.f ? 1.f / l : 0.f;
     T* to = static_cast<T*>(p.out) + tok * p.out_stride[0] + h * p.out_stride[1] + e;
 #pragma unroll
@@ -935,7 +950,7 @@ namespace attend {
 
 uint64_t tiles_workspace(uint32_t n, uint32_t tokens, uint32_t group, uint32_t head_dim) {
   const uint64_t pairs = pairs_at_most(n, tokens, group);
-  return up16(sizeof(tiles_head)) + 16 * pairs + up16(4 * pairs) +
+  return up16(sizeof(tiles_head)) + up16(4 * kMaxTileCtas) + sizeof(pair_t) * pairs + up16(4 * pairs) +
          2ull * kMaxTileCtas * (head_dim <= 64 ? kPartial<64> : kPartial<128>) * sizeof(float4);
 }
 
@@ -954,8 +969,10 @@ cudaError_t launch_tiles(const preba_pages_attend_t& p, uint32_t page_shift, int
   uint8_t* at = static_cast<uint8_t*>(workspace);
   a.head = reinterpret_cast<tiles_head*>(at);
   at += up16(sizeof(tiles_head));
-  a.pairs = reinterpret_cast<uint4*>(at);
-  at += 16 * pairs;
+  a.begin = reinterpret_cast<uint32_t*>(at);
+  at += up16(4 * kMaxTileCtas);
+  a.pairs = reinterpret_cast<pair_t*>(at);
+  at += sizeof(pair_t) * pairs;
   a.order = reinterpret_cast<uint32_t*>(at);
   at += up16(4 * pairs);
   a.partials = reinterpret_cast<float4*>(at);
