@@ -195,6 +195,7 @@ __device__ __forceinline__ void store_rows(const few_args& a, const request_t& q
   for (int i = 0; i < 2; ++i) {
     const uint32_t row = (lane >> 2) + 8 * i;
     if (row >= q.rows * a.group) continue;
+    if (!PREBA_IN_RANGE(p.status, static_cast<uint32_t>(q.row) + row / a.group < p.tokens)) continue;
     const uint32_t j = row / a.group, h = head * a.group + row - j * a.group, t = q.row + j;
     const float inv = l[i] > 0.f ? 1.f / l[i] : 0.f;
     T* to = static_cast<T*>(p.out) + t * p.out_stride[0] + h * p.out_stride[1];
@@ -213,6 +214,7 @@ __device__ __forceinline__ void store_rows(const few_args& a, const request_t& q
 // Partial sums of a CTA's first (slot 0) or last piece: pairs of columns in the fragment layout, rows 0 to
 // 7, then rows 8 to 15, then a maximum and a sum for each row.
 template <int DP> __device__ __forceinline__ float2* partial_of(const preba_pages_attend_t& p, uint32_t cta, uint32_t slot) {
+  if (!PREBA_IN_RANGE(p.status, 2 * cta + slot < 2 * kMaxSplitCtas)) cta = slot = 0;
   return reinterpret_cast<float2*>(static_cast<uint8_t*>(p.workspace) + kCounterBytes +
                                    static_cast<uint64_t>(2 * cta + slot) * few_layout<DP>::kPartial);
 }

@@ -459,6 +459,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
             item.slot = 0;
           }
         } else if (unit < unit_end) {
+          if (!PREBA_IN_RANGE(p.status, pair < plan.n_pairs)) pair = 0;
           of = a.pairs[pair];
           const uint32_t offset = unit - of.before * p.heads_kv;
           item.head = offset / of.tiles;
@@ -791,6 +792,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
       }
       if (item.whole) {
         const uint32_t h = item.head * a.group + g, tok = item.row + token + j;
+        const bool write = live && PREBA_IN_RANGE(p.status, tok < p.tokens && h < p.heads_q);
         const float inv = l > 0.f ? 1.f / l : 0.f;
         T* to = static_cast<T*>(p.out) + tok * p.out_stride[0] + h * p.out_stride[1];
 #pragma unroll 1
@@ -798,7 +800,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
           uint32_t o[32];
           tmem_load32(o, o_at + c);
           tmem_loaded(o);
-          if (live) {
+          if (write) {
 #pragma unroll
             for (int i = 0; i < 32; i += 8)
               if (c + i < static_cast<int32_t>(p.head_dim)) {
@@ -811,7 +813,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
               }
           }
         }
-        if (p.lse && live)
+        if (p.lse && write)
           p.lse[static_cast<uint64_t>(tok) * p.heads_q + h] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
       } else {
         // partial sums, four columns of 256 rows after the other, then maxima and sums
