@@ -85,12 +85,21 @@ struct pair_t {
 };
 static_assert(sizeof(pair_t) == 32, "two vector loads");
 
+// Where a CTA's run of the line begins, and what that beginning cuts in two.
+struct run_t {
+  pair_t pair;            // the pair of the run's first key tile
+  uint32_t which, head;   // its number, and the key head
+  uint32_t first, last;   // the CTAs with pieces of it, if this is the first run that begins inside it;
+                          // else the same twice
+};
+static_assert(sizeof(run_t) == 48, "three vector loads");
+
 struct tiles_args {
   preba_pages_attend_t p;
   uint32_t page_shift, group, tokens_per_tile, box_rows, box_shift, grid, max_pairs;
   tiles_head* head;
   pair_t* pairs;
-  uint32_t* begin;    // of every CTA's run in the line: the pair
+  run_t* runs;        // one per CTA
   uint32_t* order;    // pairs, longest first
   float4* partials;   // two per CTA
 };
@@ -152,7 +161,9 @@ __device__ __forceinline__ uint32_t block_exclusive(uint32_t v, uint32_t* warp_s
 }
 
 __global__ void __launch_bounds__(kPlanThreads) tiles_plan_kernel(const tiles_args a) {
-  extern __shared__ uint32_t pairs_before[];  // n + 1: pairs of the requests before
+  extern __shared__ __align__(16) uint8_t plan_smem[];
+  pair_t* near = reinterpret_cast<pair_t*>(plan_smem);  // the first kPlanThreads pairs
+  uint32_t* pairs_before = reinterpret_cast<uint32_t*>(near + kPlanThreads);  // n + 1: pairs of the requests before
   __shared__ uint32_t warp_sums[32], bins[kBins], longest;
   const preba_pages_attend_t& p = a.p;
   if (threadIdx.x == 0) longest = 0;
@@ -203,7 +214,9 @@ __global__ void __launch_bounds__(kPlanThreads) tiles_plan_kernel(const tiles_ar
     uint32_t sum;
     const uint32_t before = block_exclusive(tiles, warp_sums, sum);
     if (i < n_pairs) {
-      a.pairs[i] = {r, i - pairs_before[r], total + before, tiles, q.row, q.rows, q.keys, 0};
+      const pair_t pair{r, i - pairs_before[r], total + before, tiles, q.row, q.rows, q.keys, 0};
+      a.pairs[i] = pair;
+      if (i < kPlanThreads) near[i] = pair;
       atomicMax(&longest, tiles);
     }
     total += sum;
@@ -213,25 +226,34 @@ __global__ void __launch_bounds__(kPlanThreads) tiles_plan_kernel(const tiles_ar
   const uint64_t units = static_cast<uint64_t>(total) * p.heads_kv;
   const bool claim = 3ull * longest * a.grid <= units;
   const uint32_t per = max(kMinRun, static_cast<uint32_t>((units + a.grid - 1) / a.grid));
+  for (uint32_t c = threadIdx.x; c < a.grid; c += kPlanThreads) a.runs[c].first = a.runs[c].last = 0;
+  __syncthreads();
   if (!claim) {
-    // every run's first pair: a pair writes down the runs that begin in it
-    for (uint32_t i = threadIdx.x; i < n_pairs; i += kPlanThreads) {
-      const uint32_t from = a.pairs[i].before * p.heads_kv, to = from + a.pairs[i].tiles * p.heads_kv;
-      for (uint32_t c = (from + per - 1) / per; c * per < to && c < a.grid; ++c) a.begin[c] = i;
+    // a pair writes down the runs that begin in it, with as many threads as there are for each
+    uint32_t lanes = 32;
+    while (lanes > 1 && n_pairs * lanes > kPlanThreads) lanes /= 2;
+    for (uint32_t i = threadIdx.x / lanes; i < n_pairs; i += kPlanThreads / lanes) {
+      const pair_t pair = i < kPlanThreads ? near[i] : a.pairs[i];
+      const uint32_t from = pair.before * p.heads_kv, to = from + pair.tiles * p.heads_kv;
+      for (uint32_t c = (from + per - 1) / per + threadIdx.x % lanes; c < a.grid && c * per < to; c += lanes) {
+        const uint32_t head = (c * per - from) / pair.tiles, start = from + head * pair.tiles;
+        const bool cuts = c * per > start && (c - 1) * per <= start;
+        a.runs[c] = {pair, i, head, cuts ? c - 1 : 0, cuts ? (start + pair.tiles - 1) / per : 0};
+      }
     }
   } else {
     const uint32_t top = max(longest, 1u);
     auto bin_of = [&](uint32_t tiles) {  // longest first
       return kBins - 1 - static_cast<uint32_t>(static_cast<uint64_t>(tiles) * (kBins - 1) / top);
     };
-    for (uint32_t i = threadIdx.x; i < n_pairs; i += kPlanThreads) atomicAdd(&bins[bin_of(a.pairs[i].tiles)], 1);
+    for (uint32_t i = threadIdx.x; i < n_pairs; i += kPlanThreads) atomicAdd(&bins[bin_of(i < kPlanThreads ? near[i].tiles : a.pairs[i].tiles)], 1);
     __syncthreads();
     uint32_t sum;
     const uint32_t before = block_exclusive(bins[threadIdx.x], warp_sums, sum);
     bins[threadIdx.x] = before;
     __syncthreads();
     for (uint32_t i = threadIdx.x; i < n_pairs; i += kPlanThreads)
-      a.order[atomicAdd(&bins[bin_of(a.pairs[i].tiles)], 1)] = i;
+      a.order[atomicAdd(&bins[bin_of(i < kPlanThreads ? near[i].tiles : a.pairs[i].tiles)], 1)] = i;
   }
   if (threadIdx.x == 0) {
     tiles_head h;
@@ -410,6 +432,9 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
       mbar_init(item_empty + 8 * x, kSoftWarps + 1);
     }
     mbar_init(drained, 1);
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_q) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == kMmaWarp) {
@@ -430,6 +455,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
     if (warp == kCopyWarp) {
       // ---- work and copies
       const tiles_head plan = *a.head;
+    const run_t run = a.runs[blockIdx.x];  // means something only if the run has a key tile
       const uint32_t boxes = kTile >> a.box_shift;
       const uint32_t chunk = lane & (boxes - 1), half = lane / boxes;
       const bool mine = half < L::kHalves;
@@ -440,12 +466,19 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
       uint32_t issued = 0, q_issued = 0;
       uint32_t unit = min(static_cast<uint64_t>(blockIdx.x) * plan.per, static_cast<uint64_t>(plan.units));
       const uint32_t unit_end = min(unit + plan.per, plan.units);
-      uint32_t pair = !plan.claim && unit < unit_end ? a.begin[blockIdx.x] : 0;
+      uint32_t pair = run.which;
+      pair_t of = run.pair;  // of the run's first piece
+      bool next_pair = false;
       while (ok) {
         // the next piece
         item_t item;
         item.count = 0;
-        pair_t of;
+        if (next_pair && unit < unit_end) {
+          ++pair;
+          if (!PREBA_IN_RANGE(p.status, pair < plan.n_pairs)) pair = 0;
+          of = a.pairs[pair];
+          next_pair = false;
+        }
         if (plan.claim) {
           uint32_t k = 0;
           if (lane == 0) k = atomicAdd(&a.head->next, 1);
@@ -459,8 +492,6 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
             item.slot = 0;
           }
         } else if (unit < unit_end) {
-          if (!PREBA_IN_RANGE(p.status, pair < plan.n_pairs)) pair = 0;
-          of = a.pairs[pair];
           const uint32_t offset = unit - of.before * p.heads_kv;
           item.head = offset / of.tiles;
           item.tile = offset - item.head * of.tiles;
@@ -468,7 +499,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
           item.whole = item.count == static_cast<int32_t>(of.tiles);
           item.slot = 2 * blockIdx.x + (item.tile == 0);
           unit += item.count;
-          if (offset + item.count == of.tiles * p.heads_kv) ++pair;
+          next_pair = offset + item.count == of.tiles * p.heads_kv;
         }
         const bool done = item.count == 0;
         if (!done) {
@@ -851,74 +882,68 @@ constexpr int kJoinColumns = 16;
 template <typename T, int DP>
 __global__ void __launch_bounds__(2 * kTile, 2) tiles_join_kernel(const __grid_constant__ tiles_args a) {
   chained_begin();
-  const tiles_head plan = *a.head;
-  if (plan.claim) return;
   const preba_pages_attend_t& p = a.p;
+  constexpr uint32_t kParts = DP / kJoinColumns;
+  const uint32_t e = blockIdx.x % kParts * kJoinColumns;
+  const run_t run = a.runs[blockIdx.x / kParts];
+  const uint32_t first = run.first, last = run.last, head = run.head;
+  if (first == last || e >= p.head_dim) return;
   const int x = threadIdx.x / kTile, r = threadIdx.x % kTile;
   const int32_t j = r / static_cast<int32_t>(a.group), g = r - j * static_cast<int32_t>(a.group);
-  const uint32_t n = plan.n_pairs * p.heads_kv * (DP / kJoinColumns);
-  for (uint32_t unit = blockIdx.x; unit < n; unit += gridDim.x) {
-    const uint32_t e = unit % (DP / kJoinColumns) * kJoinColumns, of = unit / (DP / kJoinColumns);
-    const uint32_t which = of / p.heads_kv, head = of - which * p.heads_kv;
-    const pair_t info = a.pairs[which];
-    const uint32_t start = info.before * p.heads_kv + head * info.tiles;
-    const uint32_t first = start / plan.per, last = (start + info.tiles - 1) / plan.per;
-    if (first == last || e >= p.head_dim) continue;
-    // Pieces in the order of the keys, four at a time so that their loads are on the way together; the
-    // first CTA's piece begins the pair and lies in its second slot, the others in their first.
-    float m = -INFINITY, l = 0.f, acc[kJoinColumns] = {};
+  // Pieces in the order of the keys, four at a time so that their loads are on the way together; the
+  // first CTA's piece begins the pair and lies in its second slot, the others in their first.
+  float m = -INFINITY, l = 0.f, acc[kJoinColumns] = {};
 #pragma unroll 1
-    for (uint32_t c = first; c <= last; c += 4) {
-      float2 v[4];
-      float4 part[4][kJoinColumns / 4];
+  for (uint32_t c = first; c <= last; c += 4) {
+    float2 v[4];
+    float4 part[4][kJoinColumns / 4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const uint32_t cta = min(c + k, last);  // the last one again: it is not counted
-        const float4* from = a.partials + static_cast<uint64_t>(2 * cta + (cta == first)) * kPartial<DP>;
-        v[k] = __ldcg(reinterpret_cast<const float2*>(from + DP / 4 * 2 * kTile) + threadIdx.x);
+    for (int k = 0; k < 4; ++k) {
+      const uint32_t cta = min(c + k, last);  // the last one again: it is not counted
+      const float4* from = a.partials + static_cast<uint64_t>(2 * cta + (cta == first)) * kPartial<DP>;
+      v[k] = __ldcg(reinterpret_cast<const float2*>(from + DP / 4 * 2 * kTile) + threadIdx.x);
 #pragma unroll
-        for (int i = 0; i < kJoinColumns / 4; ++i)
-          part[k][i] = __ldcg(from + (e / 4 + i) * 2 * kTile + threadIdx.x);
-      }
-      const float to = fmaxf(m, fmaxf(fmaxf(v[0].x, v[1].x), fmaxf(v[2].x, v[3].x)));
-      const float keep = to == -INFINITY ? 0.f : exp2_approx(m - to);
-      m = to;
-      l *= keep;
+      for (int i = 0; i < kJoinColumns / 4; ++i)
+        part[k][i] = __ldcg(from + (e / 4 + i) * 2 * kTile + threadIdx.x);
+    }
+    const float to = fmaxf(m, fmaxf(fmaxf(v[0].x, v[1].x), fmaxf(v[2].x, v[3].x)));
+    const float keep = to == -INFINITY ? 0.f : exp2_approx(m - to);
+    m = to;
+    l *= keep;
 #pragma unroll
-      for (int i = 0; i < kJoinColumns; ++i) acc[i] *= keep;
+    for (int i = 0; i < kJoinColumns; ++i) acc[i] *= keep;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        // a piece that saw nothing left no sums: what lies in their place may be anything
-        if (c + k > last || v[k].x == -INFINITY) continue;
-        const float w = exp2_approx(v[k].x - m);
-        l = fmaf(w, v[k].y, l);
+    for (int k = 0; k < 4; ++k) {
+      // a piece that saw nothing left no sums: what lies in their place may be anything
+      if (c + k > last || v[k].x == -INFINITY) continue;
+      const float w = exp2_approx(v[k].x - m);
+      l = fmaf(w, v[k].y, l);
 #pragma unroll
-        for (int i = 0; i < kJoinColumns / 4; ++i) {
-          acc[4 * i] = fmaf(w, part[k][i].x, acc[4 * i]);
-          acc[4 * i + 1] = fmaf(w, part[k][i].y, acc[4 * i + 1]);
-          acc[4 * i + 2] = fmaf(w, part[k][i].z, acc[4 * i + 2]);
-          acc[4 * i + 3] = fmaf(w, part[k][i].w, acc[4 * i + 3]);
-        }
+      for (int i = 0; i < kJoinColumns / 4; ++i) {
+        acc[4 * i] = fmaf(w, part[k][i].x, acc[4 * i]);
+        acc[4 * i + 1] = fmaf(w, part[k][i].y, acc[4 * i + 1]);
+        acc[4 * i + 2] = fmaf(w, part[k][i].z, acc[4 * i + 2]);
+        acc[4 * i + 3] = fmaf(w, part[k][i].w, acc[4 * i + 3]);
       }
     }
-    const int32_t token = (2 * info.pair + x) * a.tokens_per_tile + j;
-    if (j >= static_cast<int32_t>(a.tokens_per_tile) || token >= info.rows) continue;
-    const uint32_t h = head * a.group + g, tok = info.row + token;
-    const float inv = l > 0.f ? 1.f / l : 0.f;
-    T* to = static_cast<T*>(p.out) + tok * p.out_stride[0] + h * p.out_stride[1] + e;
-#pragma unroll
-    for (int i = 0; i < kJoinColumns; i += 8)
-      if (e + i < p.head_dim) {
-        uint4 v;
-        v.x = pack2<T>(acc[i] * inv, acc[i + 1] * inv);
-        v.y = pack2<T>(acc[i + 2] * inv, acc[i + 3] * inv);
-        v.z = pack2<T>(acc[i + 4] * inv, acc[i + 5] * inv);
-        v.w = pack2<T>(acc[i + 6] * inv, acc[i + 7] * inv);
-        *reinterpret_cast<uint4*>(to + i) = v;
-      }
-    if (p.lse && e == 0)
-      p.lse[static_cast<uint64_t>(tok) * p.heads_q + h] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
   }
+  const int32_t token = (2 * run.pair.pair + x) * a.tokens_per_tile + j;
+  if (j >= static_cast<int32_t>(a.tokens_per_tile) || token >= run.pair.rows) return;
+  const uint32_t h = head * a.group + g, tok = run.pair.row + token;
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  T* to = static_cast<T*>(p.out) + tok * p.out_stride[0] + h * p.out_stride[1] + e;
+#pragma unroll
+  for (int i = 0; i < kJoinColumns; i += 8)
+    if (e + i < p.head_dim) {
+      uint4 v;
+      v.x = pack2<T>(acc[i] * inv, acc[i + 1] * inv);
+      v.y = pack2<T>(acc[i + 2] * inv, acc[i + 3] * inv);
+      v.z = pack2<T>(acc[i + 4] * inv, acc[i + 5] * inv);
+      v.w = pack2<T>(acc[i + 6] * inv, acc[i + 7] * inv);
+      *reinterpret_cast<uint4*>(to + i) = v;
+    }
+  if (p.lse && e == 0)
+    p.lse[static_cast<uint64_t>(tok) * p.heads_q + h] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
 }
 
 template <typename T, int DP>
@@ -937,7 +962,8 @@ cudaError_t launch(const tiles_args& a, cudaStream_t stream) {
   if (err != cudaSuccess) return err;
   err = launch_chained(tiles_kernel<T, DP>, a.grid, kThreads, L::kBytes, stream, map_q, map_k, map_v, a);
   if (err != cudaSuccess) return err;
-  return launch_chained(tiles_join_kernel<T, DP>, 4 * a.grid, 2 * kTile, 0, stream, a);
+  return launch_chained(tiles_join_kernel<T, DP>, a.grid * (DP / kJoinColumns), 2 * kTile, 0,
+                        stream, a);
 }
 
 uint64_t up16(uint64_t v) { return (v + 15) / 16 * 16; }
@@ -952,7 +978,7 @@ namespace attend {
 
 uint64_t tiles_workspace(uint32_t n, uint32_t tokens, uint32_t group, uint32_t head_dim) {
   const uint64_t pairs = pairs_at_most(n, tokens, group);
-  return up16(sizeof(tiles_head)) + up16(4 * kMaxTileCtas) + sizeof(pair_t) * pairs + up16(4 * pairs) +
+  return up16(sizeof(tiles_head)) + sizeof(run_t) * kMaxTileCtas + sizeof(pair_t) * pairs + up16(4 * pairs) +
          2ull * kMaxTileCtas * (head_dim <= 64 ? kPartial<64> : kPartial<128>) * sizeof(float4);
 }
 
@@ -971,17 +997,17 @@ cudaError_t launch_tiles(const preba_pages_attend_t& p, uint32_t page_shift, int
   uint8_t* at = static_cast<uint8_t*>(workspace);
   a.head = reinterpret_cast<tiles_head*>(at);
   at += up16(sizeof(tiles_head));
-  a.begin = reinterpret_cast<uint32_t*>(at);
-  at += up16(4 * kMaxTileCtas);
+  a.runs = reinterpret_cast<run_t*>(at);
+  at += sizeof(run_t) * kMaxTileCtas;
   a.pairs = reinterpret_cast<pair_t*>(at);
   at += sizeof(pair_t) * pairs;
   a.order = reinterpret_cast<uint32_t*>(at);
   at += up16(4 * pairs);
   a.partials = reinterpret_cast<float4*>(at);
-  const size_t smem = 4 * (static_cast<size_t>(p.n) + 1);
-  if (smem > 32 * 1024) {
+  const size_t smem = kPlanThreads * sizeof(pair_t) + 4 * (static_cast<size_t>(p.n) + 1);
+  if (smem > 40 * 1024) {  // beside 5 KB of its own; 48 KB need no leave
     const cudaError_t err = cudaFuncSetAttribute(tiles_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                 4 * (PREBA_PAGES_MAX_REQUESTS + 1));
+                                                 kPlanThreads * sizeof(pair_t) + 4 * (PREBA_PAGES_MAX_REQUESTS + 1));
     if (err != cudaSuccess) return err;
   }
   const cudaError_t err = launch_chained(tiles_plan_kernel, 1, kPlanThreads, smem, stream, a);
