@@ -384,6 +384,27 @@ __device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.s
 
 // ---- the kernel -----------------------------------------------------------------------------------
 
+// Four neighbouring threads hold four blocks of four words each, one row per thread; afterwards thread q of
+// them holds block q of all four rows, in the order of the rows.
+__device__ __forceinline__ void turn_four(uint32_t (&w)[16]) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int bit = 2; bit; bit >>= 1) {
+    const bool up = lane & bit;
+#pragma unroll
+    for (int block = 0; block < 4; ++block) {
+      if (block & bit) continue;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t &lo = w[4 * block + i], &hi = w[4 * (block | bit) + i];
+        const uint32_t got = __shfl_xor_sync(kFull, up ? lo : hi, bit);
+        lo = up ? got : lo;
+        hi = up ? hi : got;
+      }
+    }
+  }
+}
+
 // The lowest n bits, of 32.
 __device__ __forceinline__ uint32_t below(int32_t n) {
   return n <= 0 ? 0u : n >= 32 ? kFull : (1u << n) - 1;
@@ -825,23 +846,28 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
         const uint32_t h = item.head * a.group + g, tok = item.row + token + j;
         const bool write = live && PREBA_IN_RANGE(p.status, tok < p.tokens && h < p.heads_q);
         const float inv = l > 0.f ? 1.f / l : 0.f;
-        T* to = static_cast<T*>(p.out) + tok * p.out_stride[0] + h * p.out_stride[1];
+        // Four threads turn 64 bytes of their four rows around, so that a store writes 64 bytes of eight
+        // rows and not 16 bytes of 32: the stores of a tile were bound by the lines they touch (3850 clocks).
+        T* rows[4];
+        uint32_t writes = __ballot_sync(kFull, write) >> (lane & ~3);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          rows[k] = reinterpret_cast<T*>(__shfl_sync(
+              kFull, reinterpret_cast<uint64_t>(static_cast<T*>(p.out) + tok * p.out_stride[0] + h * p.out_stride[1]),
+              (lane & ~3) + k)) + 8 * (lane & 3);
 #pragma unroll 1
         for (int c = 0; c < DP; c += 32) {
-          uint32_t o[32];
+          uint32_t o[32], w[16];
           tmem_load32(o, o_at + c);
           tmem_loaded(o);
-          if (write) {
 #pragma unroll
-            for (int i = 0; i < 32; i += 8)
-              if (c + i < static_cast<int32_t>(p.head_dim)) {
-                uint4 v;
-                v.x = pack2<T>(__uint_as_float(o[i]) * inv, __uint_as_float(o[i + 1]) * inv);
-                v.y = pack2<T>(__uint_as_float(o[i + 2]) * inv, __uint_as_float(o[i + 3]) * inv);
-                v.z = pack2<T>(__uint_as_float(o[i + 4]) * inv, __uint_as_float(o[i + 5]) * inv);
-                v.w = pack2<T>(__uint_as_float(o[i + 6]) * inv, __uint_as_float(o[i + 7]) * inv);
-                *reinterpret_cast<uint4*>(to + c + i) = v;
-              }
+          for (int i = 0; i < 32; i += 2) w[i / 2] = pack2<T>(__uint_as_float(o[i]) * inv, __uint_as_float(o[i + 1]) * inv);
+          turn_four(w);
+          if (c + 8 * (lane & 3) < static_cast<int32_t>(p.head_dim)) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              if (writes >> k & 1)
+                *reinterpret_cast<uint4*>(rows[k] + c) = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
           }
         }
         if (p.lse && write)
