@@ -19,7 +19,10 @@ using namespace attend;
 // the CTAs take equal runs of it, whatever the lengths are, and a (request, key head) that crosses
 // CTAs is left as partial sums that the last of them to finish joins, in the order of the keys, so that
 // timing does not change a bit.  Within a tile each of the four warps takes 16 keys with a running maximum
-// and sum of its own; the warps are joined once per (request, key head).
+// and sum of its own; the warps are joined once per (request, key head).  128 single tokens over up to 8192
+// keys of 8 heads of 128: 272 to 278 us (1762 MB, 6.4 TB/s; a copy reaches 6.56); 4 of them over up to 2048
+// keys: 13 us, which the launch, the first loads (2.7 us), the partial sums' fence and count (1.5 us) and
+// their join (2 to 3 us) take the most of.
 
 constexpr uint64_t kCounterBytes = kMaxSplitCtas * 4;  // at the workspace's start
 constexpr int kRowsMax = 16;
