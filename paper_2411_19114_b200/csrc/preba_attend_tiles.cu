@@ -16,12 +16,13 @@
 // longest is short beside a CTA's share, CTAs claim them one by one, longest first.  Otherwise the
 // key tiles of all of them form one line, every CTA takes an equal run of it, and pieces that are not
 // whole leave partial sums which a last kernel joins in the order of the keys.  Which, and the list, is
-// decided on the device by a planning kernel, as the lengths are there.
+// decided on the device, as the lengths are there: by a planning kernel, or, where there are too few pairs
+// to be claimed, by every CTA for its own run.
 //
 // Bound by the softmax, closely followed by the products: a pair of row tiles and 128 keys takes 2048 clocks of
 // the tensor pipe and 2048 of MUFU, and about 3050 altogether.  4 prompts of up to 4096 tokens, 32 query
 // heads of 128: 324 us at 1.9 GHz, 371 us at the 1.6 GHz that the GPU holds (1.20 and 1.05 PFLOP/s); 512 tokens
-// over 30000 keys: 216 and 250 us; a step of 9 chunks and 28 single tokens with a window of 1000: 43 us.
+// over 30000 keys: 211 and 241 us; a step of 9 chunks and 28 single tokens with a window of 1000: 40 us.
 #include <algorithm>
 
 #include <type_traits>
@@ -53,7 +54,8 @@ template <int DP> struct layout {      // DP: head_dim rounded up to 64 or 128
   static constexpr uint32_t kRing = 2 * kQ;
   static constexpr uint32_t kBars = kRing + kSlots * kSlot;
   static constexpr uint32_t kItems = kBars + 512;
-  static constexpr uint32_t kBytes = kItems + 256;
+  static constexpr uint32_t kPlan = kItems + 256;      // own_plan_t
+  static constexpr uint32_t kBytes = kPlan + 2048;
   // tensor memory columns: S of A and B (P lies over them), O of A and B
   static constexpr uint32_t kS = 0, kO = 256;
 };
@@ -102,6 +104,7 @@ static_assert(sizeof(run_t) == 48, "three vector loads");
 struct tiles_args {
   preba_pages_attend_t p;
   uint32_t page_shift, group, tokens_per_tile, box_rows, box_shift, grid, max_pairs;
+  uint32_t own_plan;  // every CTA makes the plan for itself: it is small and sure to be a line
   tiles_head* head;
   pair_t* pairs;
   run_t* runs;        // one per CTA
@@ -273,6 +276,106 @@ __global__ void __launch_bounds__(kPlanThreads) tiles_plan_kernel(const tiles_ar
   }
 }
 static_assert(kBins == kPlanThreads, "one bin per thread in the sum");
+
+// The same by a CTA of the kernel itself, for itself: where there are few pairs, all of them are certain to
+// form one line, and a CTA needs its own run of it only.  One launch and 1.6 to 5 us less per call (4 chunks of 32
+// tokens over 500 keys 16.5 -> 14.9 us, 512 tokens over 30000 keys 247 -> 241 us).
+constexpr uint32_t kOwnPairs = 3 * kMaxTileCtas;  // fewer than this, and they cannot be claimed one by one
+
+struct own_plan_t {
+  run_t run;
+  uint32_t units, per;
+  uint32_t sums[12];                 // of the warps
+  uint32_t pairs_before[kOwnPairs];  // n + 1
+};
+static_assert(sizeof(own_plan_t) <= 2048, "layout::kBytes");
+
+template <int kThreads>
+__device__ __forceinline__ uint32_t cta_exclusive(uint32_t v, uint32_t* sums, uint32_t& total) {
+  static_assert(kThreads == 12 * 32, "own_plan_t::sums");
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint32_t incl = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t up = __shfl_up_sync(kFull, incl, o);
+    if (lane >= o) incl += up;
+  }
+  __syncthreads();  // what an earlier call left has been read
+  if (lane == 31) sums[warp] = incl;
+  __syncthreads();
+  const uint32_t of_warp = lane < kThreads / 32 ? sums[lane] : 0;
+  total = __reduce_add_sync(kFull, of_warp);
+  return __reduce_add_sync(kFull, lane < warp ? of_warp : 0) + incl - v;
+}
+
+__device__ __forceinline__ void plan_own(const tiles_args& a, own_plan_t& plan) {
+  const preba_pages_attend_t& p = a.p;
+  auto pairs_of = [&](uint32_t r) -> uint32_t {
+    request_t q;
+    if (!load_request(p, r, q)) {
+      if (blockIdx.x == 0) report(p.status, PREBA_ERR_BAD_TABLE);
+      return 0;
+    }
+    return (q.rows + 2 * a.tokens_per_tile - 1) / (2 * a.tokens_per_tile);
+  };
+  const uint32_t share = (p.n + kThreads - 1) / kThreads;
+  const uint32_t r0 = min(threadIdx.x * share, p.n), r1 = min(r0 + share, p.n);
+  uint32_t mine = 0, n_pairs;
+  for (uint32_t r = r0; r < r1; ++r) mine += pairs_of(r);
+  uint32_t at = cta_exclusive<kThreads>(mine, plan.sums, n_pairs);
+  for (uint32_t r = r0; r < r1; ++r) {
+    plan.pairs_before[r] = at;
+    at += pairs_of(r);
+  }
+  if (threadIdx.x == 0) plan.pairs_before[p.n] = n_pairs;
+  __syncthreads();
+  if (n_pairs > a.max_pairs) {  // rows of different requests overlap: the list ends early
+    if (threadIdx.x == 0 && blockIdx.x == 0) report(p.status, PREBA_ERR_BAD_TABLE);
+    n_pairs = a.max_pairs;
+  }
+  constexpr int kEach = (kOwnPairs + kThreads - 1) / kThreads;
+  pair_t pair[kEach];
+  uint32_t tiles = 0;
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    const uint32_t i = kEach * threadIdx.x + k;
+    pair[k].tiles = 0;
+    if (i >= n_pairs) continue;
+    uint32_t lo = 0, hi = p.n;  // the last request with no more pairs before it than i
+    while (hi - lo > 1) {
+      const uint32_t mid = (lo + hi) / 2;
+      if (plan.pairs_before[mid] <= i) lo = mid; else hi = mid;
+    }
+    request_t q;
+    load_request(p, lo, q);
+    const pair_range range = range_of(a, q, i - plan.pairs_before[lo]);
+    pair[k] = {lo, i - plan.pairs_before[lo], 0, static_cast<uint32_t>(range.end - range.begin), q.row, q.rows, q.keys, 0};
+    tiles += pair[k].tiles;
+  }
+  uint32_t total;
+  uint32_t before = cta_exclusive<kThreads>(tiles, plan.sums, total);
+  const uint32_t units = total * p.heads_kv;
+  const uint32_t per = max(kMinRun, (units + a.grid - 1) / a.grid), unit = blockIdx.x * per;
+  if (threadIdx.x == 0) {
+    plan.units = units;
+    plan.per = per;
+    if (unit >= units) a.runs[blockIdx.x].first = a.runs[blockIdx.x].last = 0;
+  }
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    const uint32_t from = before * p.heads_kv, to = from + pair[k].tiles * p.heads_kv;
+    if (unit >= from && unit < to) {  // one thread's pair
+      pair[k].before = before;
+      const uint32_t head = (unit - from) / pair[k].tiles, start = from + head * pair[k].tiles;
+      const bool cuts = unit > start && unit - per <= start;
+      plan.run = {pair[k], kEach * threadIdx.x + k, head, cuts ? blockIdx.x - 1 : 0,
+                  cuts ? (start + pair[k].tiles - 1) / per : 0};
+      a.runs[blockIdx.x] = plan.run;  // for the joining kernel
+    }
+    before += pair[k].tiles;
+  }
+  __syncthreads();
+}
 
 // ---- tensor core instructions (PTX) ---------------------------------------------------------------
 
@@ -476,14 +579,23 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
   fence_after();
   const uint32_t tmem = *tmem_slot;
   chained_begin();
+  own_plan_t& own = *reinterpret_cast<own_plan_t*>(smem + L::kPlan);
+  if (a.own_plan) plan_own(a, own);
   bool ok = true;
 
   if (warp >= kSoftWarps) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegisters));
     if (warp == kCopyWarp) {
       // ---- work and copies
-      const tiles_head plan = *a.head;
-    const run_t run = a.runs[blockIdx.x];  // means something only if the run has a key tile
+      tiles_head plan;
+    run_t run;  // means something only if the run has a key tile
+    if (a.own_plan) {
+      plan = {0, 0, own.units, 0, own.per};
+      run = own.run;
+    } else {
+      plan = *a.head;
+      run = a.runs[blockIdx.x];
+    }
       const uint32_t boxes = kTile >> a.box_shift;
       const uint32_t chunk = lane & (boxes - 1), half = lane / boxes;
       const bool mine = half < L::kHalves;
@@ -503,9 +615,22 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
         item.count = 0;
         if (next_pair && unit < unit_end) {
           ++pair;
-          if (!PREBA_IN_RANGE(p.status, pair < plan.n_pairs)) pair = 0;
-          of = a.pairs[pair];
           next_pair = false;
+          if (a.own_plan) {
+            of.before += of.tiles;
+            while (own.pairs_before[of.request + 1] <= pair) ++of.request;  // ends: the run has a key tile left
+            of.pair = pair - own.pairs_before[of.request];
+            request_t q;
+            load_request(p, of.request, q);
+            of.row = q.row;
+            of.rows = q.rows;
+            of.keys = q.keys;
+            const pair_range range = range_of(a, q, of.pair);
+            of.tiles = range.end - range.begin;
+          } else {
+            if (!PREBA_IN_RANGE(p.status, pair < plan.n_pairs)) pair = 0;
+            of = a.pairs[pair];
+          }
         }
         if (plan.claim) {
           uint32_t k = 0;
@@ -1037,14 +1162,18 @@ cudaError_t launch_tiles(const preba_pages_attend_t& p, uint32_t page_shift, int
   a.order = reinterpret_cast<uint32_t*>(at);
   at += up16(4 * pairs);
   a.partials = reinterpret_cast<float4*>(at);
+  // claims need three pairs (on one key head) a CTA at least
+  a.own_plan = pairs < kOwnPairs && pairs * p.heads_kv < 3ull * a.grid;
   const size_t smem = kPlanThreads * sizeof(pair_t) + 4 * (static_cast<size_t>(p.n) + 1);
   if (smem > 40 * 1024) {  // beside 5 KB of its own; 48 KB need no leave
     const cudaError_t err = cudaFuncSetAttribute(tiles_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                  kPlanThreads * sizeof(pair_t) + 4 * (PREBA_PAGES_MAX_REQUESTS + 1));
     if (err != cudaSuccess) return err;
   }
-  const cudaError_t err = launch_chained(tiles_plan_kernel, 1, kPlanThreads, smem, stream, a);
-  if (err != cudaSuccess) return err;
+  if (!a.own_plan) {
+    const cudaError_t err = launch_chained(tiles_plan_kernel, 1, kPlanThreads, smem, stream, a);
+    if (err != cudaSuccess) return err;
+  }
   if (p.dtype == PREBA_F16)
     return p.head_dim <= 64 ? launch<__half, 64>(a, stream) : launch<__half, 128>(a, stream);
   return p.head_dim <= 64 ? launch<__nv_bfloat16, 64>(a, stream) : launch<__nv_bfloat16, 128>(a, stream);
