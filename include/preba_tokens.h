@@ -17,6 +17,11 @@
  * captured in a CUDA graph: what they read of lengths and tables is read on the device.  Strides
  * are in elements.  Lengths and tables are checked on the device where they are used; an entry that
  * is out of range is never followed, the first such PREBA_ERR_* is stored in `status`.
+ *
+ * The kernels of these calls let the next kernel on the stream be set up while they run.  That changes
+ * nothing for an ordinary launch, but a launch that asks not to wait (PREBA_OVERLAP_PREVIOUS,
+ * PREBA_AUDIO_OVERLAP_PREVIOUS) may run beside the call directly before it, and must share no buffer
+ * with that call.
  */
 #ifndef PREBA_TOKENS_H_
 #define PREBA_TOKENS_H_
