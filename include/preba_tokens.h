@@ -35,6 +35,7 @@ extern "C" {
 #define PREBA_PAGES_MAX_REQUESTS 16384u /* requests in one call */
 #define PREBA_PAGES_MAX_PAGE 256u       /* page sizes: powers of two from 8 to this */
 #define PREBA_PAGES_MAX_HEAD_DIM 128u   /* head sizes: multiples of 8 up to this */
+#define PREBA_PAGES_MAX_KEYS 0x7ffff000u /* tokens of one request, cached and fresh (2^31 - 4096) */
 #define PREBA_ROPE_MAX_POSITION (1 << 24)
 
 /*
@@ -44,10 +45,10 @@ extern "C" {
  * step, in request order, is free_pages[*free_count - 1 - k]), and appends them to its row of the
  * table.  Slot = page * page_size + position mod page_size.  The call reads *free_count and writes
  * *free_left, and nothing that it reads: run twice on the same inputs it writes the same again.
- * A request is refused if its lengths are negative, if its row of the table is too short, if its
- * rows end beyond `tokens` (status PREBA_ERR_BAD_TABLE) or if the free pages do not suffice for it
- * and those before it (PREBA_ERR_BUFFER_TOO_SMALL): it gets no page, its slots are -1 and its kv_len
- * is 0.  Tokens behind the last request's get slot -1 and position 0, so that a step can be padded.
+ * A request is refused if its lengths are negative or add up to more than PREBA_PAGES_MAX_KEYS, if its
+ * row of the table is too short, if its rows end beyond `tokens` (status PREBA_ERR_BAD_TABLE) or if the
+ * free pages do not suffice for it and those before it (PREBA_ERR_BUFFER_TOO_SMALL): it gets no page,
+ * its slots are -1 and its kv_len is 0.  Tokens behind the last request's get slot -1 and position 0, so that a step can be padded.
  * All buffers are distinct; one kernel launch.
  * Errors: PREBA_ERR_INVALID_ARG (NULL, n == 0 or above PREBA_PAGES_MAX_REQUESTS, page_size not a power
  * of two in 8 .. PREBA_PAGES_MAX_PAGE, pages * page_size above 2^31 - 1), PREBA_ERR_CUDA.

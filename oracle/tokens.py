@@ -7,6 +7,8 @@ import math
 
 import numpy as np
 
+MAX_KEYS = 2**31 - 4096  # tokens of one request
+
 
 def plan(cached, fresh, table, free_pages, free_count, page, tokens):
     """Block table, row starts, key counts, slots, positions and pages left after a step; requests
@@ -23,7 +25,7 @@ def plan(cached, fresh, table, free_pages, free_count, page, tokens):
         begin, end = starts[-1], starts[-1] + max(f, 0)
         starts.append(end)
         pages = -(-(c + f) // page)
-        if c < 0 or f < 0 or end > tokens or pages > table.shape[1]:
+        if c < 0 or f < 0 or c + f > MAX_KEYS or end > tokens or pages > table.shape[1]:
             bad = True
             kv.append(0)
             continue

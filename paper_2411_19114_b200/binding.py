@@ -987,6 +987,7 @@ class PreparedJpeg:
 ROPE_INTERLEAVED, ROPE_AXES_IN_TURN = 1, 2
 ATTEND_CAUSAL = 1
 PAGES_MAX_REQUESTS = 16384
+PAGES_MAX_KEYS = 2**31 - 4096  # tokens of one request
 
 
 def _stream(stream) -> ctypes.c_void_p:

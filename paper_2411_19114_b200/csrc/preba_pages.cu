@@ -88,7 +88,8 @@ plan_kernel(const preba_pages_plan_t p, const uint32_t page_shift) {
   // out of range
   auto need_of = [&](int64_t cached, int64_t fresh, int64_t end) -> int64_t {
     const int64_t pages = (cached + fresh + page_mask) >> page_shift;
-    if (cached < 0 || fresh < 0 || end > p.tokens || pages > p.table_width) return -1;
+    if (cached < 0 || fresh < 0 || end > p.tokens || pages > p.table_width || cached + fresh > PREBA_PAGES_MAX_KEYS)
+      return -1;  // places within a request and numbers of keys are 32-bit, here and in the calls that follow
     return pages - ((cached + page_mask) >> page_shift);
   };
   sums_t mine{0, 0}, total;
