@@ -175,11 +175,11 @@ int preba_rope_append(const preba_rope_append_t* req, void* stream);
  *                             the caller zeroes the workspace once, every call leaves its counters
  *                             zeroed again; calls that may overlap on the device need one each.
  * A request is skipped (its rows are not written) and PREBA_ERR_BAD_TABLE stored if its rows are out of range or
- * more than max_q, or if kv_len is negative or beyond its row of the table; a seen page number that
- * is out of range reads as zeros and stores PREBA_ERR_BAD_TABLE.
+ * more than max_q, or if kv_len is negative, beyond its row of the table or above PREBA_PAGES_MAX_KEYS; a
+ * seen page number that is out of range reads as zeros and stores PREBA_ERR_BAD_TABLE.
  * Errors: PREBA_ERR_INVALID_ARG (also: a base that is not 16-byte aligned, a stride that is not a
  * multiple of 8, heads_q not a multiple of heads_kv, more than 128 query heads on one key head,
- * page_size as for preba_pages_plan, head_dim not a multiple of 8 in 8 .. PREBA_PAGES_MAX_HEAD_DIM, a
+ * page_size as for preba_pages_plan, tokens above PREBA_PAGES_MAX_KEYS, head_dim not a multiple of 8 in 8 .. PREBA_PAGES_MAX_HEAD_DIM, a
  * stride of 0 on an axis of q or a cache that has more than one entry, or tables so wide that
  * n * heads_kv * (table_width * page_size / 64 + 2) passes 2e9), PREBA_ERR_BUFFER_TOO_SMALL (workspace),
  * PREBA_ERR_CUDA.

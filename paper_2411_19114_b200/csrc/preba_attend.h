@@ -46,7 +46,8 @@ __device__ __forceinline__ bool load_request(const preba_pages_attend_t& p, uint
   q.rows = b - a;
   q.keys = kv;
   return !(a < 0 || b < a || static_cast<uint32_t>(b) > p.tokens || static_cast<uint32_t>(b - a) > p.max_q ||
-           kv < 0 || static_cast<uint64_t>(kv) > static_cast<uint64_t>(p.table_width) * p.page_size);
+           kv < 0 || static_cast<uint32_t>(kv) > PREBA_PAGES_MAX_KEYS ||  // key numbers stay 32-bit past a tile's end
+           static_cast<uint64_t>(kv) > static_cast<uint64_t>(p.table_width) * p.page_size);
 }
 
 // Rows j0 .. j1-1 of a request see keys in [lo, hi) and no others (each row its own part of them).
