@@ -180,9 +180,10 @@ int preba_rope_append(const preba_rope_append_t* req, void* stream);
  * Errors: PREBA_ERR_INVALID_ARG (also: a base that is not 16-byte aligned, a stride that is not a
  * multiple of 8, heads_q not a multiple of heads_kv, more than 128 query heads on one key head,
  * page_size as for preba_pages_plan, tokens above PREBA_PAGES_MAX_KEYS, head_dim not a multiple of 8 in 8 .. PREBA_PAGES_MAX_HEAD_DIM, a
- * stride of 0 on an axis of q or a cache that has more than one entry, or tables so wide that
- * n * heads_kv * (table_width * page_size / 64 + 2) passes 2e9), PREBA_ERR_BUFFER_TOO_SMALL (workspace),
- * PREBA_ERR_CUDA.
+ * stride of 0 on an axis of q or a cache that has more than one entry, tables so wide that
+ * n * heads_kv * (table_width * page_size / 64 + 2) passes 2e9, or, with more than 16 rows on a key head
+ * (max_q * heads_q / heads_kv), so many rows that heads_kv * (n + tokens / (2 * g)) passes 2^31 - 1, where
+ * g = 128 * heads_kv / heads_q rounded down), PREBA_ERR_BUFFER_TOO_SMALL (workspace), PREBA_ERR_CUDA.
  */
 typedef struct {
   const void* q;              /* DEVICE, [tokens, heads_q, head_dim] */

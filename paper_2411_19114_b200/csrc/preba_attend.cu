@@ -4,6 +4,7 @@
 #include <type_traits>
 
 #include "preba_attend.h"
+#include "preba_attend_plan.h"
 
 namespace preba {
 namespace {
@@ -686,13 +687,16 @@ extern "C" int preba_pages_attend(const preba_pages_attend_t* req, void* stream)
   if (!p.workspace || (reinterpret_cast<uintptr_t>(p.workspace) & 15)) return PREBA_ERR_INVALID_ARG;
   const uint32_t group = p.heads_q / p.heads_kv;
   if (p.workspace_bytes < workspace_of(p.n, p.tokens, group, p.head_dim)) return PREBA_ERR_BUFFER_TOO_SMALL;
+  const bool few = static_cast<uint64_t>(group) * p.max_q <= kRowsMax;
+  // claims of the kernel for many rows are numbered in 32 bits
+  if (!few && pairs_at_most(p.n, p.tokens, group) * p.heads_kv > INT32_MAX) return PREBA_ERR_INVALID_ARG;
   const uint32_t shift = 31 - __builtin_clz(p.page_size);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   int device = 0, sms = 0;
   cudaError_t err = cudaGetDevice(&device);
   if (err == cudaSuccess) err = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
   if (err != cudaSuccess) return finish(err);
-  if (static_cast<uint64_t>(group) * p.max_q <= kRowsMax) {
+  if (few) {
     const uint32_t box_rows = std::min<uint32_t>(p.page_size, kTileKeys);
     const few_args a{p, shift, group, box_rows, 31u - __builtin_clz(box_rows)};
     if (p.dtype == PREBA_F16)

@@ -28,13 +28,14 @@
 #include <type_traits>
 
 #include "preba_attend.h"
+#include "preba_attend_plan.h"
 
 namespace preba {
 namespace {
 
 using namespace attend;
 
-constexpr int kTile = 128;             // rows of a tile, keys of a slot
+constexpr int kTile = kTileRows;       // rows of a tile, keys of a slot
 constexpr int kSoftWarps = 8;          // four per tile
 constexpr int kCopyWarp = 8, kMmaWarp = 9;
 constexpr int kThreads = 32 * 12;       // the last two warps only complete the third warpgroup
@@ -42,7 +43,6 @@ constexpr int kThreads = 32 * 12;       // the last two warps only complete the 
 constexpr int kSoftRegisters = 208, kOtherRegisters = 88;
 static_assert(256 * kSoftRegisters + 128 * kOtherRegisters <= 168 * kThreads, "register split");
 constexpr uint32_t kTmemColumns = 512;
-constexpr uint32_t kMinRun = 2;        // key tiles of a CTA's run in the line, at least
 constexpr float kGrowth = 8.f;         // log2 of what a row may outgrow its reference by
 
 template <int DP> struct layout {      // DP: head_dim rounded up to 64 or 128
@@ -145,25 +145,26 @@ __device__ __forceinline__ pair_range range_of(const tiles_args& a, const reques
 constexpr int kPlanThreads = 1024;
 constexpr int kBins = 1024;
 
-__device__ __forceinline__ uint32_t block_exclusive(uint32_t v, uint32_t* warp_sums, uint32_t& total) {
+// In 64 bits: 2^30 pairs of up to 2^24 key tiles are possible.
+__device__ __forceinline__ uint64_t block_exclusive(uint64_t v, uint64_t* warp_sums, uint64_t& total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  uint32_t incl = v;
+  uint64_t incl = v;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const uint32_t up = __shfl_up_sync(kFull, incl, o);
+    const uint64_t up = __shfl_up_sync(kFull, incl, o);
     if (lane >= o) incl += up;
   }
   if (lane == 31) warp_sums[warp] = incl;
   __syncthreads();
-  const uint32_t s = warp_sums[lane];
-  uint32_t up_to = s;
+  const uint64_t s = warp_sums[lane];
+  uint64_t up_to = s;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const uint32_t up = __shfl_up_sync(kFull, up_to, o);
+    const uint64_t up = __shfl_up_sync(kFull, up_to, o);
     if (lane >= o) up_to += up;
   }
   total = __shfl_sync(kFull, up_to, 31);
-  const uint32_t before = __shfl_sync(kFull, up_to - s, warp);
+  const uint64_t before = __shfl_sync(kFull, up_to - s, warp);
   __syncthreads();
   return before + incl - v;
 }
@@ -172,14 +173,15 @@ __global__ void __launch_bounds__(kPlanThreads) tiles_plan_kernel(const tiles_ar
   extern __shared__ __align__(16) uint8_t plan_smem[];
   pair_t* near = reinterpret_cast<pair_t*>(plan_smem);  // the first kPlanThreads pairs
   uint32_t* pairs_before = reinterpret_cast<uint32_t*>(near + kPlanThreads);  // n + 1: pairs of the requests before
-  __shared__ uint32_t warp_sums[32], bins[kBins], longest;
+  __shared__ uint64_t warp_sums[32];
+  __shared__ uint32_t bins[kBins], longest;
   const preba_pages_attend_t& p = a.p;
   if (threadIdx.x == 0) longest = 0;
   for (uint32_t b = threadIdx.x; b < kBins; b += kPlanThreads) bins[b] = 0;
   chained_begin();
 
-  const uint32_t share = (p.n + kPlanThreads - 1) / kPlanThreads;
-  const uint32_t r0 = min(threadIdx.x * share, p.n), r1 = min(r0 + share, p.n);
+  const uint32_t each = (p.n + kPlanThreads - 1) / kPlanThreads;
+  const uint32_t r0 = min(threadIdx.x * each, p.n), r1 = min(r0 + each, p.n);
   auto pairs_of = [&](uint32_t r) -> uint32_t {
     request_t q;
     if (!load_request(p, r, q)) {
@@ -188,22 +190,20 @@ __global__ void __launch_bounds__(kPlanThreads) tiles_plan_kernel(const tiles_ar
     }
     return (q.rows + 2 * a.tokens_per_tile - 1) / (2 * a.tokens_per_tile);
   };
-  uint32_t mine = 0;
+  uint64_t mine = 0, all_pairs;
   for (uint32_t r = r0; r < r1; ++r) mine += pairs_of(r);
-  uint32_t n_pairs;
-  uint32_t at = block_exclusive(mine, warp_sums, n_pairs);
+  uint64_t at = block_exclusive(mine, warp_sums, all_pairs);
+  // rows of different requests do not overlap in a valid step; if they do, the list ends early
+  const uint64_t listed = min(all_pairs, static_cast<uint64_t>(a.max_pairs));
+  const uint32_t n_pairs = static_cast<uint32_t>(listed);
+  if (all_pairs > listed && threadIdx.x == 0) report(p.status, PREBA_ERR_BAD_TABLE);
   for (uint32_t r = r0; r < r1; ++r) {
-    pairs_before[r] = at;
+    pairs_before[r] = static_cast<uint32_t>(min(at, listed));
     at += pairs_of(r);
   }
   if (threadIdx.x == 0) pairs_before[p.n] = n_pairs;
   __syncthreads();
-  // rows of different requests do not overlap in a valid step; if they do, the list ends early
-  if (n_pairs > a.max_pairs) {
-    if (threadIdx.x == 0) report(p.status, PREBA_ERR_BAD_TABLE);
-    n_pairs = a.max_pairs;
-  }
-  uint32_t total = 0;
+  uint64_t total = 0;
   for (uint32_t base = 0; base < n_pairs; base += kPlanThreads) {
     const uint32_t i = base + threadIdx.x;
     uint32_t tiles = 0, r = 0;
@@ -219,10 +219,10 @@ __global__ void __launch_bounds__(kPlanThreads) tiles_plan_kernel(const tiles_ar
       const pair_range range = range_of(a, q, i - pairs_before[r]);
       tiles = range.end - range.begin;
     }
-    uint32_t sum;
-    const uint32_t before = block_exclusive(tiles, warp_sums, sum);
-    if (i < n_pairs) {
-      const pair_t pair{r, i - pairs_before[r], total + before, tiles, q.row, q.rows, q.keys, 0};
+    uint64_t sum;
+    const uint64_t before = total + block_exclusive(tiles, warp_sums, sum);
+    if (i < n_pairs) {  // `before` means something in a line only, where it is below 2^31
+      const pair_t pair{r, i - pairs_before[r], static_cast<uint32_t>(before), tiles, q.row, q.rows, q.keys, 0};
       a.pairs[i] = pair;
       if (i < kPlanThreads) near[i] = pair;
       atomicMax(&longest, tiles);
@@ -230,15 +230,11 @@ __global__ void __launch_bounds__(kPlanThreads) tiles_plan_kernel(const tiles_ar
     total += sum;
   }
   __syncthreads();
-  // claimed one by one if the longest is short beside a CTA's share of the line
-  const uint64_t units = static_cast<uint64_t>(total) * p.heads_kv;
-  // (prompts, longest a quarter of the share: claimed 324 us; a chunk over a long cache, longest 2.3 times
-  // the share: 216 us in equal runs, against 1.5 shares and more if each were one CTA's)
-  const bool claim = 3ull * longest * a.grid <= units;
-  const uint32_t per = max(kMinRun, static_cast<uint32_t>((units + a.grid - 1) / a.grid));
+  const share_t share = share_out(total, p.heads_kv, longest, a.grid);
+  const uint32_t per = share.per;
   for (uint32_t c = threadIdx.x; c < a.grid; c += kPlanThreads) a.runs[c].first = a.runs[c].last = 0;
   __syncthreads();
-  if (!claim) {
+  if (!share.claim) {
     // a pair writes down the runs that begin in it, with as many threads as there are for each
     uint32_t lanes = 32;
     while (lanes > 1 && n_pairs * lanes > kPlanThreads) lanes /= 2;
@@ -258,9 +254,9 @@ __global__ void __launch_bounds__(kPlanThreads) tiles_plan_kernel(const tiles_ar
     };
     for (uint32_t i = threadIdx.x; i < n_pairs; i += kPlanThreads) atomicAdd(&bins[bin_of(i < kPlanThreads ? near[i].tiles : a.pairs[i].tiles)], 1);
     __syncthreads();
-    uint32_t sum;
-    const uint32_t before = block_exclusive(bins[threadIdx.x], warp_sums, sum);
-    bins[threadIdx.x] = before;
+    uint64_t sum;
+    const uint64_t before = block_exclusive(bins[threadIdx.x], warp_sums, sum);
+    bins[threadIdx.x] = static_cast<uint32_t>(before);
     __syncthreads();
     for (uint32_t i = threadIdx.x; i < n_pairs; i += kPlanThreads)
       a.order[atomicAdd(&bins[bin_of(i < kPlanThreads ? near[i].tiles : a.pairs[i].tiles)], 1)] = i;
@@ -269,8 +265,8 @@ __global__ void __launch_bounds__(kPlanThreads) tiles_plan_kernel(const tiles_ar
     tiles_head h;
     h.next = 0;
     h.n_pairs = n_pairs;
-    h.units = static_cast<uint32_t>(units);
-    h.claim = claim;
+    h.units = share.units;
+    h.claim = share.claim;
     h.per = per;
     *a.head = h;
   }
@@ -280,7 +276,7 @@ static_assert(kBins == kPlanThreads, "one bin per thread in the sum");
 // The same by a CTA of the kernel itself, for itself: where there are few pairs, all of them are certain to
 // form one line, and a CTA needs its own run of it only.  One launch and 1.6 to 5 us less per call (4 chunks of 32
 // tokens over 500 keys 16.5 -> 14.9 us, 512 tokens over 30000 keys 247 -> 241 us).
-constexpr uint32_t kOwnPairs = 3 * kMaxTileCtas;  // fewer than this, and they cannot be claimed one by one
+static_assert(kOwnPairs == 3 * kMaxTileCtas, "fewer than this, and they cannot be claimed one by one");
 
 struct own_plan_t {
   run_t run;
@@ -1126,10 +1122,6 @@ cudaError_t launch(const tiles_args& a, cudaStream_t stream) {
 
 uint64_t up16(uint64_t v) { return (v + 15) / 16 * 16; }
 
-uint64_t pairs_at_most(uint32_t n, uint32_t tokens, uint32_t group) {
-  return tokens / (2 * (kTile / group)) + n;
-}
-
 }  // namespace
 
 namespace attend {
@@ -1162,8 +1154,8 @@ cudaError_t launch_tiles(const preba_pages_attend_t& p, uint32_t page_shift, int
   a.order = reinterpret_cast<uint32_t*>(at);
   at += up16(4 * pairs);
   a.partials = reinterpret_cast<float4*>(at);
-  // claims need three pairs (on one key head) a CTA at least
-  a.own_plan = pairs < kOwnPairs && pairs * p.heads_kv < 3ull * a.grid;
+  a.own_plan = plans_own(pairs, p.heads_kv, a.grid,
+                         std::min<uint64_t>(static_cast<uint64_t>(p.table_width) * p.page_size, PREBA_PAGES_MAX_KEYS));
   const size_t smem = kPlanThreads * sizeof(pair_t) + 4 * (static_cast<size_t>(p.n) + 1);
   if (smem > 40 * 1024) {  // beside 5 KB of its own; 48 KB need no leave
     const cudaError_t err = cudaFuncSetAttribute(tiles_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
