@@ -165,7 +165,8 @@ int preba_rope_append(const preba_rope_append_t* req, void* stream);
  * head h / (heads_q / heads_kv):
  *   out = sum_k p_k v_k / sum_k p_k,   p_k = exp(scale q.k_k - m),   m = max_k scale q.k_k
  *   lse = m + ln sum_k p_k
- * A row that sees no key is 0, its lse -inf (kv_len may be 0, or below q_len).  Products and sums
+ * A row that sees no key is 0, its lse -inf (kv_len may be 0, or below q_len); so is one whose scores
+ * are all -inf.  A row with a score that is not a number is not a number, nor is its lse.  Products and sums
  * are fp32; p is rounded to the cache's type for the product with v, as the matrix instructions
  * take it, and out is rounded once.  Cache slots that no row of the request sees may hold anything,
  * infinities and NaN included, and table entries whose pages no row sees are not followed; a key or

@@ -210,8 +210,7 @@ __device__ __forceinline__ void store_rows(const few_args& a, const request_t& q
         *reinterpret_cast<uint32_t*>(to + e) = pack2<T>(o[n][2 * i] * inv, o[n][2 * i + 1] * inv);
     }
     if (p.lse && first_tile == 0 && (lane & 3) == 0)
-      p.lse[static_cast<uint64_t>(t) * p.heads_q + h] =
-          l[i] > 0.f ? (m[i] + log2f(l[i])) * kLn2 : -INFINITY;
+      p.lse[static_cast<uint64_t>(t) * p.heads_q + h] = row_lse(m[i], l[i]);
   }
 }
 
@@ -430,7 +429,7 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
     if ((lane & 3) == 0)
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        stats[(2 * warp + 0) * kRowsMax + (lane >> 2) + 8 * i] = m[i];
+        stats[(2 * warp + 0) * kRowsMax + (lane >> 2) + 8 * i] = marked(m[i], l[i]);
         stats[(2 * warp + 1) * kRowsMax + (lane >> 2) + 8 * i] = l[i];
       }
     consumers_sync();
@@ -481,7 +480,7 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
       if (warp == 0 && (lane & 3) == 0)
 #pragma unroll
         for (int i = 0; i < 2; ++i)
-          (to - lane)[kRowsMax * DP / 2 + (lane >> 2) + 8 * i] = make_float2(m[i], l[i]);
+          (to - lane)[kRowsMax * DP / 2 + (lane >> 2) + 8 * i] = make_float2(marked(m[i], l[i]), l[i]);
       if (threadIdx.x == 0) {
         const uint32_t start = w.unit - w.count - w.tile;  // of the (request, key head)
         ctl.pieces[slot] = {1, w.request, w.head, start / run.per, (start + w.tiles - 1) / run.per};

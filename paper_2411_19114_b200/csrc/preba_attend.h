@@ -108,6 +108,14 @@ __device__ __forceinline__ float exp2_approx(float x) {
   return y;
 }
 
+// Maxima leave out what is not a number, sums do not.  A partial sum whose row saw such a score carries that
+// in its maximum too, so that -inf there means nothing but "no key seen".
+__device__ __forceinline__ float marked(float m, float l) { return l != l ? l : m; }
+// The log-sum-exp of a row from its sum and maximum in units of log2.
+__device__ __forceinline__ float row_lse(float m, float l) {
+  return l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+}
+
 template <typename T> __device__ __forceinline__ uint32_t pack2(float a, float b);
 template <> __device__ __forceinline__ uint32_t pack2<__half>(float a, float b) {
   const __half2 h = __floats2half2_rn(a, b);

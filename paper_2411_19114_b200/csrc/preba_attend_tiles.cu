@@ -999,7 +999,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
           }
         }
         if (p.lse && write)
-          p.lse[static_cast<uint64_t>(tok) * p.heads_q + h] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+          p.lse[static_cast<uint64_t>(tok) * p.heads_q + h] = row_lse(m, l);
       } else {
         // partial sums, four columns of 256 rows after the other, then maxima and sums
         float4* to = a.partials + static_cast<uint64_t>(item.slot) * kPartial<DP> + x * kTile + r;
@@ -1014,7 +1014,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
               to[(c + i) / 4 * 2 * kTile] = make_float4(__uint_as_float(o[i]), __uint_as_float(o[i + 1]),
                                                         __uint_as_float(o[i + 2]), __uint_as_float(o[i + 3]));
           }
-        reinterpret_cast<float2*>(to - (x * kTile + r) + DP / 4 * 2 * kTile)[x * kTile + r] = make_float2(m, l);
+        reinterpret_cast<float2*>(to - (x * kTile + r) + DP / 4 * 2 * kTile)[x * kTile + r] = make_float2(marked(m, l), l);
       }
       fence_before();
     }
@@ -1097,7 +1097,7 @@ __global__ void __launch_bounds__(2 * kTile, 2) tiles_join_kernel(const __grid_c
       *reinterpret_cast<uint4*>(to + i) = v;
     }
   if (p.lse && e == 0)
-    p.lse[static_cast<uint64_t>(tok) * p.heads_q + h] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+    p.lse[static_cast<uint64_t>(tok) * p.heads_q + h] = row_lse(m, l);
 }
 
 template <typename T, int DP>
