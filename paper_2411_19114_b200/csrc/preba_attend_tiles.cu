@@ -564,6 +564,9 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  chained_begin();
+  // Only now: a kernel before this one that has let it in may still have its tensor memory to allocate, and
+  // would wait for this CTA as this CTA waits for it.
   if (warp == kMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(tmem_slot)),
                  "n"(kTmemColumns)
@@ -574,7 +577,6 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
   __syncthreads();
   fence_after();
   const uint32_t tmem = *tmem_slot;
-  chained_begin();
   own_plan_t& own = *reinterpret_cast<own_plan_t*>(smem + L::kPlan);
   if (a.own_plan) plan_own(a, own);
   bool ok = true;

@@ -43,6 +43,7 @@ __device__ __forceinline__ bool range_violation(int32_t* status) {
 // for everything before it to be complete and then lets the kernel behind it be set up likewise.  No block
 // touches memory that another kernel may write or read before it has passed, and every block has to
 // pass, even one with nothing to do: so stream order holds as for any launch, whatever the neighbours are.
+// Nor does a block take what the kernel before may still be waiting for, tensor memory above all.
 namespace preba {
 __device__ __forceinline__ void chained_begin() {
   asm volatile("griddepcontrol.wait;" ::: "memory");
