@@ -178,6 +178,8 @@ int preba_rope_append(const preba_rope_append_t* req, void* stream);
  * A request is skipped (its rows are not written) and PREBA_ERR_BAD_TABLE stored if its rows are out of range or
  * more than max_q, or if kv_len is negative, beyond its row of the table or above PREBA_PAGES_MAX_KEYS; a
  * seen page number that is out of range reads as zeros and stores PREBA_ERR_BAD_TABLE.
+ * Every wait of the kernels has a limit.  If one runs out, PREBA_ERR_TIMEOUT is stored and the rows that the
+ * call would have written hold anything; nothing else does, and the workspace is left as by any call.
  * Errors: PREBA_ERR_INVALID_ARG (also: a base that is not 16-byte aligned, a stride that is not a
  * multiple of 8, heads_q not a multiple of heads_kv, more than 128 query heads on one key head,
  * page_size as for preba_pages_plan, tokens above PREBA_PAGES_MAX_KEYS, head_dim not a multiple of 8 in 8 .. PREBA_PAGES_MAX_HEAD_DIM, a

@@ -67,6 +67,9 @@ static_assert(sizeof(control_t) <= 128, "few_layout::kBytes");
 struct few_args {
   preba_pages_attend_t p;
   uint32_t page_shift, group, box_rows, box_shift;
+#if defined(PREBA_CHECKED)
+  wait_limits_t limits = wait_limits();
+#endif
 };
 
 __device__ __forceinline__ uint32_t few_tiles(const preba_pages_attend_t& p, const request_t& q,
@@ -247,6 +250,7 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
   chained_begin();
   find_run(a, &ctl.run, ctl.warp_sums);  // synchronises
   const run_t run = ctl.run;
+  waits_t wait(a);
   if (run.begin >= run.end) return;
   walk_t w;
   w.unit = run.begin;
@@ -276,7 +280,7 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
         const bool wanted = mine && key < w.hi && key + static_cast<int32_t>(a.box_rows) > w.lo;
         int32_t from = page;
         if (t + 1 < w.count) page = entry(key + kTileKeys);
-        ok = mbar_wait(empty + 8 * stage, phase);
+        ok = wait(empty + 8 * stage, phase);
         if (!ok) break;
         const uint32_t count = __popc(__ballot_sync(kFull, wanted));
         if (lane == 0) mbar_arrive_expect_tx(full + 8 * stage, count * a.box_rows * 128);
@@ -346,7 +350,7 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
     l[0] = l[1] = 0.f;
     int32_t key0 = (w.lo / kTileKeys + w.tile) * kTileKeys + 16 * warp;
     for (uint32_t t = 0; t < w.count && ok; ++t, key0 += kTileKeys) {
-      ok = mbar_wait(full + 8 * stage, phase);
+      ok = wait(full + 8 * stage, phase);
       if (!ok) break;
       const uint32_t ks_base = base + stage * L::kStage, vs_base = ks_base + L::kOperand;
       float s[2][4] = {};
@@ -668,6 +672,17 @@ extern "C" int preba_pages_attend_query(uint32_t n, uint32_t tokens, uint32_t he
   *workspace_bytes = workspace_of(n, tokens, heads_q / heads_kv, head_dim);
   return PREBA_OK;
 }
+
+#if defined(PREBA_CHECKED)
+// For tests of the checked build: from the next call on, a warp's wait runs out after `waits` that did not, or
+// when it has polled `polls` times.  0, 0: as ever.
+static std::atomic<uint32_t> g_checked_waits{UINT32_MAX}, g_checked_polls{preba::attend::kSpinLimit};
+extern "C" void preba_checked_waits(uint32_t waits, uint32_t polls) {
+  g_checked_waits = polls ? waits : UINT32_MAX;
+  g_checked_polls = polls ? polls : preba::attend::kSpinLimit;
+}
+preba::attend::wait_limits_t preba::attend::wait_limits() { return {g_checked_waits, g_checked_polls}; }
+#endif
 
 extern "C" int preba_pages_attend(const preba_pages_attend_t* req, void* stream) {
   using namespace preba;

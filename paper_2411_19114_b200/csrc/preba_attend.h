@@ -85,12 +85,36 @@ __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
       : "memory");
   return ok != 0;
 }
-// Waits for the phase with the given parity to complete; false if the limit ran out.
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity) {
-  for (uint32_t it = 0; it < kSpinLimit; ++it)
-    if (mbar_try_wait(bar, parity)) return true;
+// A whole warp waits for the phase with the given parity to complete; false if the limit ran out.  The lanes
+// agree on it: what follows are instructions that the whole warp has to take part in.
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, uint32_t limit = kSpinLimit) {
+  for (uint32_t it = 0; it < limit; ++it)
+    if (__all_sync(kFull, mbar_try_wait(bar, parity))) return true;
   return false;
 }
+
+// The waits of a warp.  The checked build can have them run out early (preba_checked_waits), so that tests
+// see what the kernels leave then; what a kernel waits for after that, before it returns, has the full limit.
+#if defined(PREBA_CHECKED)
+struct wait_limits_t {
+  uint32_t waits, polls;  // waits of a warp before one runs out; polls of one wait
+};
+wait_limits_t wait_limits();
+struct waits_t {
+  wait_limits_t left;
+  template <typename A> __device__ __forceinline__ explicit waits_t(const A& a) : left(a.limits) {}
+  __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity) {
+    if (left.waits == 0) return false;
+    --left.waits;
+    return mbar_wait(bar, parity, left.polls);
+  }
+};
+#else
+struct waits_t {
+  template <typename A> __device__ __forceinline__ explicit waits_t(const A&) {}
+  __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity) { return mbar_wait(bar, parity); }
+};
+#endif
 
 // One box of a four-dimensional tensor into shared memory.
 __device__ __forceinline__ void tensor_copy(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y,

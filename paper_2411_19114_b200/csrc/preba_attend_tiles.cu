@@ -110,6 +110,9 @@ struct tiles_args {
   run_t* runs;        // one per CTA
   uint32_t* order;    // pairs, longest first
   float4* partials;   // two per CTA
+#if defined(PREBA_CHECKED)
+  wait_limits_t limits = wait_limits();
+#endif
 };
 
 struct pair_range {
@@ -579,6 +582,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
   const uint32_t tmem = *tmem_slot;
   own_plan_t& own = *reinterpret_cast<own_plan_t*>(smem + L::kPlan);
   if (a.own_plan) plan_own(a, own);
+  waits_t wait(a);
   bool ok = true;
 
   if (warp >= kSoftWarps) {
@@ -670,7 +674,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
             item.last[x] = max(item.first[x], min(range.last[x], item.tile + item.count));
           }
         }
-        ok = mbar_wait(item_empty + 8 * out.slot, out.phase ^ 1);
+        ok = wait(item_empty + 8 * out.slot, out.phase ^ 1);
         if (!ok) break;
         if (lane == 0) {
           items[out.slot] = item;
@@ -679,7 +683,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
         out.step();
         if (done) break;
         // queries
-        ok = mbar_wait(q_empty, q_ring.phase ^ 1);
+        ok = wait(q_empty, q_ring.phase ^ 1);
         if (!ok) break;
         if (lane == 0) {
           const uint32_t bytes = a.tokens_per_tile * a.group * 128 * L::kHalves;
@@ -710,7 +714,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
           const uint32_t bytes = __popc(__ballot_sync(kFull, want)) * a.box_rows * 128;
 #pragma unroll
           for (int v = 0; v < 2; ++v) {
-            ok = ok && mbar_wait(kv_empty + 8 * kv.slot, kv.phase ^ 1);
+            ok = ok && wait(kv_empty + 8 * kv.slot, kv.phase ^ 1);
             if (!ok) break;
             if (lane == 0) mbar_arrive_expect_tx(kv_full + 8 * kv.slot, bytes);
             __syncwarp();
@@ -735,14 +739,14 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
       ring<1> q_ring, p_ring[2];
       ring<2> in;
       while (ok) {
-        ok = mbar_wait(item_full + 8 * in.slot, in.phase);
+        ok = wait(item_full + 8 * in.slot, in.phase);
         if (!ok) break;
         const item_t item = items[in.slot];
         __syncwarp();
         if (lane == 0) mbar_arrive(item_empty + 8 * in.slot);
         in.step();
         if (item.count == 0) break;
-        ok = mbar_wait(q_full, q_ring.phase);
+        ok = wait(q_full, q_ring.phase);
         if (!ok) break;
         q_ring.step();
         const int32_t end = item.tile + item.count;
@@ -773,7 +777,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
           __syncwarp();
         };
         // keys of the first tile
-        ok = mbar_wait(kv_full + 8 * kv.slot, kv.phase);
+        ok = wait(kv_full + 8 * kv.slot, kv.phase);
         if (!ok) break;
         fence_after();
         k_slot = kv.slot;
@@ -786,7 +790,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
           if (item.count == 1) mma_commit(q_empty);
         }
         for (int32_t t = item.tile; t < end && ok; ++t) {
-          ok = mbar_wait(kv_full + 8 * kv.slot, kv.phase);
+          ok = wait(kv_full + 8 * kv.slot, kv.phase);
           if (!ok) break;
           v_slot = kv.slot;
           kv.step();
@@ -810,11 +814,11 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
           for (int x = 0; x < 2; ++x) {
             if (t >= item.first[x] && t < item.last[x]) {
               // the product with the first half of P while the second is being made
-              ok = ok && mbar_wait(h_full + 8 * x, p_ring[x].phase);
+              ok = ok && wait(h_full + 8 * x, p_ring[x].phase);
               if (!ok) break;
               fence_after();
               pv(x, t > item.first[x], 0, kTile / 32);
-              ok = ok && mbar_wait(p_full + 8 * x, p_ring[x].phase);
+              ok = ok && wait(p_full + 8 * x, p_ring[x].phase);
               if (!ok) break;
               p_ring[x].step();
               fence_after();
@@ -823,7 +827,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
             }
             if (t + 1 >= item.first[x] && t + 1 < item.last[x]) {
               if (!k_waited) {
-                ok = ok && mbar_wait(kv_full + 8 * kv.slot, kv.phase);
+                ok = ok && wait(kv_full + 8 * kv.slot, kv.phase);
                 if (!ok) break;
                 fence_after();
                 k_slot = kv.slot;
@@ -845,7 +849,9 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
       }
       if (!ok) {
         report(p.status, PREBA_ERR_TIMEOUT);
-        if (lane == 0) mma_commit(drained);  // what was issued ends before the memory goes to another
+        // what was issued ends before the memory goes to another; a commit counts its own thread's products
+        if (elected()) mma_commit(drained);
+        __syncwarp();
         mbar_wait(drained, 0);
       }
     }
@@ -866,7 +872,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
     ring<1> s_ring, o_ring;
     ring<2> in;
     while (ok) {
-      ok = mbar_wait(item_full + 8 * in.slot, in.phase);
+      ok = wait(item_full + 8 * in.slot, in.phase);
       if (!ok) break;
       const item_t item = items[in.slot];
       const int32_t first = items[in.slot].first[x], last = items[in.slot].last[x];
@@ -886,7 +892,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
       seen_by(p, q, token + tokens - 1, token + tokens, all_lo, high);
       float m = -INFINITY, l = 0.f;
       for (int32_t t = first; t < last && ok; ++t) {
-        ok = mbar_wait(s_full + 8 * x, s_ring.phase);
+        ok = wait(s_full + 8 * x, s_ring.phase);
         if (!ok) break;
         s_ring.step();
         fence_after();
@@ -967,7 +973,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
       if (!ok) break;
       const bool any = first < last;
       if (any) {
-        ok = mbar_wait(o_full + 8 * x, o_ring.phase);
+        ok = wait(o_full + 8 * x, o_ring.phase);
         if (!ok) break;
         o_ring.step();
         fence_after();
