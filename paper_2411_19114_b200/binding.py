@@ -1023,6 +1023,15 @@ def _heads(t, name: str, dims: int, dtype=None):
     return t
 
 
+def _status(t):
+    """A CUDA int32 tensor of one element, or None."""
+    import torch
+
+    if t is not None and (t.dtype != torch.int32 or t.numel() != 1 or not t.is_cuda):
+        raise ValueError("status must be an int32 CUDA tensor with one element")
+    return t
+
+
 def _same(name: str, got, want) -> None:
     if tuple(got) != tuple(want):
         raise ValueError(f"{name} has shape {tuple(got)}, expected {tuple(want)}")
@@ -1042,6 +1051,8 @@ class _Prepared:
     """The arguments of one call, marshalled once; calling it enqueues the work."""
 
     def _bind(self, name: str, struct, stream, keep) -> None:
+        if len({t.device for t in keep if t is not None}) > 1:
+            raise ValueError(f"{name}: the operands are on different devices")
         self._name, self._call = name, getattr(lib(), name)
         self._keep = (struct, keep)
         self._args = (ctypes.byref(struct), _stream(stream))
@@ -1074,7 +1085,7 @@ class PreparedPagesPlan(_Prepared):
         s.cached, s.fresh, s.block_table = _ptr(cached), _ptr(fresh), _ptr(block_table)
         s.free_pages, s.free_count, s.cu_q = _ptr(free_pages), _ptr(free_count), _ptr(cu_q)
         s.kv_len, s.slots, s.positions = _ptr(kv_len), _ptr(slots), _ptr(positions)
-        s.free_left, s.status = _ptr(free_left), _ptr(status)
+        s.free_left, s.status = _ptr(free_left), _ptr(_status(status))
         s.table_stride, s.table_width = block_table.stride(0), block_table.shape[1]
         s.free_capacity, s.n, s.tokens = free_pages.numel(), n, slots.numel()
         s.page_size = page_size
@@ -1105,7 +1116,7 @@ class PreparedRopePositions(_Prepared):
         _same("positions", positions.shape[:1], (3,))
         s = PrebaRopePositions()
         s.spans, s.span_begin, s.cached = _ptr(spans), _ptr(span_begin), _ptr(cached)
-        s.cu_q, s.positions, s.status = _ptr(cu_q), _ptr(positions), _ptr(status)
+        s.cu_q, s.positions, s.status = _ptr(cu_q), _ptr(positions), _ptr(_status(status))
         s.axis_stride, s.n_spans, s.n = positions.stride(0), spans.shape[0], n
         s.tokens = positions.shape[1]
         self._bind("preba_rope_positions", s, stream,
@@ -1149,7 +1160,7 @@ class PreparedRopeAppend(_Prepared):
         s = PrebaRopeAppend()
         s.q, s.k, s.v, s.q_out = _ptr(q), _ptr(k), _ptr(v), _ptr(q_out)
         s.k_cache, s.v_cache, s.positions = _ptr(k_cache), _ptr(v_cache), _ptr(positions)
-        s.slots, s.inv_freq, s.status = _ptr(slots), _ptr(inv_freq), _ptr(status)
+        s.slots, s.inv_freq, s.status = _ptr(slots), _ptr(inv_freq), _ptr(_status(status))
         s.q_stride[:], s.k_stride[:], s.v_stride[:] = q.stride()[:2], k.stride()[:2], v.stride()[:2]
         s.q_out_stride[:], s.cache_stride[:] = q_out.stride()[:2], k_cache.stride()[:3]
         s.axis_stride, s.sections[:] = positions.stride(0), sections
@@ -1200,12 +1211,14 @@ class PreparedPagesAttend(_Prepared):
         _same("kv_len", _ints(kv_len, "kv_len").shape, (n,))
         if lse is not None:
             _same("lse", lse.shape, (tokens, hq))
-            if lse.dtype != torch.float32 or not lse.is_contiguous():
-                raise ValueError("lse must be a contiguous float32 tensor")
+            if lse.dtype != torch.float32 or not lse.is_cuda or not lse.is_contiguous():
+                raise ValueError("lse must be a contiguous float32 CUDA tensor")
+        if not workspace.is_cuda or not workspace.is_contiguous():
+            raise ValueError("workspace must be a contiguous CUDA tensor")
         s = PrebaPagesAttend()
         s.q, s.k_cache, s.v_cache, s.out = _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(out)
         s.block_table, s.cu_q, s.kv_len = _ptr(block_table), _ptr(cu_q), _ptr(kv_len)
-        s.lse, s.workspace, s.status = _ptr(lse), _ptr(workspace), _ptr(status)
+        s.lse, s.workspace, s.status = _ptr(lse), _ptr(workspace), _ptr(_status(status))
         s.workspace_bytes = workspace.numel() * workspace.element_size()
         s.q_stride[:], s.out_stride[:] = q.stride()[:2], out.stride()[:2]
         s.k_stride[:], s.v_stride[:] = k_cache.stride()[:3], v_cache.stride()[:3]
