@@ -990,13 +990,12 @@ PAGES_MAX_REQUESTS = 16384
 PAGES_MAX_KEYS = 2**31 - 4096  # tokens of one request
 
 
-def _stream(stream) -> ctypes.c_void_p:
-    """A torch stream, a raw cudaStream_t or None for torch's current stream."""
-    if stream is None:
-        import torch
+def _current_stream():
+    """A function from a device's index to the cudaStream_t that is current there (the one that torch's
+    own generated code uses: 0.05 us a call, ``torch.cuda.current_stream`` takes 3)."""
+    import torch
 
-        stream = torch.cuda.current_stream()
-    return ctypes.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
+    return torch._C._cuda_getCurrentRawStream
 
 
 def _ints(t, name: str, dims: int = 1):
@@ -1048,17 +1047,23 @@ def _code(t) -> int:
 
 
 class _Prepared:
-    """The arguments of one call, marshalled once; calling it enqueues the work."""
+    """The arguments of one call, marshalled once; calling it enqueues the work on the ``stream`` that
+    was given (a torch stream or a raw cudaStream_t), or else on the one that is current at the call."""
 
     def _bind(self, name: str, struct, stream, keep) -> None:
         if len({t.device for t in keep if t is not None}) > 1:
             raise ValueError(f"{name}: the operands are on different devices")
         self._name, self._call = name, getattr(lib(), name)
         self._keep = (struct, keep)
-        self._args = (ctypes.byref(struct), _stream(stream))
+        self._struct, self._stream = ctypes.byref(struct), None
+        if stream is not None:
+            self._stream = ctypes.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
+        else:
+            self._current, self._device = _current_stream(), keep[0].device.index
 
     def __call__(self) -> None:
-        rc = self._call(*self._args)
+        stream = self._stream
+        rc = self._call(self._struct, self._current(self._device) if stream is None else stream)
         if rc != OK:
             raise PrebaError(rc, self._name)
 

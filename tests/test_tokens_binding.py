@@ -85,3 +85,16 @@ def test_operands_on_different_devices_are_refused():
     for call in (plan, positions, append, attend):
         with pytest.raises(ValueError, match="devices"):
             call(status=gpu(torch.zeros(1, dtype=torch.int32, device="meta")))
+
+
+def test_the_stream_is_the_one_that_is_current_at_the_call(monkeypatch):
+    current, used = [11], []
+    monkeypatch.setattr(pb, "_current_stream", lambda: lambda device: current[0])
+    for make in (plan, positions, append, attend):
+        for stream, want in ((None, [11, 12]), (77, [77, 77])):
+            call, current[0] = make(stream=stream), 11
+            call._call = lambda struct, at: used.append(getattr(at, "value", at)) or pb.OK
+            call()
+            current[0] = 12
+            call()
+            assert used[-2:] == want
