@@ -76,8 +76,9 @@ class Server:
                                 dtype=torch.uint8, device="cuda")
         pb.preba_pages_attend(q, self.layer.k_cache, self.layer.v_cache, self.table, self.cu_q, self.kv_len,
                               out, workspace, max_q=max_q, scale=DIM ** -0.5, status=self.status)
-        # the step is over: what was fresh is cached, what was taken from the stack is gone
-        self.cached.copy_(self.kv_len)
+        # the step is over: what was fresh is cached, what was taken from the stack is gone.  A request
+        # that was refused (status; its kv_len is 0) keeps its tokens and pages and can be tried again
+        self.cached.copy_(torch.where(self.kv_len > 0, self.kv_len, self.cached))
         self.free_count.copy_(self.free_left)
         return q, out, positions, slots
 

@@ -48,7 +48,9 @@ extern "C" {
  * A request is refused if its lengths are negative or add up to more than PREBA_PAGES_MAX_KEYS, if its
  * row of the table is too short, if its rows end beyond `tokens` (status PREBA_ERR_BAD_TABLE) or if the
  * free pages do not suffice for it and those before it (PREBA_ERR_BUFFER_TOO_SMALL): it gets no page,
- * its slots are -1 and its kv_len is 0.  Tokens behind the last request's get slot -1 and position 0, so that a step can be padded.
+ * its slots are -1 and its kv_len is 0.  What it held it still holds: a caller that takes kv_len over as the
+ * next step's `cached` leaves out the zeros, and may ask for the same tokens again.
+ * Tokens behind the last request's get slot -1 and position 0, so that a step can be padded.
  * All buffers are distinct; one kernel launch.
  * Errors: PREBA_ERR_INVALID_ARG (NULL, n == 0 or above PREBA_PAGES_MAX_REQUESTS, page_size not a power
  * of two in 8 .. PREBA_PAGES_MAX_PAGE, pages * page_size above 2^31 - 1), PREBA_ERR_CUDA.
