@@ -1036,6 +1036,15 @@ def _same(name: str, got, want) -> None:
         raise ValueError(f"{name} has shape {tuple(got)}, expected {tuple(want)}")
 
 
+def _strides(t, dims: int) -> list:
+    """The first strides; an axis of one entry has none to speak of, whatever the tensor says."""
+    return [s if n > 1 else 0 for s, n in zip(t.stride()[:dims], t.shape)]
+
+
+def _row_stride(t) -> int:
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
 def _ptr(t):
     return t.data_ptr() if t is not None else None
 
@@ -1091,7 +1100,7 @@ class PreparedPagesPlan(_Prepared):
         s.free_pages, s.free_count, s.cu_q = _ptr(free_pages), _ptr(free_count), _ptr(cu_q)
         s.kv_len, s.slots, s.positions = _ptr(kv_len), _ptr(slots), _ptr(positions)
         s.free_left, s.status = _ptr(free_left), _ptr(_status(status))
-        s.table_stride, s.table_width = block_table.stride(0), block_table.shape[1]
+        s.table_stride, s.table_width = _row_stride(block_table), block_table.shape[1]
         s.free_capacity, s.n, s.tokens = free_pages.numel(), n, slots.numel()
         s.page_size = page_size
         s.pages = (2**31 - 1) // max(1, page_size) if pages is None else pages
@@ -1154,7 +1163,7 @@ class PreparedRopeAppend(_Prepared):
         _same("q_out", q_out.shape, (tokens, hq, d))
         _same("k_cache", k_cache.shape[2:], (hk, d))
         _same("v_cache", v_cache.shape, k_cache.shape)
-        if v_cache.stride() != k_cache.stride():
+        if _strides(v_cache, 3) != _strides(k_cache, 3):
             raise ValueError("k_cache and v_cache must have the same strides")
         _same("positions", _ints(positions, "positions", 2).shape, (3, tokens))
         _same("slots", _ints(slots, "slots").shape, (tokens,))
@@ -1166,8 +1175,8 @@ class PreparedRopeAppend(_Prepared):
         s.q, s.k, s.v, s.q_out = _ptr(q), _ptr(k), _ptr(v), _ptr(q_out)
         s.k_cache, s.v_cache, s.positions = _ptr(k_cache), _ptr(v_cache), _ptr(positions)
         s.slots, s.inv_freq, s.status = _ptr(slots), _ptr(inv_freq), _ptr(_status(status))
-        s.q_stride[:], s.k_stride[:], s.v_stride[:] = q.stride()[:2], k.stride()[:2], v.stride()[:2]
-        s.q_out_stride[:], s.cache_stride[:] = q_out.stride()[:2], k_cache.stride()[:3]
+        s.q_stride[:], s.k_stride[:], s.v_stride[:] = _strides(q, 2), _strides(k, 2), _strides(v, 2)
+        s.q_out_stride[:], s.cache_stride[:] = _strides(q_out, 2), _strides(k_cache, 3)
         s.axis_stride, s.sections[:] = positions.stride(0), sections
         s.tokens, s.heads_q, s.heads_kv, s.head_dim = tokens, hq, hk, d
         s.rotary_dim = 2 * inv_freq.numel()
@@ -1225,9 +1234,9 @@ class PreparedPagesAttend(_Prepared):
         s.block_table, s.cu_q, s.kv_len = _ptr(block_table), _ptr(cu_q), _ptr(kv_len)
         s.lse, s.workspace, s.status = _ptr(lse), _ptr(workspace), _ptr(_status(status))
         s.workspace_bytes = workspace.numel() * workspace.element_size()
-        s.q_stride[:], s.out_stride[:] = q.stride()[:2], out.stride()[:2]
-        s.k_stride[:], s.v_stride[:] = k_cache.stride()[:3], v_cache.stride()[:3]
-        s.table_stride, s.table_width = block_table.stride(0), block_table.shape[1]
+        s.q_stride[:], s.out_stride[:] = _strides(q, 2), _strides(out, 2)
+        s.k_stride[:], s.v_stride[:] = _strides(k_cache, 3), _strides(v_cache, 3)
+        s.table_stride, s.table_width = _row_stride(block_table), block_table.shape[1]
         s.n, s.tokens, s.max_q, s.heads_q, s.heads_kv = n, tokens, max_q, hq, k_cache.shape[2]
         s.head_dim, s.pages, s.page_size = d, k_cache.shape[0], k_cache.shape[1]
         s.window, s.dtype, s.scale = window, _code(q), scale
