@@ -86,8 +86,9 @@ int preba_pages_plan(const preba_pages_plan_t* plan, void* stream);
  * B + max((t-1)*step + 1, h, w).  A request's tokens past its spans are text.  The call writes the
  * positions of tokens cached[r] .. cached[r] + cu_q[r+1] - cu_q[r] - 1 of every request, so that it
  * serves whole prompts, chunks that begin inside an image, and single tokens alike.
- * A span with a negative member, with w == 0 or step == 0 where h > 0, or whose tokens exceed 2^24 counts as
- * empty (status PREBA_ERR_BAD_TABLE); a request whose rows or spans are out of range is skipped (the same).
+ * A span with a negative member, with w == 0 or step == 0 where h > 0, or whose tokens or step exceed 2^24
+ * counts as empty (status PREBA_ERR_BAD_TABLE); a request whose rows or spans are out of range is skipped (the
+ * same).  Positions are formed modulo 2^32: steps and extents that add up to more than 2^31 - 1 wrap.
  * Rows behind the last request's are written as 0.  One kernel launch.
  * Errors: PREBA_ERR_INVALID_ARG, PREBA_ERR_CUDA.
  */
