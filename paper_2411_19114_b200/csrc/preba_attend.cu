@@ -21,9 +21,11 @@ using namespace attend;
 // CTAs is left as partial sums that the last of them to finish joins, in the order of the keys, so that
 // timing does not change a bit.  Within a tile each of the four warps takes 16 keys with a running maximum
 // and sum of its own; the warps are joined once per (request, key head).  128 single tokens over up to 8192
-// keys of 8 heads of 128: 272 to 278 us (1762 MB, 6.4 TB/s; a copy reaches 6.56); 4 of them over up to 2048
+// keys of 8 heads of 128: 277 to 281 us (1762 MB, 6.3 TB/s; a copy reaches 6.56); 4 of them over up to 2048
 // keys: 13 us, which the launch, the first loads (2.7 us), the partial sums' fence and count (1.5 us) and
-// their join (2 to 3 us) take the most of.
+// their join (2 to 3 us) take the most of.  Probabilities are rounded to 16 bits for the product, as the
+// matrix instructions take them, their sums are not: with the one rounding of the result the error against
+// 64 bits is up to 1.04 times that of the one rounding alone.
 
 constexpr uint64_t kCounterBytes = kMaxSplitCtas * 4;  // at the workspace's start
 constexpr int kRowsMax = 16;
@@ -701,6 +703,10 @@ extern "C" int preba_pages_attend(const preba_pages_attend_t* req, void* stream)
   if (!p.workspace || (reinterpret_cast<uintptr_t>(p.workspace) & 15)) return PREBA_ERR_INVALID_ARG;
   const uint32_t group = p.heads_q / p.heads_kv;
   if (p.workspace_bytes < workspace_of(p.n, p.tokens, group, p.head_dim)) return PREBA_ERR_BUFFER_TOO_SMALL;
+  // One 16-row fragment holds the rows of a key head, or the other kernel takes them.  64 requests of up to 8192
+  // keys of 8 heads of 128 (floor by bytes 133 us), rows on a key head: 4 and 8: 144 us here, 177 there; 16: 149
+  // and 183; 17 to 128 there only, 178 to 213.  4 requests of up to 2048 keys, 8 rows: 13.5 and 20.2, 16: 17.3
+  // and 20.1.  The longest request of a step decides, so that one chunk takes its single tokens along.
   const bool few = static_cast<uint64_t>(group) * p.max_q <= kRowsMax;
   // claims of the kernel for many rows are numbered in 32 bits
   if (!few && pairs_at_most(p.n, p.tokens, group) * p.heads_kv > INT32_MAX) return PREBA_ERR_INVALID_ARG;

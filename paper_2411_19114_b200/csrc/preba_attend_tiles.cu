@@ -19,10 +19,16 @@
 // decided on the device, as the lengths are there: by a planning kernel, or, where there are too few pairs
 // to be claimed, by every CTA for its own run.
 //
-// Bound by the softmax, closely followed by the products: a pair of row tiles and 128 keys takes 2048 clocks of
-// the tensor pipe and 2048 of MUFU, and about 3050 altogether.  4 prompts of up to 4096 tokens, 32 query
-// heads of 128: 324 us at 1.9 GHz, 371 us at the 1.6 GHz that the GPU holds (1.20 and 1.05 PFLOP/s); 512 tokens
-// over 30000 keys: 211 and 241 us; a step of 9 chunks and 28 single tokens with a window of 1000: 40 us.
+// P is rounded to 16 bits because the matrix instructions take it so; its row sums are not.  With the one
+// rounding of the result the error against 64 bits is 1.3 to 1.4 times that of the one rounding alone.
+//
+// Bound by the chain of a row tile, not by a unit: a pair of row tiles and 128 keys takes 2048 clocks of the
+// tensor pipe and 2048 of MUFU and 3050 altogether, because a tile's softmax (1845 clocks of its threads), the
+// second half of P V (256), Q K^T of the next keys (512) and the hand-overs between them follow one another; the
+// softmax of both tiles without products takes 2480.  4 prompts of up to 4096 tokens, 32 query heads of 128:
+// 325 us at the full clock, 372 to 381 at the 1.57 GHz that the GPU holds under it (1.20 and 1.03 PFLOP/s);
+// 512 tokens over 30000 keys: 211 us, and 245 to 250 at 1.47 GHz; a step of 9 chunks and 28 single tokens with
+// a window of 1000: 40 to 42 us.
 #include <algorithm>
 
 #include <type_traits>
@@ -590,14 +596,14 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
     if (warp == kCopyWarp) {
       // ---- work and copies
       tiles_head plan;
-    run_t run;  // means something only if the run has a key tile
-    if (a.own_plan) {
-      plan = {0, 0, own.units, 0, own.per};
-      run = own.run;
-    } else {
-      plan = *a.head;
-      run = a.runs[blockIdx.x];
-    }
+      run_t run;  // means something only if the run has a key tile
+      if (a.own_plan) {
+        plan = {0, 0, own.units, 0, own.per};
+        run = own.run;
+      } else {
+        plan = *a.head;
+        run = a.runs[blockIdx.x];
+      }
       const uint32_t boxes = kTile >> a.box_shift;
       const uint32_t chunk = lane & (boxes - 1), half = lane / boxes;
       const bool mine = half < L::kHalves;

@@ -24,7 +24,7 @@ __device__ __forceinline__ void report(int32_t* status, int32_t code) {
 // sums only.  A step has hundreds of requests and up to hundreds of thousands of tokens, so every CTA
 // adds the lengths up for itself (they come from L2 after the first) instead of waiting for
 // another to do it: one launch, no flag between CTAs.  Bound by latency: two loads, a sum over the block, a
-// search, two loads, a store.  4.7 us a call for 64 single tokens, 6.2 us for 145 K tokens of 1500 requests
+// search, two loads, a store.  4.0 us a call for 64 single tokens, 6.0 us for 145 K tokens of 1500 requests
 // (1.2 MB) in a sequence of calls.
 
 constexpr int kPlanThreads = 512;
@@ -204,7 +204,7 @@ plan_kernel(const preba_pages_plan_t p, const uint32_t page_shift) {
 // Requests are independent, so no sum crosses them: a warp takes a run of consecutive rows, adds up
 // the spans of the requests it meets 32 at a time, and writes the rows of every span that lie in
 // its run.  No shared memory, no limit on spans or requests.  Bound by latency (the search, the lengths, the
-// spans, the store): 4.2 us a call for 76 K rows of prompts with images, 3.1 us for 256 single tokens.
+// spans, the store): 4.1 us a call for 76 K rows of prompts with images, 3.1 us for 256 single tokens.
 
 constexpr int kPosThreads = 128;
 constexpr uint32_t kPosMaxTokens = 1u << 24;  // of one span
@@ -347,8 +347,8 @@ positions_kernel(const preba_rope_positions_t p, const uint32_t run) {
 // A CTA takes a few tokens: it works out their cosines and sines once (one per pair, in 64 bits up to
 // the reduced angle; all heads of a token share them) and then moves the heads, eight pairs or sixteen
 // copied elements to a thread, in 16-byte loads and stores.  Where there are few tokens, several CTAs share
-// one and each takes a part of its heads, so that no thread moves more than one job.  Bound by bytes: 54.4 us
-// for 16 K rows of 32 + 8 + 8 heads of 128 (327 MB, 6.0 TB/s), 5.5 us for 20 MB, 3.5 us for 32 rows.
+// one and each takes a part of its heads, so that no thread moves more than one job.  Bound by bytes: 54 to
+// 57 us for 16 K rows of 32 + 8 + 8 heads of 128 (327 MB, 5.8 TB/s), 5.6 us for 20 MB, 3.3 us for 32 rows.
 
 constexpr int kRopeThreads = 256;
 constexpr uint32_t kRopeTokens = 4;
