@@ -53,7 +53,9 @@ EXPORTS = ("preba_query", "preba_pack", "preba_preprocess", "preba_preprocess_ex
            "preba_audio_layout", "preba_audio_resample_query", "preba_audio_resample",
            "preba_jpeg_query", "preba_jpeg_decode",
            "preba_pages_plan", "preba_rope_positions", "preba_rope_append",
-           "preba_pages_attend_query", "preba_pages_attend")
+           "preba_pages_attend_query", "preba_pages_attend",
+           "preba_beam_select_query", "preba_beam_select", "preba_beam_pages_query", "preba_beam_pages",
+           "preba_pages_copy")
 
 
 class PrebaImg(ctypes.Structure):
@@ -188,6 +190,34 @@ class PrebaPagesAttend(ctypes.Structure):
         ("reserved", ctypes.c_uint32)]
 
 
+class PrebaBeamSelect(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_void_p) for f in (
+        "logits", "scores", "done", "allowed", "weights", "tokens", "parents", "scores_out", "done_out",
+        "workspace")] + [
+        ("workspace_bytes", ctypes.c_uint64), ("status", ctypes.c_void_p),
+        ("row_stride", ctypes.c_uint64), ("allowed_stride", ctypes.c_uint64)] + [
+        (f, ctypes.c_uint32) for f in ("n", "beams", "width", "vocab")] + [
+        ("end_token", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class PrebaBeamPages(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_void_p) for f in (
+        "parents", "lengths", "kept", "table", "table_out", "lengths_out", "copies", "free_pages",
+        "free_count", "free_left", "status", "workspace")] + [
+        ("workspace_bytes", ctypes.c_uint64), ("table_stride", ctypes.c_uint64),
+        ("table_out_stride", ctypes.c_uint64)] + [
+        (f, ctypes.c_uint32) for f in (
+            "table_width", "free_capacity", "n", "beams", "page_size", "pages")]
+
+
+class PrebaPagesCopy(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_void_p) for f in ("copies", "k_caches", "v_caches", "status")] + [
+        ("cache_stride", ctypes.c_uint64 * 3)] + [
+        (f, ctypes.c_uint32) for f in (
+            "rows", "layers", "heads_kv", "head_dim", "pages", "page_size")] + [
+        ("dtype", ctypes.c_int32), ("reserved", ctypes.c_uint32)]
+
+
 UTT_DTYPE = np.dtype([("offset", "<u8"), ("length", "<u4"), ("frames", "<u4")])
 AUDIO_MELS = 80
 TABLE_DTYPE = np.dtype([("offset", "<u8"), ("h", "<u4"), ("w", "<u4")])
@@ -295,7 +325,14 @@ def lib() -> ctypes.CDLL:
         L.preba_jpeg_decode.restype = ctypes.c_int
         L.preba_pages_attend_query.argtypes = [ctypes.c_uint32] * 5 + [u64p]
         L.preba_pages_attend_query.restype = ctypes.c_int
-        for name, struct in (("preba_pages_plan", PrebaPagesPlan),
+        L.preba_beam_select_query.argtypes = [ctypes.c_uint32] * 4 + [ctypes.c_int32, u64p]
+        L.preba_beam_select_query.restype = ctypes.c_int
+        L.preba_beam_pages_query.argtypes = [ctypes.c_uint32] * 3 + [u64p]
+        L.preba_beam_pages_query.restype = ctypes.c_int
+        for name, struct in (("preba_beam_select", PrebaBeamSelect),
+                             ("preba_beam_pages", PrebaBeamPages),
+                             ("preba_pages_copy", PrebaPagesCopy),
+                             ("preba_pages_plan", PrebaPagesPlan),
                              ("preba_rope_positions", PrebaRopePositions),
                              ("preba_rope_append", PrebaRopeAppend),
                              ("preba_pages_attend", PrebaPagesAttend)):
@@ -1248,3 +1285,187 @@ class PreparedPagesAttend(_Prepared):
 def preba_pages_attend(*args, **kwargs) -> None:
     """One ``preba_pages_attend`` call; the arguments are those of ``PreparedPagesAttend``."""
     PreparedPagesAttend(*args, **kwargs)()
+
+
+# ---- beam search: selection, block tables of the beams, copies of open pages -----------------------
+
+BEAMS_MAX, BEAMS_MAX_WIDTH, BEAMS_MAX_VOCAB = 32, 64, 1 << 20
+COPY_MAX_LAYERS = 128
+
+
+def _dense(t, name: str, dtype, shape):
+    """A contiguous CUDA tensor of one type and shape."""
+    if t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} CUDA tensor")
+    _same(name, t.shape, shape)
+    return t
+
+
+def _workspace(t):
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError("workspace must be a contiguous CUDA tensor")
+    return t
+
+
+def _logits_code(dtype) -> int:
+    import torch
+
+    code = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}.get(dtype)
+    if code is None:
+        raise ValueError("logits must be float32, float16 or bfloat16")
+    return code
+
+
+def preba_beam_select_query(n: int, beams: int, width: int, vocab: int, dtype) -> int:
+    """Bytes of workspace that ``preba_beam_select`` needs at these sizes (``dtype``: the logits')."""
+    out = ctypes.c_uint64()
+    rc = lib().preba_beam_select_query(n, beams, width, vocab, _logits_code(dtype), ctypes.byref(out))
+    if rc != OK:
+        raise PrebaError(rc, "preba_beam_select_query")
+    return int(out.value)
+
+
+class PreparedBeamSelect(_Prepared):
+    """``preba_beam_select``, marshalled once.  ``logits`` [n * beams, vocab] with any row stride,
+    ``scores`` and ``weights`` (or None) float32 [n * beams], ``done`` (or None) uint8 or bool
+    [n * beams], ``allowed`` (or None) int32 or uint32 [n * beams or 1, ceil(vocab / 32)], ``tokens``
+    and ``parents`` int32, ``scores_out`` float32 and ``done_out`` (or None) uint8 or bool, all
+    [n, width], ``workspace`` a CUDA tensor of ``preba_beam_select_query`` bytes."""
+
+    def __init__(self, logits, scores, tokens, parents, scores_out, workspace, end_token: int = -1,
+                 done=None, done_out=None, allowed=None, weights=None, status=None, stream=None):
+        import torch
+
+        code = _logits_code(logits.dtype)
+        if logits.dim() != 2 or not logits.is_cuda or (logits.shape[1] > 1 and logits.stride(1) != 1):
+            raise ValueError("logits must be a CUDA tensor with 2 dimensions, the last contiguous")
+        rows, vocab = logits.shape
+        if logits.stride(0) < 0:
+            raise ValueError("logits has a negative stride")
+        if tokens.dim() != 2 or tokens.shape[0] == 0 or rows % tokens.shape[0]:
+            raise ValueError("tokens must be [n, width], and logits must have a multiple of n rows")
+        n, width = tokens.shape
+        _dense(scores, "scores", torch.float32, (rows,))
+        _dense(tokens, "tokens", torch.int32, (n, width))
+        _dense(parents, "parents", torch.int32, (n, width))
+        _dense(scores_out, "scores_out", torch.float32, (n, width))
+        if weights is not None:
+            _dense(weights, "weights", torch.float32, (rows,))
+        for t, name, want in ((done, "done", (rows,)), (done_out, "done_out", (n, width))):
+            if t is not None:
+                _dense(t, name, torch.bool if t.dtype == torch.bool else torch.uint8, want)
+        s = PrebaBeamSelect()
+        if allowed is not None:
+            if (allowed.dtype not in (torch.int32, torch.uint32) or allowed.dim() != 2 or not allowed.is_cuda
+                    or (allowed.shape[1] > 1 and allowed.stride(1) != 1) or allowed.stride(0) < 0):
+                raise ValueError("allowed must be an int32 CUDA tensor with 2 dimensions, the last contiguous")
+            _same("allowed", allowed.shape, (rows if allowed.shape[0] != 1 else 1, -(-vocab // 32)))
+            s.allowed_stride = allowed.stride(0) if allowed.shape[0] > 1 else 0
+        s.logits, s.scores, s.done, s.allowed = _ptr(logits), _ptr(scores), _ptr(done), _ptr(allowed)
+        s.weights, s.tokens, s.parents = _ptr(weights), _ptr(tokens), _ptr(parents)
+        s.scores_out, s.done_out, s.workspace = _ptr(scores_out), _ptr(done_out), _ptr(_workspace(workspace))
+        s.workspace_bytes = workspace.numel() * workspace.element_size()
+        s.status, s.row_stride = _ptr(_status(status)), _row_stride(logits)
+        s.n, s.beams, s.width, s.vocab = n, rows // n, width, vocab
+        s.end_token, s.dtype = end_token, code
+        self._bind("preba_beam_select", s, stream,
+                   (logits, scores, done, allowed, weights, tokens, parents, scores_out, done_out, workspace,
+                    status))
+
+
+def preba_beam_select(*args, **kwargs) -> None:
+    """One ``preba_beam_select`` call; the arguments are those of ``PreparedBeamSelect``."""
+    PreparedBeamSelect(*args, **kwargs)()
+
+
+def preba_beam_pages_query(n: int, beams: int, table_width: int) -> int:
+    """Bytes of workspace that ``preba_beam_pages`` needs at these sizes."""
+    out = ctypes.c_uint64()
+    rc = lib().preba_beam_pages_query(n, beams, table_width, ctypes.byref(out))
+    if rc != OK:
+        raise PrebaError(rc, "preba_beam_pages_query")
+    return int(out.value)
+
+
+class PreparedBeamPages(_Prepared):
+    """``preba_beam_pages``, marshalled once.  All but the workspace are int32 CUDA tensors:
+    ``parents``, ``lengths`` and ``lengths_out`` [n * beams], ``table`` and ``table_out`` [n * beams,
+    width], ``copies`` [n * beams, 4], ``free_pages`` (the stack), ``free_count`` and ``free_left`` [1],
+    ``kept`` [n] or None; ``workspace`` a CUDA tensor of ``preba_beam_pages_query`` bytes.  ``parents`` may
+    also be [n, beams], as ``preba_beam_select`` writes them.  ``pages`` is the cache's page count (None:
+    whatever 31-bit slots can name)."""
+
+    def __init__(self, parents, lengths, table, table_out, lengths_out, copies, free_pages, free_count,
+                 free_left, page_size: int, workspace, beams: int, pages: int | None = None, kept=None,
+                 status=None, stream=None):
+        import torch
+
+        rows, width = _ints(table, "table", 2).shape
+        if beams < 1 or rows % beams:
+            raise ValueError("table must have a row for every beam of every request")
+        _same("table_out", _ints(table_out, "table_out", 2).shape, (rows, width))
+        if parents.dim() == 2:
+            _dense(parents, "parents", torch.int32, (rows // beams, beams))
+        else:
+            _same("parents", _ints(parents, "parents").shape, (rows,))
+        for t, name, want in ((lengths, "lengths", rows), (lengths_out, "lengths_out", rows),
+                              (free_count, "free_count", 1), (free_left, "free_left", 1)):
+            _same(name, _ints(t, name).shape, (want,))
+        _dense(copies, "copies", torch.int32, (rows, 4))
+        _ints(free_pages, "free_pages")
+        if kept is not None:
+            _same("kept", _ints(kept, "kept").shape, (rows // beams,))
+        if min(table.stride(0), table_out.stride(0)) < 0:
+            raise ValueError("table has a negative stride")
+        s = PrebaBeamPages()
+        s.parents, s.lengths, s.kept, s.table = _ptr(parents), _ptr(lengths), _ptr(kept), _ptr(table)
+        s.table_out, s.lengths_out, s.copies = _ptr(table_out), _ptr(lengths_out), _ptr(copies)
+        s.free_pages, s.free_count, s.free_left = _ptr(free_pages), _ptr(free_count), _ptr(free_left)
+        s.status, s.workspace = _ptr(_status(status)), _ptr(_workspace(workspace))
+        s.workspace_bytes = workspace.numel() * workspace.element_size()
+        s.table_stride, s.table_out_stride, s.table_width = _row_stride(table), _row_stride(table_out), width
+        s.free_capacity, s.n, s.beams, s.page_size = free_pages.numel(), rows // beams, beams, page_size
+        s.pages = (2**31 - 1) // max(1, page_size) if pages is None else pages
+        self._bind("preba_beam_pages", s, stream,
+                   (parents, lengths, kept, table, table_out, lengths_out, copies, free_pages, free_count,
+                    free_left, workspace, status))
+
+
+def preba_beam_pages(*args, **kwargs) -> None:
+    """One ``preba_beam_pages`` call; the arguments are those of ``PreparedBeamPages``."""
+    PreparedBeamPages(*args, **kwargs)()
+
+
+class PreparedPagesCopy(_Prepared):
+    """``preba_pages_copy``, marshalled once.  ``copies`` int32 [rows, 4] as ``preba_beam_pages`` writes
+    them, ``k_caches`` and ``v_caches`` lists of a cache per layer, all [pages, page_size, heads_kv, d]
+    with the same strides over a contiguous last dimension."""
+
+    def __init__(self, copies, k_caches, v_caches, status=None, stream=None):
+        import torch
+
+        caches = [*k_caches, *v_caches]
+        if len(k_caches) != len(v_caches) or not caches:
+            raise ValueError("k_caches and v_caches must have a cache for every layer")
+        _dense(copies, "copies", torch.int32, (copies.shape[0], 4))
+        for c in caches:
+            _heads(c, "cache", 4, caches[0].dtype)
+            _same("cache", c.shape, caches[0].shape)
+            if _strides(c, 3) != _strides(caches[0], 3):
+                raise ValueError("all caches must have the same strides")
+        s = PrebaPagesCopy()
+        layers = len(k_caches)
+        pointers = [(ctypes.c_void_p * layers)(*[c.data_ptr() for c in part]) for part in (k_caches, v_caches)]
+        s.copies, s.status = _ptr(copies), _ptr(_status(status))
+        s.k_caches, s.v_caches = (ctypes.cast(x, ctypes.c_void_p) for x in pointers)
+        s.cache_stride[:] = _strides(caches[0], 3)
+        s.rows, s.layers = copies.shape[0], layers
+        s.pages, s.page_size, s.heads_kv, s.head_dim = caches[0].shape
+        s.dtype = _code(caches[0])
+        self._pointers = pointers
+        self._bind("preba_pages_copy", s, stream, (copies, *caches, status))
+
+
+def preba_pages_copy(*args, **kwargs) -> None:
+    """One ``preba_pages_copy`` call; the arguments are those of ``PreparedPagesCopy``."""
+    PreparedPagesCopy(*args, **kwargs)()
