@@ -31,6 +31,64 @@ extern "C" {
 #define PREBA_COPY_MAX_LAYERS 128u
 
 /*
+ * preba_cross_attend — attention of the decoder's rows to the states of an encoder, which lie packed
+ * one request after the other and belong to all rows of theirs: request r owns rows cu_q[r] .. cu_q[r+1]-1 (its
+ * beams' single tokens, or a whole prompt) and states cu_k[r] .. cu_k[r+1]-1.  Row i sees the first seen[i]
+ * states of its request, all of them without `seen` (a row of a prompt with images sees those of the images before
+ * it, a row of a stream what has arrived).  Per query head h, with the key head h / (heads_q / heads_kv):
+ *   out = sum_k p_k v_k / sum_k p_k,   p_k = exp(scale q.k_k - m),   m = max_k scale q.k_k
+ *   lse = m + ln sum_k p_k
+ * A row that sees no state is 0, its lse -inf; so is one whose scores are all -inf.  A row with a score that is not a
+ * number is not a number, nor is its lse.  Products and sums are fp32; p is rounded to the type of the states for the product
+ * with v, as the matrix instructions take it, and out is rounded once.  States that no row of the request sees may
+ * hold anything, infinities and NaN included; a state that is not finite and that some row sees may show
+ * in other rows of its request.  Rows behind cu_q[n] are not written.  Results do not depend on timing.
+ *   preba_cross_attend_query  bytes of workspace that a call with these sizes needs (host only);
+ *                             the caller zeroes the workspace once, every call leaves its counters
+ *                             zeroed again; calls that may overlap on the device need one each.
+ * A request is skipped (its rows are not written) and PREBA_ERR_BAD_TABLE stored if its rows or states are out of range or
+ * its rows more than max_q.
+ * Every wait of the kernels has a limit.  If one runs out, PREBA_ERR_TIMEOUT is stored and the rows that the
+ * call would have written hold anything; nothing else does, and the workspace is left as by any call.
+ * Errors: PREBA_ERR_INVALID_ARG (NULL, sizes of 0, n above PREBA_PAGES_MAX_REQUESTS, tokens or states above
+ * PREBA_PAGES_MAX_KEYS, a base that is not 16-byte aligned, a stride that is not a multiple of 8, heads_q not a multiple of
+ * heads_kv, heads_q above 65535, more than 128 query heads on one key head, head_dim not a multiple of 8 in
+ * 8 .. PREBA_PAGES_MAX_HEAD_DIM, a stride of 0 on an axis of q, k or v that has more than one entry, so many states that
+ * heads_kv * (n + states / 128) passes 2e9, or so many rows that heads_kv * (n + tokens / (2 * g)) passes 2^31 - 1, where
+ * g = 128 * heads_kv / heads_q rounded down), PREBA_ERR_BUFFER_TOO_SMALL (workspace), PREBA_ERR_CUDA.
+ */
+typedef struct {
+  const void* q;              /* DEVICE, [tokens, heads_q, head_dim] */
+  const void* k;              /* DEVICE, [states, heads_kv, head_dim] */
+  const void* v;              /* DEVICE, likewise */
+  const int32_t* cu_q;        /* DEVICE, n + 1 */
+  const int32_t* cu_k;        /* DEVICE, n + 1 */
+  const int32_t* seen;        /* DEVICE, tokens, or NULL */
+  void* out;                  /* DEVICE, [tokens, heads_q, head_dim] */
+  float* lse;                 /* DEVICE, [tokens, heads_q] contiguous, or NULL */
+  void* workspace;            /* DEVICE, 16-byte aligned */
+  uint64_t workspace_bytes;
+  int32_t* status;            /* DEVICE word or NULL */
+  uint64_t q_stride[2];       /* token, head */
+  uint64_t out_stride[2];
+  uint64_t k_stride[2];       /* state, head */
+  uint64_t v_stride[2];
+  uint32_t n;
+  uint32_t tokens;
+  uint32_t states;
+  uint32_t max_q;             /* no request has more rows than this */
+  uint32_t heads_q;
+  uint32_t heads_kv;
+  uint32_t head_dim;
+  int32_t dtype;              /* PREBA_F16 or PREBA_BF16: q, k, v and out */
+  float scale;
+  uint32_t reserved;
+} preba_cross_attend_t;
+int preba_cross_attend_query(uint32_t n, uint32_t tokens, uint32_t heads_q, uint32_t heads_kv,
+                             uint32_t head_dim, uint64_t* workspace_bytes);
+int preba_cross_attend(const preba_cross_attend_t* req, void* stream);
+
+/*
  * preba_beam_select — the best `width` continuations of every request over its beams and the vocabulary.
  * Row i = r * beams + b offers every token v that `allowed` leaves it, at
  *   value = scores[i] + x_v - ln sum_u exp x_u   (u over the allowed tokens),   rank = weights[i] * value,

@@ -55,7 +55,7 @@ EXPORTS = ("preba_query", "preba_pack", "preba_preprocess", "preba_preprocess_ex
            "preba_pages_plan", "preba_rope_positions", "preba_rope_append",
            "preba_pages_attend_query", "preba_pages_attend",
            "preba_beam_select_query", "preba_beam_select", "preba_beam_pages_query", "preba_beam_pages",
-           "preba_pages_copy")
+           "preba_pages_copy", "preba_cross_attend_query", "preba_cross_attend")
 
 
 class PrebaImg(ctypes.Structure):
@@ -188,6 +188,16 @@ class PrebaPagesAttend(ctypes.Structure):
             "page_size", "window")] + [
         ("dtype", ctypes.c_int32), ("flags", ctypes.c_uint32), ("scale", ctypes.c_float),
         ("reserved", ctypes.c_uint32)]
+
+
+class PrebaCrossAttend(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_void_p) for f in (
+        "q", "k", "v", "cu_q", "cu_k", "seen", "out", "lse", "workspace")] + [
+        ("workspace_bytes", ctypes.c_uint64), ("status", ctypes.c_void_p)] + [
+        (f, ctypes.c_uint64 * 2) for f in ("q_stride", "out_stride", "k_stride", "v_stride")] + [
+        (f, ctypes.c_uint32) for f in (
+            "n", "tokens", "states", "max_q", "heads_q", "heads_kv", "head_dim")] + [
+        ("dtype", ctypes.c_int32), ("scale", ctypes.c_float), ("reserved", ctypes.c_uint32)]
 
 
 class PrebaBeamSelect(ctypes.Structure):
@@ -329,7 +339,10 @@ def lib() -> ctypes.CDLL:
         L.preba_beam_select_query.restype = ctypes.c_int
         L.preba_beam_pages_query.argtypes = [ctypes.c_uint32] * 3 + [u64p]
         L.preba_beam_pages_query.restype = ctypes.c_int
-        for name, struct in (("preba_beam_select", PrebaBeamSelect),
+        L.preba_cross_attend_query.argtypes = [ctypes.c_uint32] * 5 + [u64p]
+        L.preba_cross_attend_query.restype = ctypes.c_int
+        for name, struct in (("preba_cross_attend", PrebaCrossAttend),
+                             ("preba_beam_select", PrebaBeamSelect),
                              ("preba_beam_pages", PrebaBeamPages),
                              ("preba_pages_copy", PrebaPagesCopy),
                              ("preba_pages_plan", PrebaPagesPlan),
@@ -1287,7 +1300,7 @@ def preba_pages_attend(*args, **kwargs) -> None:
     PreparedPagesAttend(*args, **kwargs)()
 
 
-# ---- beam search: selection, block tables of the beams, copies of open pages -----------------------
+# ---- beam search: attention to an encoder's states, selection, block tables, copies of open pages ---
 
 BEAMS_MAX, BEAMS_MAX_WIDTH, BEAMS_MAX_VOCAB = 32, 64, 1 << 20
 COPY_MAX_LAYERS = 128
@@ -1305,6 +1318,57 @@ def _workspace(t):
     if not t.is_cuda or not t.is_contiguous():
         raise ValueError("workspace must be a contiguous CUDA tensor")
     return t
+
+
+def preba_cross_attend_query(n: int, tokens: int, heads_q: int, heads_kv: int, head_dim: int) -> int:
+    """Bytes of workspace that ``preba_cross_attend`` needs at these sizes (zeroed once)."""
+    out = ctypes.c_uint64()
+    rc = lib().preba_cross_attend_query(n, tokens, heads_q, heads_kv, head_dim, ctypes.byref(out))
+    if rc != OK:
+        raise PrebaError(rc, "preba_cross_attend_query")
+    return int(out.value)
+
+
+class PreparedCrossAttend(_Prepared):
+    """``preba_cross_attend``, marshalled once.  ``q``, ``out`` [tokens, heads_q, d], ``k``, ``v`` [states,
+    heads_kv, d] (views of one projection's output will do), ``cu_q`` and ``cu_k`` int32 [n + 1], ``seen``
+    int32 [tokens] or None, ``workspace`` a zeroed CUDA tensor of ``preba_cross_attend_query`` bytes,
+    ``lse`` float32 [tokens, heads_q] or None."""
+
+    def __init__(self, q, k, v, cu_q, cu_k, out, workspace, max_q: int, scale: float, seen=None, lse=None,
+                 status=None, stream=None):
+        import torch
+
+        _heads(q, "q", 3)
+        tokens, hq, d = q.shape
+        _heads(out, "out", 3, q.dtype), _heads(k, "k", 3, q.dtype), _heads(v, "v", 3, q.dtype)
+        _same("out", out.shape, q.shape)
+        _same("k", k.shape[2:], (d,))
+        _same("v", v.shape, k.shape)
+        n = cu_q.numel() - 1
+        _ints(cu_q, "cu_q")
+        _same("cu_k", _ints(cu_k, "cu_k").shape, (n + 1,))
+        if seen is not None:
+            _same("seen", _ints(seen, "seen").shape, (tokens,))
+        if lse is not None:
+            _dense(lse, "lse", torch.float32, (tokens, hq))
+        s = PrebaCrossAttend()
+        s.q, s.k, s.v, s.out = _ptr(q), _ptr(k), _ptr(v), _ptr(out)
+        s.cu_q, s.cu_k, s.seen, s.lse = _ptr(cu_q), _ptr(cu_k), _ptr(seen), _ptr(lse)
+        s.workspace, s.status = _ptr(_workspace(workspace)), _ptr(_status(status))
+        s.workspace_bytes = workspace.numel() * workspace.element_size()
+        s.q_stride[:], s.out_stride[:] = _strides(q, 2), _strides(out, 2)
+        s.k_stride[:], s.v_stride[:] = _strides(k, 2), _strides(v, 2)
+        s.n, s.tokens, s.states, s.max_q = n, tokens, k.shape[0], max_q
+        s.heads_q, s.heads_kv, s.head_dim = hq, k.shape[1], d
+        s.dtype, s.scale = _code(q), scale
+        self._bind("preba_cross_attend", s, stream,
+                   (q, k, v, cu_q, cu_k, seen, out, lse, workspace, status))
+
+
+def preba_cross_attend(*args, **kwargs) -> None:
+    """One ``preba_cross_attend`` call; the arguments are those of ``PreparedCrossAttend``."""
+    PreparedCrossAttend(*args, **kwargs)()
 
 
 def _logits_code(dtype) -> int:

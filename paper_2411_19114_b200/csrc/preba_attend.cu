@@ -561,12 +561,6 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant
   }
 }
 
-int finish(cudaError_t err) {
-  if (err == cudaSuccess) return PREBA_OK;
-  g_last_cuda_error = static_cast<int>(err);
-  return PREBA_ERR_CUDA;
-}
-
 bool sizes_ok(uint32_t n, uint32_t tokens, uint32_t heads_q, uint32_t heads_kv, uint32_t head_dim) {
   return n >= 1 && n <= PREBA_PAGES_MAX_REQUESTS && tokens >= 1 && tokens <= PREBA_PAGES_MAX_KEYS && heads_q >= 1 &&
          heads_q <= 65535 && heads_kv >= 1 && heads_q % heads_kv == 0 && heads_q / heads_kv <= 128 &&
@@ -605,6 +599,12 @@ cudaError_t encoder(encode_fn* fn) {
 
 namespace attend {
 
+int finish(cudaError_t err) {
+  if (err == cudaSuccess) return PREBA_OK;
+  g_last_cuda_error = static_cast<int>(err);
+  return PREBA_ERR_CUDA;
+}
+
 cudaError_t tensor_map(CUtensorMap* map, int dtype, const void* base, const uint64_t* dims,
                        const uint64_t* strides, const uint32_t* box) {
   encode_fn encode;
@@ -628,6 +628,14 @@ cudaError_t cache_map(CUtensorMap* map, const preba_pages_attend_t& p, const voi
   const uint64_t order[3] = {strides[1], strides[2], strides[0]};
   const uint32_t box[2] = {box_rows, 1};
   return tensor_map(map, p.dtype, cache, dims, order, box);
+}
+
+cudaError_t states_map(CUtensorMap* map, const preba_pages_attend_t& p, uint32_t states, const void* base,
+                       const uint64_t* strides, uint32_t box_rows) {
+  const uint64_t dims[4] = {p.head_dim, states, p.heads_kv, 1};
+  const uint64_t order[3] = {strides[1], strides[2], 0};
+  const uint32_t box[2] = {box_rows, 1};
+  return tensor_map(map, p.dtype, base, dims, order, box);
 }
 
 }  // namespace attend
@@ -688,6 +696,7 @@ preba::attend::wait_limits_t preba::attend::wait_limits() { return {g_checked_wa
 
 extern "C" int preba_pages_attend(const preba_pages_attend_t* req, void* stream) {
   using namespace preba;
+  using attend::finish;
   if (!req) return PREBA_ERR_INVALID_ARG;
   const preba_pages_attend_t& p = *req;
   if (!sizes_ok(p.n, p.tokens, p.heads_q, p.heads_kv, p.head_dim) || !operand_ok(p.q, p.q_stride, 2) ||

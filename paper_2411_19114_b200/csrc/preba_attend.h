@@ -1,4 +1,4 @@
-// Shared by the two attention kernels (preba_attend.cu): requests, barriers, tensor copies.
+// Shared by the attention kernels (preba_attend.cu, preba_attend_tiles.cu, preba_cross.cu): requests, barriers, tensor copies.
 #ifndef PREBA_ATTEND_H_
 #define PREBA_ATTEND_H_
 
@@ -27,10 +27,20 @@ cudaError_t tensor_map(CUtensorMap* map, int dtype, const void* base, const uint
 cudaError_t cache_map(CUtensorMap* map, const preba_pages_attend_t& p, const void* cache,
                       const uint64_t* strides, uint32_t box_rows);
 
+// Packed states (preba_cross_attend): boxes of box_rows states of one head; strides of state and head are strides[1], [2].
+cudaError_t states_map(CUtensorMap* map, const preba_pages_attend_t& p, uint32_t states, const void* base,
+                       const uint64_t* strides, uint32_t box_rows);
+constexpr uint32_t kStateRows = 32;  // so that a request's last tile brings few states of the next one
+
 // The kernel for many rows (preba_attend_tiles.cu): its workspace and its launches.
 uint64_t tiles_workspace(uint32_t n, uint32_t tokens, uint32_t group, uint32_t head_dim);
 cudaError_t launch_tiles(const preba_pages_attend_t& p, uint32_t page_shift, int sms, void* workspace,
                          cudaStream_t stream);
+cudaError_t launch_packed_tiles(const preba_pages_attend_t& p, const int32_t* cu_k, const int32_t* seen, uint32_t states,
+                                int sms, void* workspace, cudaStream_t stream);
+
+// Results of host functions that launch (preba_attend.cu).
+int finish(cudaError_t err);
 
 __device__ __forceinline__ void report(int32_t* status, int32_t code) {
   if (status) atomicCAS(status, 0, code);
@@ -57,6 +67,25 @@ __device__ __forceinline__ void seen_by(const preba_pages_attend_t& p, const req
   hi = (p.flags & PREBA_ATTEND_CAUSAL) ? max(0, min(q.keys, at0 + j1)) : q.keys;
   lo = p.window ? static_cast<int32_t>(max(static_cast<int64_t>(0),
                                            static_cast<int64_t>(at0) + j0 + 1 - p.window)) : 0;
+}
+
+// The same for packed states: a request's states are cu_k[r] .. cu_k[r + 1] - 1 of `states`.
+__device__ __forceinline__ bool load_packed(const preba_pages_attend_t& p, const int32_t* cu_k, uint32_t states, uint32_t r,
+                                            request_t& q) {
+  const int32_t a = p.cu_q[r], b = p.cu_q[r + 1], c = cu_k[r], d = cu_k[r + 1];
+  q.row = a;
+  q.rows = b - a;
+  q.keys = d - c;
+  return !(a < 0 || b < a || static_cast<uint32_t>(b) > p.tokens || static_cast<uint32_t>(b - a) > p.max_q || c < 0 || d < c ||
+           static_cast<uint32_t>(d) > states);
+}
+// Rows j0 .. j1-1 of a request see its first states only, up to this many of them.
+__device__ __forceinline__ int32_t packed_seen(uint32_t tokens, const int32_t* seen, const request_t& q, int32_t j0, int32_t j1) {
+  if (!seen) return q.keys;
+  int32_t hi = 0;
+  for (int32_t j = j0; j < j1; ++j)
+    if (static_cast<uint32_t>(q.row + j) < tokens) hi = max(hi, seen[q.row + j]);
+  return min(hi, q.keys);
 }
 
 // ---- shared-memory barriers and tensor copies (PTX) ------------------------------------------

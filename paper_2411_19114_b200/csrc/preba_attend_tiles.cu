@@ -19,6 +19,9 @@
 // decided on the device, as the lengths are there: by a planning kernel, or, where there are too few pairs
 // to be claimed, by every CTA for its own run.
 //
+// The same kernels serve preba_cross_attend, whose keys are the states of an encoder and lie one after the other
+// (Packed): requests, what their rows see and the copies differ, and nothing else.
+//
 // P is rounded to 16 bits because the matrix instructions take it so; its row sums are not.  With the one
 // rounding of the result the error against 64 bits is 1.3 to 1.4 times that of the one rounding alone.
 //
@@ -35,6 +38,7 @@
 
 #include "preba_attend.h"
 #include "preba_attend_plan.h"
+#include "preba_tensor.h"
 
 namespace preba {
 namespace {
@@ -116,16 +120,37 @@ struct tiles_args {
   run_t* runs;        // one per CTA
   uint32_t* order;    // pairs, longest first
   float4* partials;   // two per CTA
+  const int32_t* cu_k;  // packed states instead of pages: first state of each request, n + 1
+  const int32_t* seen;  // and how many of them each row sees, or NULL: all
+  uint32_t states;
 #if defined(PREBA_CHECKED)
   wait_limits_t limits = wait_limits();
 #endif
 };
+
+// A request and what its rows see: keys in pages (Packed false), or states that lie one after the other.
+template <bool Packed>
+__device__ __forceinline__ bool request_of(const tiles_args& a, uint32_t r, request_t& q) {
+  if (Packed) return load_packed(a.p, a.cu_k, a.states, r, q);
+  return load_request(a.p, r, q);
+}
+template <bool Packed>
+__device__ __forceinline__ void seen_of(const tiles_args& a, const request_t& q, int32_t j0, int32_t j1, int32_t& lo,
+                                        int32_t& hi) {
+  if (Packed) {
+    lo = 0;
+    hi = packed_seen(a.p.tokens, a.seen, q, j0, j1);
+  } else {
+    seen_by(a.p, q, j0, j1, lo, hi);
+  }
+}
 
 struct pair_range {
   int32_t lo, hi;                // keys
   int32_t first[2], last[2];     // key tiles of A and B
   int32_t begin, end;            // of both
 };
+template <bool Packed>
 __device__ __forceinline__ pair_range range_of(const tiles_args& a, const request_t& q, uint32_t pair) {
   pair_range r;
   r.lo = r.hi = 0;
@@ -137,7 +162,7 @@ __device__ __forceinline__ pair_range range_of(const tiles_args& a, const reques
     r.first[x] = r.last[x] = 0;
     if (j0 >= j1) continue;  // only B
     int32_t lo, hi;
-    seen_by(a.p, q, j0, j1, lo, hi);
+    seen_of<Packed>(a, q, j0, j1, lo, hi);
     lo = min(lo, max(0, q.keys - 1));  // rows behind all keys see nothing: one empty tile
     r.first[x] = lo / kTile;
     r.last[x] = max(r.first[x] + 1, (hi + kTile - 1) / kTile);
@@ -178,6 +203,7 @@ __device__ __forceinline__ uint64_t block_exclusive(uint64_t v, uint64_t* warp_s
   return before + incl - v;
 }
 
+template <bool Packed>
 __global__ void __launch_bounds__(kPlanThreads) tiles_plan_kernel(const tiles_args a) {
   extern __shared__ __align__(16) uint8_t plan_smem[];
   pair_t* near = reinterpret_cast<pair_t*>(plan_smem);  // the first kPlanThreads pairs
@@ -193,7 +219,7 @@ __global__ void __launch_bounds__(kPlanThreads) tiles_plan_kernel(const tiles_ar
   const uint32_t r0 = min(threadIdx.x * each, p.n), r1 = min(r0 + each, p.n);
   auto pairs_of = [&](uint32_t r) -> uint32_t {
     request_t q;
-    if (!load_request(p, r, q)) {
+    if (!request_of<Packed>(a, r, q)) {
       report(p.status, PREBA_ERR_BAD_TABLE);
       return 0;
     }
@@ -224,8 +250,8 @@ __global__ void __launch_bounds__(kPlanThreads) tiles_plan_kernel(const tiles_ar
         if (pairs_before[mid] <= i) lo = mid; else hi = mid;
       }
       r = lo;
-      load_request(p, r, q);
-      const pair_range range = range_of(a, q, i - pairs_before[r]);
+      request_of<Packed>(a, r, q);
+      const pair_range range = range_of<Packed>(a, q, i - pairs_before[r]);
       tiles = range.end - range.begin;
     }
     uint64_t sum;
@@ -313,11 +339,12 @@ __device__ __forceinline__ uint32_t cta_exclusive(uint32_t v, uint32_t* sums, ui
   return __reduce_add_sync(kFull, lane < warp ? of_warp : 0) + incl - v;
 }
 
+template <bool Packed>
 __device__ __forceinline__ void plan_own(const tiles_args& a, own_plan_t& plan) {
   const preba_pages_attend_t& p = a.p;
   auto pairs_of = [&](uint32_t r) -> uint32_t {
     request_t q;
-    if (!load_request(p, r, q)) {
+    if (!request_of<Packed>(a, r, q)) {
       if (blockIdx.x == 0) report(p.status, PREBA_ERR_BAD_TABLE);
       return 0;
     }
@@ -352,8 +379,8 @@ __device__ __forceinline__ void plan_own(const tiles_args& a, own_plan_t& plan) 
       if (plan.pairs_before[mid] <= i) lo = mid; else hi = mid;
     }
     request_t q;
-    load_request(p, lo, q);
-    const pair_range range = range_of(a, q, i - plan.pairs_before[lo]);
+    request_of<Packed>(a, lo, q);
+    const pair_range range = range_of<Packed>(a, q, i - plan.pairs_before[lo]);
     pair[k] = {lo, i - plan.pairs_before[lo], 0, static_cast<uint32_t>(range.end - range.begin), q.row, q.rows, q.keys, 0};
     tiles += pair[k].tiles;
   }
@@ -382,50 +409,13 @@ __device__ __forceinline__ void plan_own(const tiles_args& a, own_plan_t& plan) 
   __syncthreads();
 }
 
-// ---- tensor core instructions (PTX) ---------------------------------------------------------------
+// ---- arithmetic -----------------------------------------------------------------------------------
 
-__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-
-// Shared-memory operand: rows of 128 bytes in the 128-byte swizzle, eight rows (1024 bytes) to a group.
-// `leading` is the distance between 64-element columns of an operand whose rows are its contraction
-// axis.  The low word of the descriptor; the high one is the same for all.
-__device__ __forceinline__ uint32_t operand(uint32_t addr, uint32_t leading) {
-  return (addr & 0x3ffff) >> 4 | (leading >> 4) << 16;
-}
-constexpr uint32_t kOperandHigh = (1024 >> 4) | 1u << 14 | 2u << 29;
 // fp32 accumulator, 128 rows, `columns` columns; values: the second operand's rows are contracted.
 template <typename T> __device__ __forceinline__ constexpr uint32_t shape(uint32_t columns, bool values) {
   const uint32_t kind = sizeof(T) == 2 && !std::is_same<T, __half>::value ? 1 : 0;  // bfloat16 : binary16
   return 1u << 4 | kind << 7 | kind << 10 | (values ? 1u << 16 : 0u) | (columns / 8) << 17 | (kTile / 16) << 24;
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t add) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t.reg .b64 x, y;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-      "mov.b64 x, {%1, %5};\n\tmov.b64 y, {%2, %5};\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n\t}" ::"r"(d), "r"(a), "r"(b), "r"(idesc),
-      "r"(add), "n"(kOperandHigh)
-      : "memory");
-}
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t add) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t.reg .b64 y;\n\tsetp.ne.u32 p, %4, 0;\n\tmov.b64 y, {%2, %5};\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n\t}" ::"r"(d), "r"(a), "r"(b), "r"(idesc),
-      "r"(add), "n"(kOperandHigh)
-      : "memory");
-}
-// One lane of the (converged) warp, always the same.
-__device__ __forceinline__ bool elected() {
-  uint32_t yes;
-  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
-  return yes != 0;
-}
-// Arrives at the barrier when all matrix products issued before have finished.
-__device__ __forceinline__ void mma_commit(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar)
-               : "memory");
-}
-
 // Arithmetic on two fp32 numbers at once, and a maximum of three.
 __device__ __forceinline__ uint64_t pair(float a, float b) {
   uint64_t v;
@@ -461,41 +451,6 @@ __device__ __forceinline__ float max3(uint32_t a, uint32_t b, uint32_t c) {
 __device__ __forceinline__ float max3(float a, float b, float c) {
   return max3(a, __float_as_uint(b), __float_as_uint(c));
 }
-
-#define PREBA_R8(v, i) "+r"(v[i]), "+r"(v[i + 1]), "+r"(v[i + 2]), "+r"(v[i + 3]), "+r"(v[i + 4]), \
-    "+r"(v[i + 5]), "+r"(v[i + 6]), "+r"(v[i + 7])
-#define PREBA_I8(v, i) "r"(v[i]), "r"(v[i + 1]), "r"(v[i + 2]), "r"(v[i + 3]), "r"(v[i + 4]), \
-    "r"(v[i + 5]), "r"(v[i + 6]), "r"(v[i + 7])
-#define PREBA_L32 "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24," \
-    "%25,%26,%27,%28,%29,%30,%31}"
-// 32 columns of the thread's row.  The registers hold them once tmem_loaded() has returned.
-__device__ __forceinline__ void tmem_load32(uint32_t* v, uint32_t addr) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 " PREBA_L32 ", [%32];"
-               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]),
-                 "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]),
-                 "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]),
-                 "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]),
-                 "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
-               : "r"(addr)
-               : "memory");
-}
-// Nothing that uses the 32 registers moves above it.
-__device__ __forceinline__ void tmem_loaded(uint32_t* v) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : PREBA_R8(v, 0), PREBA_R8(v, 8), PREBA_R8(v, 16), PREBA_R8(v, 24)::"memory");
-}
-__device__ __forceinline__ void tmem_store32(uint32_t addr, const uint32_t* v) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], " PREBA_L32 ";" ::PREBA_I8(v, 0), PREBA_I8(v, 8),
-               PREBA_I8(v, 16), PREBA_I8(v, 24), "r"(addr)
-               : "memory");
-}
-__device__ __forceinline__ void tmem_store16(uint32_t addr, const uint32_t* v) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::
-          PREBA_I8(v, 0), PREBA_I8(v, 8), "r"(addr)
-      : "memory");
-}
-__device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // ---- the kernel -----------------------------------------------------------------------------------
 
@@ -533,7 +488,7 @@ template <int N> struct ring {
   }
 };
 
-template <typename T, int DP>
+template <typename T, int DP, bool Packed>
 __global__ void __launch_bounds__(kThreads, 1)
 tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
              const __grid_constant__ CUtensorMap map_v, const __grid_constant__ tiles_args a) {
@@ -587,7 +542,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
   fence_after();
   const uint32_t tmem = *tmem_slot;
   own_plan_t& own = *reinterpret_cast<own_plan_t*>(smem + L::kPlan);
-  if (a.own_plan) plan_own(a, own);
+  if (a.own_plan) plan_own<Packed>(a, own);
   waits_t wait(a);
   bool ok = true;
 
@@ -629,11 +584,11 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
             while (own.pairs_before[of.request + 1] <= pair) ++of.request;  // ends: the run has a key tile left
             of.pair = pair - own.pairs_before[of.request];
             request_t q;
-            load_request(p, of.request, q);
+            request_of<Packed>(a, of.request, q);
             of.row = q.row;
             of.rows = q.rows;
             of.keys = q.keys;
-            const pair_range range = range_of(a, q, of.pair);
+            const pair_range range = range_of<Packed>(a, q, of.pair);
             of.tiles = range.end - range.begin;
           } else {
             if (!PREBA_IN_RANGE(p.status, pair < plan.n_pairs)) pair = 0;
@@ -665,7 +620,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
         const bool done = item.count == 0;
         if (!done) {
           const request_t q{of.row, of.rows, of.keys};
-          const pair_range range = range_of(a, q, of.pair);
+          const pair_range range = range_of<Packed>(a, q, of.pair);
           item.request = of.request;
           item.row = q.row;
           item.rows = q.rows;
@@ -703,17 +658,18 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
         ++q_issued;
         q_ring.step();
         // keys and values, tile by tile
-        const int32_t* row = p.block_table + static_cast<uint64_t>(item.request) * p.table_stride;
+        const int32_t* row = Packed ? nullptr : p.block_table + static_cast<uint64_t>(item.request) * p.table_stride;
+        const int32_t state0 = Packed ? a.cu_k[item.request] : 0;
         int32_t key = item.tile * kTile + (chunk << a.box_shift);
         auto wanted = [&](int32_t k) {
           return mine && k < item.hi && k + static_cast<int32_t>(a.box_rows) > item.lo;
         };
-        int32_t entry = wanted(key) ? row[key >> a.page_shift] : 0;
+        int32_t entry = !Packed && wanted(key) ? row[key >> a.page_shift] : 0;
         for (int32_t t = 0; t < item.count && ok; ++t, key += kTile) {
           int32_t page = entry;
           const bool want = wanted(key);
-          if (t + 1 < item.count) entry = wanted(key + kTile) ? row[(key + kTile) >> a.page_shift] : 0;
-          if (want && (page < 0 || static_cast<uint32_t>(page) >= p.pages)) {
+          if (!Packed && t + 1 < item.count) entry = wanted(key + kTile) ? row[(key + kTile) >> a.page_shift] : 0;
+          if (!Packed && want && (page < 0 || static_cast<uint32_t>(page) >= p.pages)) {
             report(p.status, PREBA_ERR_BAD_TABLE);
             page = p.pages;  // beyond the tensor: the box is filled with zeros
           }
@@ -726,7 +682,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
             __syncwarp();
             if (want)
               tensor_copy(base + L::kRing + kv.slot * L::kSlot + dst, v ? &map_v : &map_k, half * 64,
-                          key & (p.page_size - 1), item.head, page, kv_full + 8 * kv.slot);
+                          Packed ? state0 + key : key & (p.page_size - 1), item.head, page, kv_full + 8 * kv.slot);
             ++issued;
             kv.step();
           }
@@ -892,10 +848,15 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
       const bool live = j < tokens;
       request_t q{item.row, item.rows, item.keys};
       int32_t row_lo = 0, row_hi = 0, low, high;
-      if (live) seen_by(p, q, token + j, token + j + 1, row_lo, row_hi);
+      if (live) seen_of<Packed>(a, q, token + j, token + j + 1, row_lo, row_hi);
       int32_t all_lo, all_hi;  // keys that every row of the tile sees
-      seen_by(p, q, token, token + 1, low, all_hi);
-      seen_by(p, q, token + tokens - 1, token + tokens, all_lo, high);
+      if (Packed) {
+        all_lo = 0;
+        all_hi = __reduce_min_sync(kFull, live ? row_hi : INT32_MAX);  // of the warp's rows
+      } else {
+        seen_by(p, q, token, token + 1, low, all_hi);
+        seen_by(p, q, token + tokens - 1, token + tokens, all_lo, high);
+      }
       float m = -INFINITY, l = 0.f;
       for (int32_t t = first; t < last && ok; ++t) {
         ok = wait(s_full + 8 * x, s_ring.phase);
@@ -1114,7 +1075,7 @@ __global__ void __launch_bounds__(2 * kTile, 2) tiles_join_kernel(const __grid_c
     p.lse[static_cast<uint64_t>(tok) * p.heads_q + h] = row_lse(m, l);
 }
 
-template <typename T, int DP>
+template <typename T, int DP, bool Packed>
 cudaError_t launch(const tiles_args& a, cudaStream_t stream) {
   using L = layout<DP>;
   const preba_pages_attend_t& p = a.p;
@@ -1123,12 +1084,17 @@ cudaError_t launch(const tiles_args& a, cudaStream_t stream) {
   const uint64_t strides_q[3] = {p.q_stride[1], p.q_stride[0], 0};
   const uint32_t box_q[2] = {a.group, a.tokens_per_tile};
   cudaError_t err = tensor_map(&map_q, p.dtype, p.q, dims_q, strides_q, box_q);
-  if (err == cudaSuccess) err = cache_map(&map_k, p, p.k_cache, p.k_stride, a.box_rows);
-  if (err == cudaSuccess) err = cache_map(&map_v, p, p.v_cache, p.v_stride, a.box_rows);
+  if (Packed) {
+    if (err == cudaSuccess) err = states_map(&map_k, p, a.states, p.k_cache, p.k_stride, a.box_rows);
+    if (err == cudaSuccess) err = states_map(&map_v, p, a.states, p.v_cache, p.v_stride, a.box_rows);
+  } else {
+    if (err == cudaSuccess) err = cache_map(&map_k, p, p.k_cache, p.k_stride, a.box_rows);
+    if (err == cudaSuccess) err = cache_map(&map_v, p, p.v_cache, p.v_stride, a.box_rows);
+  }
   if (err == cudaSuccess)
-    err = cudaFuncSetAttribute(tiles_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes);
+    err = cudaFuncSetAttribute(tiles_kernel<T, DP, Packed>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes);
   if (err != cudaSuccess) return err;
-  err = launch_chained(tiles_kernel<T, DP>, a.grid, kThreads, L::kBytes, stream, map_q, map_k, map_v, a);
+  err = launch_chained(tiles_kernel<T, DP, Packed>, a.grid, kThreads, L::kBytes, stream, map_q, map_k, map_v, a);
   if (err != cudaSuccess) return err;
   return launch_chained(tiles_join_kernel<T, DP>, a.grid * (DP / kJoinColumns), 2 * kTile, 0,
                         stream, a);
@@ -1146,14 +1112,14 @@ uint64_t tiles_workspace(uint32_t n, uint32_t tokens, uint32_t group, uint32_t h
          2ull * kMaxTileCtas * (head_dim <= 64 ? kPartial<64> : kPartial<128>) * sizeof(float4);
 }
 
-cudaError_t launch_tiles(const preba_pages_attend_t& p, uint32_t page_shift, int sms, void* workspace,
-                         cudaStream_t stream) {
-  tiles_args a{};
-  a.p = p;
-  a.page_shift = page_shift;
+namespace {
+
+// What the two ways share: `a` holds what is theirs.
+template <bool Packed>
+cudaError_t launch_planned(tiles_args& a, int sms, uint64_t keys_at_most, void* workspace, cudaStream_t stream) {
+  const preba_pages_attend_t& p = a.p;
   a.group = p.heads_q / p.heads_kv;
   a.tokens_per_tile = kTile / a.group;
-  a.box_rows = std::min<uint32_t>(p.page_size, kTile);
   a.box_shift = 31 - __builtin_clz(a.box_rows);
   a.grid = std::min(sms, kMaxTileCtas);
   const uint64_t pairs = pairs_at_most(p.n, p.tokens, a.group);
@@ -1168,21 +1134,43 @@ cudaError_t launch_tiles(const preba_pages_attend_t& p, uint32_t page_shift, int
   a.order = reinterpret_cast<uint32_t*>(at);
   at += up16(4 * pairs);
   a.partials = reinterpret_cast<float4*>(at);
-  a.own_plan = plans_own(pairs, p.heads_kv, a.grid,
-                         std::min<uint64_t>(static_cast<uint64_t>(p.table_width) * p.page_size, PREBA_PAGES_MAX_KEYS));
+  a.own_plan = plans_own(pairs, p.heads_kv, a.grid, keys_at_most);
   const size_t smem = kPlanThreads * sizeof(pair_t) + 4 * (static_cast<size_t>(p.n) + 1);
   if (smem > 40 * 1024) {  // beside 5 KB of its own; 48 KB need no leave
-    const cudaError_t err = cudaFuncSetAttribute(tiles_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    const cudaError_t err = cudaFuncSetAttribute(tiles_plan_kernel<Packed>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                  kPlanThreads * sizeof(pair_t) + 4 * (PREBA_PAGES_MAX_REQUESTS + 1));
     if (err != cudaSuccess) return err;
   }
   if (!a.own_plan) {
-    const cudaError_t err = launch_chained(tiles_plan_kernel, 1, kPlanThreads, smem, stream, a);
+    const cudaError_t err = launch_chained(tiles_plan_kernel<Packed>, 1, kPlanThreads, smem, stream, a);
     if (err != cudaSuccess) return err;
   }
   if (p.dtype == PREBA_F16)
-    return p.head_dim <= 64 ? launch<__half, 64>(a, stream) : launch<__half, 128>(a, stream);
-  return p.head_dim <= 64 ? launch<__nv_bfloat16, 64>(a, stream) : launch<__nv_bfloat16, 128>(a, stream);
+    return p.head_dim <= 64 ? launch<__half, 64, Packed>(a, stream) : launch<__half, 128, Packed>(a, stream);
+  return p.head_dim <= 64 ? launch<__nv_bfloat16, 64, Packed>(a, stream) : launch<__nv_bfloat16, 128, Packed>(a, stream);
+}
+
+}  // namespace
+
+cudaError_t launch_tiles(const preba_pages_attend_t& p, uint32_t page_shift, int sms, void* workspace,
+                         cudaStream_t stream) {
+  tiles_args a{};
+  a.p = p;
+  a.page_shift = page_shift;
+  a.box_rows = std::min<uint32_t>(p.page_size, kTile);
+  return launch_planned<false>(
+      a, sms, std::min<uint64_t>(static_cast<uint64_t>(p.table_width) * p.page_size, PREBA_PAGES_MAX_KEYS), workspace, stream);
+}
+
+cudaError_t launch_packed_tiles(const preba_pages_attend_t& p, const int32_t* cu_k, const int32_t* seen, uint32_t states,
+                                int sms, void* workspace, cudaStream_t stream) {
+  tiles_args a{};
+  a.p = p;
+  a.cu_k = cu_k;
+  a.seen = seen;
+  a.states = states;
+  a.box_rows = kStateRows;
+  return launch_planned<true>(a, sms, states, workspace, stream);
 }
 
 }  // namespace attend

@@ -13,7 +13,7 @@ from paper_2411_19114_b200 import binding as pb
 from paper_2411_19114_b200 import build as pbuild
 
 ROOT = Path(__file__).resolve().parent.parent
-STRUCTS = {"preba_beam_select_t": pb.PrebaBeamSelect, "preba_beam_pages_t": pb.PrebaBeamPages,
+STRUCTS = {"preba_cross_attend_t": pb.PrebaCrossAttend, "preba_beam_select_t": pb.PrebaBeamSelect, "preba_beam_pages_t": pb.PrebaBeamPages,
            "preba_pages_copy_t": pb.PrebaPagesCopy}
 
 
@@ -132,6 +132,31 @@ def test_copies_refuse_caches_that_are_not_there_or_not_aligned():
     assert pb.lib().preba_pages_copy(None, None) == pb.ERR_INVALID_ARG
 
 
+CROSS = dict(workspace_bytes=1 << 40, q_stride=(512, 64), out_stride=(512, 64), k_stride=(128, 64), v_stride=(128, 64), n=2,
+             tokens=6, states=100, max_q=3, heads_q=8, heads_kv=2, head_dim=64, dtype=pb.F16, scale=0.125)
+
+
+@pytest.mark.parametrize("change", [
+    dict(n=0), dict(n=16385), dict(tokens=0), dict(tokens=0x7ffff001), dict(states=0), dict(states=0x7ffff001), dict(max_q=0),
+    dict(heads_q=0), dict(heads_q=7), dict(heads_q=258), dict(heads_kv=0), dict(head_dim=0), dict(head_dim=60), dict(head_dim=136),
+    dict(dtype=pb.F32), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("inf")), dict(scale=float("nan")),
+    dict(q=None), dict(k=None), dict(v=None), dict(cu_q=None), dict(cu_k=None), dict(out=None), dict(workspace=None),
+    dict(q=4104), dict(k=4104), dict(v=4104), dict(out=4104), dict(workspace=4104), dict(q_stride=(512, 60)),
+    dict(k_stride=(0, 64)), dict(v_stride=(128, 0)), dict(q_stride=(0, 64)), dict(k_stride=(1 << 38, 64)),
+    dict(states=0x7f000000, heads_kv=128, heads_q=128), dict(tokens=0x7f000000, heads_q=512, heads_kv=8)])
+def test_cross_attention_refuses(change):
+    assert call("preba_cross_attend", filled(pb.PrebaCrossAttend, **{**CROSS, **change})) == pb.ERR_INVALID_ARG
+
+
+def test_cross_attention_refuses_a_small_workspace():
+    need = pb.preba_cross_attend_query(2, 6, 8, 2, 64)
+    s = filled(pb.PrebaCrossAttend, **{**CROSS, "workspace_bytes": need - 1})
+    assert call("preba_cross_attend", s) == pb.ERR_BUFFER_TOO_SMALL
+    assert pb.lib().preba_cross_attend(None, None) == pb.ERR_INVALID_ARG
+    with pytest.raises(pb.PrebaError):
+        pb.preba_cross_attend_query(2, 6, 8, 3, 64)
+
+
 def test_the_binding_refuses_what_it_cannot_describe():
     t = lambda *shape, dtype=torch.int32: torch.zeros(shape, dtype=dtype)  # noqa: E731
     f = torch.float32
@@ -140,6 +165,9 @@ def test_the_binding_refuses_what_it_cannot_describe():
         pb.PreparedBeamSelect(*good)
     with pytest.raises(ValueError):
         pb.PreparedBeamSelect(t(6, 100, dtype=torch.float64), *good[1:])
+    h = lambda *shape: torch.zeros(shape, dtype=torch.float16)  # noqa: E731
+    with pytest.raises(ValueError):
+        pb.PreparedCrossAttend(h(6, 8, 64), h(9, 2, 64), h(9, 2, 64), t(3), t(3), h(6, 8, 64), t(99), 3, 0.1)
     with pytest.raises(ValueError):
         pb.PreparedBeamPages(t(6), t(6), t(6, 9), t(6, 9), t(6), t(6, 4), t(50), t(1), t(1), 16, t(999), 3)
     with pytest.raises(ValueError):
