@@ -54,7 +54,7 @@ extern "C" {
  * PREBA_PAGES_MAX_KEYS, a base that is not 16-byte aligned, a stride that is not a multiple of 8, heads_q not a multiple of
  * heads_kv, heads_q above 65535, more than 128 query heads on one key head, head_dim not a multiple of 8 in
  * 8 .. PREBA_PAGES_MAX_HEAD_DIM, a stride of 0 on an axis of q, k or v that has more than one entry, so many states that
- * heads_kv * (n + states / 128) passes 2e9, or so many rows that heads_kv * (n + tokens / (2 * g)) passes 2^31 - 1, where
+ * heads_kv * (2 * n + states / 128) passes 2e9, or so many rows that heads_kv * (n + tokens / (2 * g)) passes 2^31 - 1, where
  * g = 128 * heads_kv / heads_q rounded down), PREBA_ERR_BUFFER_TOO_SMALL (workspace), PREBA_ERR_CUDA.
  */
 typedef struct {

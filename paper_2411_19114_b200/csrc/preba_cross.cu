@@ -34,145 +34,178 @@ constexpr int kFewRows = 64;          // rows on a key head that this kernel tak
 constexpr int kSoftWarps = 4, kSoftThreads = 32 * kSoftWarps;
 constexpr int kCopyWarp = 4, kMmaWarp = 5;
 constexpr int kThreads = 192;
-constexpr uint32_t kMinTiles = 2;     // a CTA's run is not shorter than this
+constexpr uint32_t kMinUnits = 3;     // a CTA's run is not shorter than this
+constexpr uint32_t kWholeTiles = 8;   // tiles of a (request, key head) that is not split where there is a CTA for each
 constexpr uint64_t kMostUnits = 2000000000;  // of the line
+constexpr uint64_t kNowhere = ~0ull;  // of a column without a row
 constexpr float kGrowth = 8.f;        // log2 of what a row may outgrow its reference by
 constexpr uint64_t kCounterBytes = kMaxTileCtas * 4;  // at the workspace's start
 
-// DP: head_dim rounded up to 64 or 128; N: rows rounded up to 16, 32 or 64.
-template <int DP, int N> struct layout {
-  static constexpr int kHalves = DP / 64;
+// D: head_dim rounded up to 64 or 128.  H: key heads of a piece.  Heads of up to 64 are taken in pairs, whose rows in memory
+// lie side by side more often than not: 64 requests of 5 beams over 1500 states of 20 heads of 64, single heads 76 us (61 if
+// each head's states lie together), pairs 60 us.  The product with the values then has the elements of both heads as its 128
+// rows, and of its columns each half belongs to one of them.  N: columns, R rows of each head.
+template <int D, int H, int R> struct layout {
+  static constexpr int N = H * R;
+  static constexpr int kHalves = H * D / 64;                // of 64 elements: of one head, or of a pair
   static constexpr uint32_t kHalf = kTile * 128;            // 64 elements of 128 states
   static constexpr uint32_t kSlot = kHalves * kHalf;        // a tile of keys, or of values
-  static constexpr int kSlots = DP == 128 ? 5 : 10;
-  static constexpr uint32_t kP = kSlots * kSlot;            // two tiles of P^T: 128 states of 128 bytes
-  static constexpr uint32_t kQ = kP + 2 * kTile * 128;      // 64 elements of N rows, twice where DP is 128
-  static constexpr uint32_t kStats = kQ + kHalves * N * 128;
+  static constexpr int kSlots = kHalves == 1 ? 10 : N <= 32 ? 6 : 5;
+  // Two tiles of P^T, 128 states of N rows each in lines of 128 bytes: side by side if they fit, else one after the other
+  static constexpr uint32_t kP = kSlots * kSlot;
+  static constexpr uint32_t kPNext = N <= 32 ? N * 2 : kTile * 128;
+  static constexpr uint32_t kQ = kP + (N <= 32 ? 1 : 2) * kTile * 128;  // two sets of queries: 64 elements of R rows, once or twice
+  static constexpr uint32_t kQSize = kHalves * R * 128;
+  static constexpr uint32_t kStats = kQ + 2 * kQSize;
   static constexpr uint32_t kBars = kStats + 8 * N * 4 + N * 8;
-  static constexpr uint32_t kControl = kBars + 8 * (2 * kSlots + 8);
+  static constexpr uint32_t kControl = kBars + 8 * (2 * kSlots + 12);
   static constexpr uint32_t kBytes = kControl + 256;
-  // Tensor memory columns.  P^T of 64 rows fills a line of 128 bytes, that of fewer leaves the rest of it unused.
+  // Tensor memory columns.
   static constexpr uint32_t kS = 0, kO = 2 * N;
   static constexpr uint32_t kColumns = N == 64 ? 256 : N == 32 ? 128 : 64;
-  // With head_dim 64 the product has 128 rows all the same; what the upper 64 hold is read from behind the tile (there is
+  // One head of 64: the product has 128 rows all the same; what the upper 64 hold is read from behind the tile (there is
   // always something of this CTA's there) and never looked at.
   static constexpr uint32_t kLeading = kHalf;
-  static_assert(kBars % 8 == 0 && kBytes <= 227 * 1024, "shared memory");
+  static_assert(kBars % 8 == 0 && kBytes <= 227 * 1024 && kP >= kTile * 128, "shared memory");
 };
-// Floats of a partial sum: O^T row by row, then a maximum and a sum for each.
-template <int DP> constexpr uint32_t kPartial = kFewRows * DP + 2 * kFewRows;
+// Floats of a partial sum: O^T column by column, then a maximum and a sum for each.
+template <int D> constexpr uint32_t kPartial = kFewRows * D + 2 * kFewRows;
+constexpr uint32_t kDirect = 4;  // pieces of a (request, head) that the CTA with the first of them joins on the spot, at most
 
 // What a call is about beside the sizes it shares with the paged attention.
 struct cross_args {
   preba_pages_attend_t p;
   const int32_t* cu_k;
   const int32_t* seen;
-  uint32_t states, group, grid;
+  uint32_t states, group, grid, q_rows;  // q_rows: tokens of a request, at most
+  uint32_t heads;                        // key heads, or pairs of them
 #if defined(PREBA_CHECKED)
   wait_limits_t limits = wait_limits();
 #endif
 };
 
 struct piece_t {
-  int32_t live;          // 0: none
   uint32_t request, head;
   uint32_t first, last;  // CTAs that hold pieces of the same (request, key head)
 };
+// A request as the walk needs it.
+struct entry_t {
+  request_t q;
+  int32_t state0, hi;  // its first state, and how many of them some row sees
+  uint32_t tiles;      // on one key head (or pair); 0: it has no rows or is at fault
+};
 struct run_t {
-  uint32_t begin, end, per;  // units of one tile of one key head; units per CTA
+  uint32_t begin, end, per;  // units; units per CTA
   uint32_t request, offset;  // of the first unit
+  entry_t entry;
 };
 struct control_t {
   run_t run;
   piece_t pieces[2];
   uint64_t warp_sums[kThreads / 32];
-  uint32_t joins[2], tmem;
+  uint32_t warp_pieces[kThreads / 32], warp_longest[kThreads / 32], joins[2], alone, tmem;
 };
 static_assert(sizeof(control_t) <= 256, "layout::kBytes");
 
-__device__ __forceinline__ uint32_t tiles_of(const cross_args& a, const request_t& q, int32_t& hi) {
-  if (q.rows == 0) return 0;
-  hi = packed_seen(a.p.tokens, a.seen, q, 0, q.rows);
-  return max(1, (hi + kTile - 1) / kTile);  // a request whose rows see nothing still has its zeros to write
-}
-__device__ __forceinline__ uint32_t units_of(const cross_args& a, uint32_t r) {
-  request_t q;
-  int32_t hi;
-  return load_packed(a.p, a.cu_k, a.states, r, q) ? tiles_of(a, q, hi) * a.p.heads_kv : 0;
+__device__ __forceinline__ bool load_entry(const cross_args& a, uint32_t r, entry_t& e) {
+  e.tiles = 0;
+  if (!load_packed(a.p, a.cu_k, a.states, r, e.q)) return false;
+  e.state0 = a.cu_k[r];
+  e.hi = packed_seen(a.p.tokens, a.seen, e.q, 0, e.q.rows);
+  if (e.q.rows) e.tiles = max(1, (e.hi + kTile - 1) / kTile);  // one that sees nothing still has its zeros to write
+  return true;
 }
 
-// Where a CTA's run begins: the block adds up the tiles of all requests, each thread of a run of them.
+// Where a CTA's run begins: the block adds up the units of all requests, each thread of a run of them.  The units of a (request,
+// key head) are one for its beginning and end, which cost about what a tile does, and one for each tile.  Where there is a CTA
+// for every (request, key head), and none of them is long, each takes one and nothing has to be joined (two
+// requests of up to 3 tiles on 8 heads: 8.1 us, in equal runs 11.3).
 __device__ __forceinline__ void find_run(const cross_args& a, control_t& ctl) {
   const preba_pages_attend_t& p = a.p;
   const uint32_t chunk = (p.n + kThreads - 1) / kThreads;
   const uint32_t r0 = min(threadIdx.x * chunk, p.n), r1 = min(r0 + chunk, p.n);
   uint64_t mine = 0;
+  uint32_t my_pieces = 0, longest = 0;
+  entry_t e{};
   for (uint32_t r = r0; r < r1; ++r) {
-    mine += units_of(a, r);
-    request_t q;
-    if (blockIdx.x == 0 && !load_packed(p, a.cu_k, a.states, r, q)) report(p.status, PREBA_ERR_BAD_TABLE);
+    if (!load_entry(a, r, e) && blockIdx.x == 0) report(p.status, PREBA_ERR_BAD_TABLE);
+    if (e.tiles) mine += static_cast<uint64_t>(e.tiles + 1) * a.heads, my_pieces += a.heads;
+    longest = max(longest, e.tiles);
   }
   uint64_t incl = mine;
+  uint32_t pieces_incl = my_pieces;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const uint64_t up = __shfl_up_sync(kFull, incl, o);
-    if (lane >= o) incl += up;
+    const uint32_t pieces_up = __shfl_up_sync(kFull, pieces_incl, o);
+    if (lane >= o) incl += up, pieces_incl += pieces_up;
   }
-  if (lane == 31) ctl.warp_sums[warp] = incl;
+  longest = __reduce_max_sync(kFull, longest);
+  if (lane == 31) ctl.warp_sums[warp] = incl, ctl.warp_pieces[warp] = pieces_incl, ctl.warp_longest[warp] = longest;
   __syncthreads();
   uint64_t sum = 0, before = 0;
+  uint32_t pieces = 0, pieces_before = 0;  // at most 16384 * 65535
 #pragma unroll
   for (int w = 0; w < kThreads / 32; ++w) {
-    if (w < warp) before += ctl.warp_sums[w];
+    if (w < warp) before += ctl.warp_sums[w], pieces_before += ctl.warp_pieces[w];
     sum += ctl.warp_sums[w];
+    pieces += ctl.warp_pieces[w];
+    longest = max(longest, ctl.warp_longest[w]);
   }
   // requests that do not overlap never come to more (the host has seen to it); if they do, nothing is done
   if (sum > kMostUnits && blockIdx.x == 0 && threadIdx.x == 0) report(p.status, PREBA_ERR_BAD_TABLE);
   const uint32_t total = sum > kMostUnits ? 0 : static_cast<uint32_t>(sum);
-  const uint32_t per = max(kMinTiles, (total + gridDim.x - 1) / gridDim.x);
-  const uint32_t begin = min(static_cast<uint64_t>(blockIdx.x) * per, static_cast<uint64_t>(total));
-  uint64_t at = before + incl - mine;
-  if (threadIdx.x == 0) {
-    ctl.run.begin = begin;
-    ctl.run.end = min(begin + per, total);
-    ctl.run.per = per;
-  }
-  if (begin < total && begin >= at && begin < at + mine) {
+  const bool whole = pieces <= gridDim.x && longest <= kWholeTiles;
+  const uint32_t per = whole ? 1 : max(kMinUnits, (total + gridDim.x - 1) / gridDim.x);
+  const uint32_t all = whole ? pieces : total;  // in pieces, or in units
+  const uint32_t begin = min(static_cast<uint64_t>(blockIdx.x) * per, static_cast<uint64_t>(all));
+  uint64_t at = whole ? pieces_before + pieces_incl - my_pieces : before + incl - mine;
+  if (begin >= all) {
+    if (threadIdx.x == 0) ctl.run.begin = ctl.run.end = 0;
+  } else if (begin >= at && begin < at + (whole ? my_pieces : mine)) {  // one thread
     uint32_t r = r0;
     for (;; ++r) {
-      const uint32_t units = units_of(a, r);
-      if (begin < at + units) break;
-      at += units;
+      if (r1 - r0 > 1) load_entry(a, r, e);
+      const uint32_t here = e.tiles == 0 ? 0 : whole ? a.heads : (e.tiles + 1) * a.heads;
+      if (begin < at + here) break;
+      at += here;
     }
-    ctl.run.request = r;
-    ctl.run.offset = static_cast<uint32_t>(begin - at);
+    const uint32_t from = static_cast<uint32_t>(begin - at);
+    if (whole) ctl.run = {0, e.tiles + 1, e.tiles + 1, r, from * (e.tiles + 1), e};
+    else ctl.run = {begin, min(begin + per, all), per, r, from, e};
   }
   __syncthreads();
 }
 
 // Walks a CTA's run piece by piece; every warp does so for itself.
 struct walk_t {
-  uint32_t unit, end, request, offset;  // next unit; offset within the request
-  request_t q;
-  int32_t hi;                           // states that some row sees
-  uint32_t tiles, head, tile, count;    // of the current piece
+  uint32_t unit, end, per, request, offset;  // next unit; offset within the request
+  entry_t of;
+  uint32_t start, head, tile, count;         // the current piece; start: of the (request, key head)
   __device__ __forceinline__ explicit walk_t(const run_t& run)
-      : unit(run.begin), end(run.end), request(run.request), offset(run.offset) {}
+      : unit(run.begin), end(run.end), per(run.per), request(run.request), offset(run.offset), of(run.entry) {}
   __device__ __forceinline__ bool next(const cross_args& a) {
-    if (unit >= end) return false;
-    for (;; ++request, offset = 0) {    // ends: unit < end, so a later request has tiles
-      if (!load_packed(a.p, a.cu_k, a.states, request, q)) continue;
-      tiles = tiles_of(a, q, hi);
-      if (offset < tiles * a.p.heads_kv) break;
+    while (unit < end) {
+      while (offset >= (of.tiles + 1) * a.heads || of.tiles == 0) {  // ends: unit < end, so a later request has tiles
+        offset = 0;
+        load_entry(a, ++request, of);
+      }
+      const uint32_t units = of.tiles + 1;
+      head = offset / units;
+      const uint32_t at = offset - head * units, take = min(units - at, end - unit);
+      start = unit - at;
+      unit += take;
+      offset += take;
+      tile = at ? at - 1 : 0;
+      count = at ? take : take - 1;
+      if (count) return true;
     }
-    head = offset / tiles;
-    tile = offset - head * tiles;
-    count = min(tiles - tile, end - unit);
-    unit += count;
-    offset += count;
-    return true;
+    return false;
   }
+  __device__ __forceinline__ bool whole() const { return count == of.tiles; }
+  __device__ __forceinline__ uint32_t first_cta() const { return (start + 1) / per; }
+  __device__ __forceinline__ uint32_t last_cta() const { return (start + of.tiles) / per; }
 };
 
 // 128 rows; the first operand's rows or columns are contracted, as the second's are.
@@ -242,25 +275,27 @@ template <int N> __device__ __forceinline__ int column_of(int i) {
   return N == 16 ? lane >> 1 : N == 32 ? lane : 2 * lane + i;
 }
 
-template <int DP> __device__ __forceinline__ float* partial_of(const cross_args& a, uint32_t cta, uint32_t slot) {
-  if (!PREBA_IN_RANGE(a.p.status, 2 * cta + slot < 2 * kMaxTileCtas)) cta = slot = 0;
+template <int D> __device__ __forceinline__ float* partial_of(const cross_args& a, uint32_t cta, uint32_t slot) {
+  if (!PREBA_IN_RANGE(a.p.status, 2 * cta + slot < 2 * a.grid)) cta = slot = 0;
   return reinterpret_cast<float*>(static_cast<uint8_t*>(a.p.workspace) + kCounterBytes) +
-         static_cast<uint64_t>(2 * cta + slot) * kPartial<DP>;
+         static_cast<uint64_t>(2 * cta + slot) * kPartial<D>;
 }
 
-template <typename T, int DP, int N>
+template <typename T, int D, int H, int R>
 __global__ void __launch_bounds__(kThreads, 1)
-cross_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-             const __grid_constant__ cross_args a) {
-  using L = layout<DP, N>;
+cross_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+             const __grid_constant__ CUtensorMap map_v, const __grid_constant__ cross_args a) {
+  using L = layout<D, H, R>;
+  constexpr int N = L::N;
   extern __shared__ __align__(1024) uint8_t smem[];
   const preba_pages_attend_t& p = a.p;
   const int lane = threadIdx.x & 31;
   const int warp = __shfl_sync(kFull, threadIdx.x >> 5, 0);
   const uint32_t base = smem_addr(smem);
   const uint32_t kv_full = base + L::kBars, kv_empty = kv_full + 8 * L::kSlots;
-  const uint32_t q_full = kv_empty + 8 * L::kSlots, drained = q_full + 8;
-  const uint32_t s_full = drained + 8, p_full = s_full + 16, o_done = p_full + 16;  // two each
+  const uint32_t drained = kv_empty + 8 * L::kSlots;
+  const uint32_t s_full = drained + 8, p_full = s_full + 16, o_done = p_full + 16, q_full = o_done + 16,
+                 q_empty = q_full + 16;  // two each
   control_t& ctl = *reinterpret_cast<control_t*>(smem + L::kControl);
 
   if (threadIdx.x == 0) {
@@ -268,14 +303,16 @@ cross_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       mbar_init(kv_full + 8 * s, 1);
       mbar_init(kv_empty + 8 * s, 1);
     }
-    mbar_init(q_full, kSoftWarps);
     mbar_init(drained, 1);
     for (int x = 0; x < 2; ++x) {
+      mbar_init(q_full + 8 * x, 1);
+      mbar_init(q_empty + 8 * x, 1);
       mbar_init(s_full + 8 * x, 1);
       mbar_init(p_full + 8 * x, kSoftWarps);
       mbar_init(o_done + 8 * x, 1);
     }
-    ctl.pieces[0].live = ctl.pieces[1].live = 0;
+    ctl.joins[0] = ctl.joins[1] = 0;
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_q) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -303,15 +340,27 @@ cross_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     // ---- copies: a lane per box of 32 states, 64 elements wide
     constexpr uint32_t kBoxes = kTile / kStateRows;
     const uint32_t chunk = lane % kBoxes, half = lane / kBoxes;
-    const bool mine = half < L::kHalves;
     const uint32_t dst = half * L::kHalf + chunk * kStateRows * 128;
+    const uint32_t x = H == 2 ? 0 : half * 64, of_pair = H == 2 ? half : 0;  // a half is elements of the head, or a head of the pair
     walk_t w(run);
-    uint32_t slot = 0, phase = 1, issued = 0;  // a fresh barrier counts as emptied
+    uint32_t slot = 0, phase = 1, issued = 0, pieces = 0;  // a fresh barrier counts as emptied
     while (ok && w.next(a)) {
-      const int32_t state0 = a.cu_k[w.request];
+      const int32_t state0 = w.of.state0;
+      // the piece's queries, and whatever lies behind them up to q_rows tokens
+      const uint32_t qb = pieces & 1;
+      ok = wait(q_empty + 8 * qb, (pieces >> 1 & 1) ^ 1);
+      if (!ok) break;
+      ++pieces;
+      if (lane == 0) {
+        mbar_arrive_expect_tx(q_full + 8 * qb, a.q_rows * a.group * 128 * L::kHalves);
+        for (int h = 0; h < L::kHalves; ++h)  // a head behind the last reads as 0
+          tensor_copy(base + L::kQ + qb * L::kQSize + h * R * 128, &map_q, H == 2 ? 0 : 64 * h,
+                      (H * w.head + (H == 2 ? h : 0)) * a.group, w.of.q.row, 0, q_full + 8 * qb);
+      }
+      const bool mine = half < L::kHalves && H * w.head + of_pair < p.heads_kv;
       int32_t key = w.tile * kTile + chunk * kStateRows;
       for (uint32_t t = 0; t < w.count && ok; ++t, key += kTile) {
-        const bool want = mine && key < w.hi;
+        const bool want = mine && key < w.of.hi;
         const uint32_t bytes = __popc(__ballot_sync(kFull, want)) * kStateRows * 128;
 #pragma unroll
         for (int v = 0; v < 2; ++v) {
@@ -320,7 +369,7 @@ cross_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
           if (lane == 0) mbar_arrive_expect_tx(kv_full + 8 * slot, bytes);
           __syncwarp();
           if (want)
-            tensor_copy(base + slot * L::kSlot + dst, v ? &map_v : &map_k, half * 64, state0 + key, w.head, 0,
+            tensor_copy(base + slot * L::kSlot + dst, v ? &map_v : &map_k, x, state0 + key, H * w.head + of_pair, 0,
                         kv_full + 8 * slot);
           ++issued;
           if (++slot == L::kSlots) slot = 0, phase ^= 1;
@@ -331,51 +380,53 @@ cross_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
       report(p.status, PREBA_ERR_TIMEOUT);
       for (uint32_t i = issued - min(issued, static_cast<uint32_t>(L::kSlots)); i < issued; ++i)
         mbar_wait(kv_full + 8 * (i % L::kSlots), (i / L::kSlots) & 1);
+      for (uint32_t i = pieces - min(pieces, 2u); i < pieces; ++i) mbar_wait(q_full + 8 * (i & 1), (i >> 1) & 1);
     }
   } else if (warp == kMmaWarp) {
     // ---- matrix products: one lane issues, the warp clears values that nobody sees
-    constexpr uint32_t kQkShape = shape<T>(N, false), kPvShape = shape<T>(N, true);
+    constexpr uint32_t kQkShape = shape<T>(R, false), kPvShape = shape<T>(N, true);
     walk_t w(run);
-    uint32_t slot = 0, phase = 0, q_phase = 0;
-    uint32_t n_s = 0, n_p = 0;  // tiles so far
+    uint32_t slot = 0, phase = 0;
+    uint32_t n_s = 0, n_p = 0, pieces = 0;  // tiles and pieces so far
     auto step = [&]() {
       const uint32_t s = slot;
       if (++slot == L::kSlots) slot = 0, phase ^= 1;
       return s;
     };
-    auto qk = [&]() {
+    auto qk = [&](bool last) {
       ok = ok && wait(kv_full + 8 * slot, phase);
       if (!ok) return;
       fence_after();
       const uint32_t k_slot = step();
       const uint32_t k_op = __shfl_sync(kFull, operand(base + k_slot * L::kSlot, 16), 0);
-      const uint32_t q_op = __shfl_sync(kFull, operand(base + L::kQ, 16), 0);
+      const uint32_t qb = pieces & 1;
+      const uint32_t q_op = __shfl_sync(kFull, operand(base + L::kQ + qb * L::kQSize, 16), 0);
       const uint32_t d = __shfl_sync(kFull, tmem + L::kS + (n_s & 1) * N, 0);
       if (elected()) {
 #pragma unroll
-        for (int ks = 0; ks < DP / 16; ++ks)
-          mma_ss(d, k_op + (((ks / 4) * L::kHalf + (ks % 4) * 32) >> 4), q_op + (((ks / 4) * N * 128 + (ks % 4) * 32) >> 4),
-                 kQkShape, ks > 0);
+        for (int ks = 0; ks < H * D / 16; ++ks)  // of the head, or of one head of the pair after the other
+          mma_ss(H == 2 ? d + ks / 4 * R : d, k_op + (((ks / 4) * L::kHalf + (ks % 4) * 32) >> 4),
+                 q_op + (((ks / 4) * R * 128 + (ks % 4) * 32) >> 4), kQkShape, H == 2 ? ks % 4 > 0 : ks > 0);
         mma_commit(s_full + 8 * (n_s & 1));
         mma_commit(kv_empty + 8 * k_slot);
+        if (last) mma_commit(q_empty + 8 * qb);
       }
       __syncwarp();
       ++n_s;
     };
-    while (ok && w.next(a)) {
-      ok = wait(q_full, q_phase);
+    for (; ok && w.next(a); ++pieces) {
+      ok = wait(q_full + 8 * (pieces & 1), (pieces >> 1) & 1);
       if (!ok) break;
-      q_phase ^= 1;
       fence_after();
-      qk();
+      qk(w.count == 1);
       for (uint32_t t = 0; t < w.count && ok; ++t) {
         // values come before the next keys; the scores of the next tile are made while this one's are looked at
         const uint32_t v_slot = slot, v_phase = phase;
         step();
-        if (t + 1 < w.count) qk();
+        if (t + 1 < w.count) qk(t + 2 == w.count);
         ok = ok && wait(kv_full + 8 * v_slot, v_phase);
         if (!ok) break;
-        const int32_t seen = w.hi - static_cast<int32_t>((w.tile + t) * kTile);
+        const int32_t seen = w.of.hi - static_cast<int32_t>((w.tile + t) * kTile);
         if (seen < kTile) {
           // values outside the seen states may be anything, and 0 times NaN is NaN: clear them
           uint8_t* at = smem + v_slot * L::kSlot;
@@ -390,7 +441,7 @@ cross_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         if (!ok) break;
         fence_after();
         const uint32_t v_op = __shfl_sync(kFull, operand(base + v_slot * L::kSlot, L::kLeading), 0);
-        const uint32_t p_op = __shfl_sync(kFull, operand(base + L::kP + b * kTile * 128, 16), 0);
+        const uint32_t p_op = __shfl_sync(kFull, operand(base + L::kP + b * L::kPNext, 16), 0);
         const uint32_t d = __shfl_sync(kFull, tmem + L::kO, 0);
         if (elected()) {
 #pragma unroll
@@ -421,37 +472,45 @@ cross_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     uint64_t* row_at = reinterpret_cast<uint64_t*>(row_hi + 2 * N); // where a row's result goes
     walk_t w(run);
     uint32_t n = 0;  // tiles so far
+    // A piece whose partial sums are on their way is counted a tile later, when they have arrived: a fence behind them
+    // waits for 2 to 4 us while all SMs read
+    bool pending = false;
+    piece_t pending_piece{};
+    uint32_t before_pending = 0;  // counted before it, known to thread 0 when it is needed
+    auto count_piece = [&]() {  // behind a barrier behind everybody's fence
+      if (r == 0) before_pending = atomicAdd(static_cast<uint32_t*>(p.workspace) + pending_piece.first, 1);
+      pending = false;
+    };
+    auto counted = [&](int which) {
+      if (r != 0) return;
+      const bool last = before_pending == pending_piece.last - pending_piece.first;
+      if (last) static_cast<uint32_t*>(p.workspace)[pending_piece.first] = 0;  // as the next call wants it
+      ctl.pieces[which] = pending_piece;
+      ctl.joins[which] = last;
+    };
+    bool first_counted = false;
     while (w.next(a)) {
-      const int32_t rows = w.q.rows * a.group;
+      const request_t q = w.of.q;
+      const int32_t rows = q.rows * a.group;
       const bool go = !soft_any(!ok);
       ok = go;
-      // queries, 16 bytes at a time; rows that are not there are 0 and take part in nothing
-      for (int i = r; i < N * (DP / 8); i += kSoftThreads) {
-        const int row = i / (DP / 8), e = i % (DP / 8) * 8;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (row < rows && e < static_cast<int>(p.head_dim)) {
-          const uint32_t j = row / a.group, h = w.head * a.group + row - j * a.group;
-          v = *reinterpret_cast<const uint4*>(static_cast<const T*>(p.q) + (w.q.row + j) * p.q_stride[0] + h * p.q_stride[1] + e);
-        }
-        *reinterpret_cast<uint4*>(smem + L::kQ + e / 64 * N * 128 + row * 128 + ((e / 8 % 8 ^ (row & 7)) << 4)) = v;
-      }
       float m = -INFINITY;  // of row r, where there is one: the largest score of those looked at when it grew last
       int32_t hi = 0;
+      // the row of column r: query row j, query head h
+      const uint32_t kv_head = H * w.head + r / R, in_head = r % R;
+      const bool row_there = r < N && in_head < static_cast<uint32_t>(rows) && kv_head < p.heads_kv;
+      const uint32_t j = in_head / a.group, h = kv_head * a.group + in_head - j * a.group;
       if (r < N) {
-        const uint32_t j = r / a.group, h = w.head * a.group + r - j * a.group;
-        if (r < rows) hi = packed_seen(p.tokens, a.seen, w.q, j, j + 1);
+        if (row_there) hi = packed_seen(p.tokens, a.seen, q, j, j + 1);
         row_hi[r] = hi;
-        row_at[r] = r < rows ? (w.q.row + j) * p.out_stride[0] + h * p.out_stride[1] : 0;
-        ref[r] = 0.f;
+        row_at[r] = row_there ? (q.row + j) * p.out_stride[0] + h * p.out_stride[1] : kNowhere;
+        ref[r] = row_there ? 0.f : INFINITY;  // columns without a row hold whatever lay behind the queries: they outgrow nothing
       }
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      __syncwarp();
-      fence_before();
-      if (lane == 0) mbar_arrive(q_full);
       soft_sync();  // what every row sees is there
-      int32_t all = w.hi;  // states that every row sees
+      int32_t all = w.of.hi;  // states that every row sees
       if (a.seen)
-        for (int c = 0; c < rows; ++c) all = min(all, row_hi[c]);
+        for (int c = 0; c < N; ++c)
+          if (row_at[c] != kNowhere) all = min(all, row_hi[c]);
       float l[N];
 #pragma unroll
       for (int c = 0; c < N; ++c) l[c] = 0.f;
@@ -479,11 +538,15 @@ cross_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
           }
           return top;
         };
+        const bool count_now = pending && t == 1;
+        if (count_now) __threadfence();
         ok = ok && wait(s_full + 8 * b, (n >> 1) & 1);
         fence_after();
         scores();
         // a row that sees a state and has no reference yet gets one
-        if (soft_any(exponents() > kGrowth || (m == -INFINITY && hi > 0) || !ok)) {
+        const bool slow = soft_any(exponents() > kGrowth || (m == -INFINITY && hi > 0) || !ok);
+        if (count_now) count_piece();
+        if (slow) {
           if (soft_any(!ok)) {
             ok = false;
             break;
@@ -499,7 +562,7 @@ cross_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             const float top = fmaxf(fmaxf(stats[r], stats[N + r]), fmaxf(stats[2 * N + r], stats[3 * N + r])) * scale;
             const float to = fmaxf(m, top);
             keep[r] = to == -INFINITY ? 0.f : exp2_approx(m - to);
-            ref[r] = to == -INFINITY ? 0.f : to;
+            if (row_there) ref[r] = to == -INFINITY ? 0.f : to;
             m = to;
           }
           soft_sync();
@@ -522,7 +585,8 @@ cross_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
           exponents();
         }
         if (t > 1) ok = ok && wait(o_done + 8 * b, ((n - 2) >> 1) & 1);  // that product has read its P
-        uint8_t* to = smem + L::kP + b * kTile * 128 + r * 128;
+        uint8_t* to = smem + L::kP + (N <= 32 ? 0 : b * L::kPNext) + r * 128;
+        const uint32_t chunk0 = N <= 32 ? b * (N / 8) : 0;
 #pragma unroll
         for (int c = 0; c < N; c += 8) {
           uint32_t e[4];
@@ -532,7 +596,7 @@ cross_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             l[c + i] += z0, l[c + i + 1] += z1;
             e[i / 2] = pack2<T>(z0, z1);
           }
-          if (ok) *reinterpret_cast<uint4*>(to + ((c / 8 ^ (r & 7)) << 4)) = make_uint4(e[0], e[1], e[2], e[3]);
+          if (ok) *reinterpret_cast<uint4*>(to + (((chunk0 + c / 8) ^ (r & 7)) << 4)) = make_uint4(e[0], e[1], e[2], e[3]);
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         fence_before();
@@ -540,112 +604,202 @@ cross_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         if (ok && lane == 0) mbar_arrive(p_full + 8 * b);
       }
       // ---- the piece is over: the threads' sums are joined
+      const bool whole = w.whole(), begins = w.tile == 0;
+      const piece_t x{w.request, w.head, w.first_cta(), w.last_cta()};
+      uint32_t* counter = static_cast<uint32_t*>(p.workspace) + x.first;
+      uint32_t arrived = 0;
+      if (r == 0 && begins && !whole) arrived = *static_cast<volatile uint32_t*>(counter);
       ok = ok && wait(o_done + 8 * ((n - 1) & 1), ((n - 1) >> 1) & 1);
       fence_after();
-      uint32_t o[N];
-      tmem_load<N>(o, tmem + lanes + L::kO);
+      // a thread has an element of one head, and the columns of that head
+      constexpr int kMine = H == 2 ? R : N;
+      const int e = r % (H == 2 ? 64 : 128), col0 = H == 2 ? r / 64 * R : 0;
+      uint32_t o[kMine];
+      tmem_load<kMine>(o, tmem + lanes + L::kO + col0);
       fence_before();
       sum_columns<N>(l);
 #pragma unroll
       for (int i = 0; i < (N + 31) / 32; ++i) stats[warp * N + column_of<N>(i)] = l[i];
-      soft_sync();
-      const bool whole = w.count == w.tiles;
-      const uint32_t piece = w.tile == 0;
-      float* part = partial_of<DP>(a, blockIdx.x, piece);
-      if (r < rows) {
-        const float sum = (stats[r] + stats[N + r]) + (stats[2 * N + r] + stats[3 * N + r]);
-        if (whole) {
-          keep[r] = inverse_of(sum);
-          const uint32_t j = r / a.group, h = w.head * a.group + r - j * a.group;
-          if (p.lse && PREBA_IN_RANGE(p.status, w.q.row + j < p.tokens))
-            p.lse[static_cast<uint64_t>(w.q.row + j) * p.heads_q + h] = row_lse(m, sum);
-        } else {
-          reinterpret_cast<float2*>(part + kFewRows * DP)[r] = make_float2(marked(m, sum), sum);
+      // The others' pieces were counted when they were over, which for a run's first piece is early: if they are all there
+      // the CTA with the first piece joins them on the spot, and its own is never written down
+      if (r == 0) {
+        ctl.alone = begins && !whole && arrived == x.last - x.first && x.last - x.first < kDirect;
+        if (ctl.alone) {
+          *counter = 0;  // as the next call wants it
+          __threadfence();
         }
       }
+      if (pending) __threadfence();
       soft_sync();
-      if (whole) {
-        if (r < static_cast<int>(p.head_dim)) {
+      if (pending) count_piece();  // the piece after it had one tile
+      const bool here = ctl.alone;
+      float sum = 0.f;
+      if (row_there) sum = (stats[r] + stats[N + r]) + (stats[2 * N + r] + stats[3 * N + r]);
+      if (whole || here) {
+        if (here) {
+          // weights of the pieces in the order of the states, as below; nobody reads P now
+          float* weights = reinterpret_cast<float*>(smem + L::kP);
+          if (row_there) {
+            float2 stat[kDirect];
+            stat[0] = make_float2(marked(m, sum), sum);
 #pragma unroll
-          for (int c = 0; c < N; ++c)
-            if (c < rows) static_cast<T*>(p.out)[row_at[c] + r] = result_of<T>(__uint_as_float(o[c]), keep[c]);
+            for (uint32_t k = 1; k < kDirect; ++k)
+              stat[k] = x.first + k <= x.last ? __ldcg(reinterpret_cast<const float2*>(partial_of<D>(a, x.first + k, 0) + kFewRows * D) + r)
+                                              : make_float2(-INFINITY, 0.f);
+            float top = -INFINITY;
+#pragma unroll
+            for (uint32_t k = 0; k < kDirect; ++k) top = fmaxf(top, stat[k].x);
+            sum = 0.f;
+#pragma unroll
+            for (uint32_t k = 0; k < kDirect; ++k) {
+              const float weight = stat[k].x == -INFINITY ? 0.f : exp2_approx(stat[k].x - top);
+              if (weight != 0.f) sum = fmaf(weight, stat[k].y, sum);
+              weights[k * N + r] = weight;
+            }
+            m = top;
+          }
+          soft_sync();
+#pragma unroll
+          for (int c = 0; c < kMine; ++c) {
+            const float weight = weights[col0 + c];
+            o[c] = weight == 0.f ? 0u : __float_as_uint(fmaf(weight, __uint_as_float(o[c]), 0.f));
+          }
+          for (uint32_t k = 1; x.first + k <= x.last; ++k) {
+            const float* from = partial_of<D>(a, x.first + k, 0) + col0 * D + e;
+            float part[kMine];
+#pragma unroll
+            for (int c = 0; c < kMine; ++c) part[c] = row_at[col0 + c] != kNowhere && e < D ? __ldcg(from + c * D) : 0.f;
+#pragma unroll
+            for (int c = 0; c < kMine; ++c) {
+              const float weight = weights[k * N + col0 + c];
+              if (weight != 0.f) o[c] = __float_as_uint(fmaf(weight, part[c], __uint_as_float(o[c])));
+            }
+          }
+          soft_sync();  // the weights have been read
+        }
+        if (row_there) {
+          keep[r] = inverse_of(sum);
+          if (p.lse && PREBA_IN_RANGE(p.status, q.row + j < p.tokens && h < p.heads_q))
+            p.lse[static_cast<uint64_t>(q.row + j) * p.heads_q + h] = row_lse(m, sum);
+        }
+        soft_sync();
+        // turned around in shared memory (nobody reads P now), so that 16 bytes of a row are stored at a time
+        T* turned = reinterpret_cast<T*>(smem + L::kP);
+        if (e < D) {
+#pragma unroll
+          for (int c = 0; c < kMine; ++c) turned[(col0 + c) * D + e] = result_of<T>(__uint_as_float(o[c]), keep[col0 + c]);
+        }
+        soft_sync();
+#pragma unroll
+        for (int i = 0; i < N * D / 8; i += kSoftThreads) {
+          const int c = (i + r) / (D / 8), at = (i + r) % (D / 8) * 8;
+          if (row_at[c] != kNowhere && at < static_cast<int>(p.head_dim))
+            *reinterpret_cast<uint4*>(static_cast<T*>(p.out) + row_at[c] + at) = *reinterpret_cast<const uint4*>(turned + c * D + at);
         }
       } else {
-        if (r < DP) {
+        float* part = partial_of<D>(a, blockIdx.x, begins);
+        if (row_there) reinterpret_cast<float2*>(part + kFewRows * D)[r] = make_float2(marked(m, sum), sum);
+        if (e < D) {
 #pragma unroll
-          for (int c = 0; c < N; ++c)
-            if (c < rows) part[c * DP + r] = __uint_as_float(o[c]);
+          for (int c = 0; c < kMine; ++c)
+            if (row_at[col0 + c] != kNowhere) part[(col0 + c) * D + e] = __uint_as_float(o[c]);
         }
-        if (r == 0) {
-          const uint32_t start = w.unit - w.count - w.tile;  // of the (request, key head)
-          ctl.pieces[piece] = {1, w.request, w.head, start / run.per, (start + w.tiles - 1) / run.per};
+        if (w.unit < w.end) {
+          pending = first_counted = true;
+          pending_piece = x;
+        } else {
+          if (first_counted) counted(0);
+          first_counted = false;
+          __threadfence();
+          soft_sync();
+          pending_piece = x;
+          count_piece();
+          counted(1);
         }
       }
       soft_sync();  // what lies in shared memory has been read
     }
     if (!ok) report(p.status, PREBA_ERR_TIMEOUT);
+    if (first_counted) {
+      counted(0);
+      soft_sync();
+    }
 
     // ---- join the CTAs: whoever finishes a (request, key head) last adds its pieces up
-    if (ctl.pieces[0].live || ctl.pieces[1].live) {
+    if (ctl.joins[0] || ctl.joins[1]) {
       __threadfence();
-      soft_sync();
-      uint32_t* counters = static_cast<uint32_t*>(p.workspace);
-      if (r < 2) {
-        const piece_t& x = ctl.pieces[r];
-        uint32_t last = 0;
-        if (x.live) {
-          last = atomicAdd(&counters[x.first], 1) == x.last - x.first;
-          if (last) counters[x.first] = 0;  // as the next call wants it
-          __threadfence();
-        }
-        ctl.joins[r] = last;
-      }
-      soft_sync();
 #pragma unroll 1
       for (int i = 0; i < 2; ++i) {
         if (!ctl.joins[i]) continue;
         const piece_t x = ctl.pieces[i];
         request_t q;
         load_packed(p, a.cu_k, a.states, x.request, q);
-        const int32_t rows = q.rows * a.group;
-        // a thread per element, rows in turn; pieces in the order of the states.  The first CTA's piece begins the
-        // (request, key head) and lies in its slot 1, the others in slot 0
-#pragma unroll 1
-        for (int c = DP == 64 ? r / 64 : 0; c < rows; c += DP == 64 ? 2 : 1) {
-          const int e = r % DP;
-          float top = -INFINITY, sum = 0.f, acc = 0.f;
-#pragma unroll 1
-          for (uint32_t k = x.first; k <= x.last; k += 8) {
-            float2 stat[8];
-            float part[8];
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-              const uint32_t cta = min(k + u, x.last);  // the last one again: it is not counted
-              const float* from = partial_of<DP>(a, cta, cta == x.first);
-              stat[u] = __ldcg(reinterpret_cast<const float2*>(from + kFewRows * DP) + c);
-              part[u] = __ldcg(from + c * DP + e);
+        const uint32_t rows = q.rows * a.group, count = x.last - x.first + 1;
+        // The first CTA's piece begins the (request, key head) and lies in its slot 1, the others in slot 0.  A thread per row
+        // makes weights of the pieces' maxima and sums, in the order of the states; they lie where the tiles were
+        float2* stat = reinterpret_cast<float2*>(smem);  // of piece and column: maximum and sum, then weight
+        static_assert(kMaxTileCtas * N * sizeof(float2) <= L::kP, "room for the weights");
+        if (r < N) {
+          const uint32_t kv_head = H * x.head + r / R, in_head = r % R;
+          const uint32_t j = in_head / a.group, h = kv_head * a.group + in_head - j * a.group;
+          row_at[r] = kNowhere;
+          if (in_head < rows && kv_head < p.heads_kv && PREBA_IN_RANGE(p.status, q.row + j < p.tokens && h < p.heads_q)) {
+            float top = -INFINITY, sum = 0.f;
+#pragma unroll 8
+            for (uint32_t k = 0; k < count; ++k) {
+              const float2 v = __ldcg(reinterpret_cast<const float2*>(partial_of<D>(a, x.first + k, k == 0) + kFewRows * D) + r);
+              stat[k * N + r] = v;
+              top = fmaxf(top, v.x);
             }
-            float to = top;
+            for (uint32_t k = 0; k < count; ++k) {
+              const float2 v = stat[k * N + r];
+              const float weight = v.x == -INFINITY ? 0.f : exp2_approx(v.x - top);
+              if (weight != 0.f) sum = fmaf(weight, v.y, sum);
+              stat[k * N + r].x = weight;
+            }
+            keep[r] = inverse_of(sum);
+            row_at[r] = (q.row + j) * p.out_stride[0] + h * p.out_stride[1];
+            if (p.lse) p.lse[static_cast<uint64_t>(q.row + j) * p.heads_q + h] = row_lse(top, sum);
+          }
+        }
+        soft_sync();
+        // four elements of a row each, several rows and pieces on the way together
+        constexpr int kEach = N * D / 4 / kSoftThreads, kGo = kEach < 4 ? kEach : 4;
+#pragma unroll 1
+        for (int i0 = 0; i0 < kEach; i0 += kGo) {
+          float4 acc[kGo];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) to = fmaxf(to, stat[u].x);
-            const float keep = to == -INFINITY ? 0.f : exp2_approx(top - to);
-            top = to;
-            sum *= keep, acc *= keep;
+          for (int i = 0; i < kGo; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+          for (uint32_t k = 0; k < count; ++k) {
+            const float* from = partial_of<D>(a, x.first + k, k == 0);
+            float4 v[kGo];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
-              const float weight = k + u > x.last || stat[u].x == -INFINITY ? 0.f : exp2_approx(stat[u].x - to);
-              if (weight != 0.f) {  // a piece that saw nothing left no sums
-                sum = fmaf(weight, stat[u].y, sum);
-                acc = fmaf(weight, part[u], acc);
-              }
+            for (int i = 0; i < kGo; ++i) {
+              const int at = (i0 + i) * kSoftThreads + r, c = at / (D / 4);
+              v[i] = row_at[c] != kNowhere ? __ldcg(reinterpret_cast<const float4*>(from) + at) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+#pragma unroll
+            for (int i = 0; i < kGo; ++i) {
+              const int c = ((i0 + i) * kSoftThreads + r) / (D / 4);
+              const float weight = row_at[c] != kNowhere ? stat[k * N + c].x : 0.f;
+              if (weight == 0.f) continue;  // a piece that saw nothing left no sums
+              acc[i].x = fmaf(weight, v[i].x, acc[i].x);
+              acc[i].y = fmaf(weight, v[i].y, acc[i].y);
+              acc[i].z = fmaf(weight, v[i].z, acc[i].z);
+              acc[i].w = fmaf(weight, v[i].w, acc[i].w);
             }
           }
-          const uint32_t j = c / a.group, h = x.head * a.group + c - j * a.group, tok = q.row + j;
-          if (!PREBA_IN_RANGE(p.status, tok < p.tokens)) continue;
-          if (e < static_cast<int>(p.head_dim))
-            static_cast<T*>(p.out)[tok * p.out_stride[0] + h * p.out_stride[1] + e] = result_of<T>(acc, inverse_of(sum));
-          if (p.lse && e == 0) p.lse[static_cast<uint64_t>(tok) * p.heads_q + h] = row_lse(top, sum);
+#pragma unroll
+          for (int i = 0; i < kGo; ++i) {
+            const int at = (i0 + i) * kSoftThreads + r, c = at / (D / 4), e = at % (D / 4) * 4;
+            if (row_at[c] == kNowhere || e >= static_cast<int>(p.head_dim)) continue;
+            alignas(8) T v[4] = {result_of<T>(acc[i].x, keep[c]), result_of<T>(acc[i].y, keep[c]), result_of<T>(acc[i].z, keep[c]),
+                                 result_of<T>(acc[i].w, keep[c])};
+            *reinterpret_cast<uint2*>(static_cast<T*>(p.out) + row_at[c] + e) = *reinterpret_cast<const uint2*>(v);
+          }
         }
+        soft_sync();  // the other (request, key head) has weights of its own
       }
     }
   }
@@ -669,19 +823,27 @@ uint64_t cross_workspace(uint32_t n, uint32_t tokens, uint32_t group, uint32_t h
   return kCounterBytes + std::max(few, tiles_workspace(n, tokens, group, head_dim));
 }
 
-template <typename T, int DP, int N> cudaError_t launch_cross(const cross_args& a, cudaStream_t stream) {
-  using L = layout<DP, N>;
-  CUtensorMap map_k, map_v;
-  cudaError_t err = states_map(&map_k, a.p, a.states, a.p.k_cache, a.p.k_stride, kStateRows);
+template <typename T, int D, int H, int R> cudaError_t launch_cross(cross_args& a, cudaStream_t stream) {
+  using L = layout<D, H, R>;
+  a.heads = (a.p.heads_kv + H - 1) / H;
+  CUtensorMap map_q, map_k, map_v;
+  const uint64_t dims_q[4] = {a.p.head_dim, a.p.heads_q, a.p.tokens, 1};
+  const uint64_t strides_q[3] = {a.p.q_stride[1], a.p.q_stride[0], 0};
+  const uint32_t box_q[2] = {a.group, a.q_rows};
+  cudaError_t err = tensor_map(&map_q, a.p.dtype, a.p.q, dims_q, strides_q, box_q);
+  if (err == cudaSuccess) err = states_map(&map_k, a.p, a.states, a.p.k_cache, a.p.k_stride, kStateRows);
   if (err == cudaSuccess) err = states_map(&map_v, a.p, a.states, a.p.v_cache, a.p.v_stride, kStateRows);
   if (err == cudaSuccess)
-    err = cudaFuncSetAttribute(cross_kernel<T, DP, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes);
+    err = cudaFuncSetAttribute(cross_kernel<T, D, H, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes);
   if (err != cudaSuccess) return err;
-  return launch_chained(cross_kernel<T, DP, N>, a.grid, kThreads, L::kBytes, stream, map_k, map_v, a);
+  return launch_chained(cross_kernel<T, D, H, R>, a.grid, kThreads, L::kBytes, stream, map_q, map_k, map_v, a);
 }
-template <typename T, int DP> cudaError_t launch_cross(const cross_args& a, uint32_t rows, cudaStream_t stream) {
-  return rows <= 16 ? launch_cross<T, DP, 16>(a, stream) : rows <= 32 ? launch_cross<T, DP, 32>(a, stream)
-                                                                      : launch_cross<T, DP, 64>(a, stream);
+template <typename T> cudaError_t launch_few(cross_args& a, uint32_t rows, cudaStream_t stream) {
+  if (a.p.head_dim <= 64)
+    return rows <= 16 ? launch_cross<T, 64, 2, 16>(a, stream) : rows <= 32 ? launch_cross<T, 64, 2, 32>(a, stream)
+                                                                           : launch_cross<T, 64, 1, 64>(a, stream);
+  return rows <= 16 ? launch_cross<T, 128, 1, 16>(a, stream) : rows <= 32 ? launch_cross<T, 128, 1, 32>(a, stream)
+                                                                          : launch_cross<T, 128, 1, 64>(a, stream);
 }
 
 bool base_ok(const void* base, const uint64_t* strides) {
@@ -714,7 +876,7 @@ extern "C" int preba_cross_attend(const preba_cross_attend_t* req, void* stream)
       !strides_used(c.q_stride, c.tokens, c.heads_q) || !strides_used(c.k_stride, c.states, c.heads_kv) ||
       !strides_used(c.v_stride, c.states, c.heads_kv) || !c.cu_q || !c.cu_k || c.max_q == 0 || c.states == 0 ||
       c.states > PREBA_PAGES_MAX_KEYS || (c.dtype != PREBA_F16 && c.dtype != PREBA_BF16) ||
-      static_cast<double>(c.heads_kv) * (c.n + c.states / 128.0) > kMostUnits || !(c.scale > 0.f) || !(c.scale < INFINITY) ||
+      static_cast<double>(c.heads_kv) * (2.0 * c.n + c.states / 128.0) > kMostUnits || !(c.scale > 0.f) || !(c.scale < INFINITY) ||
       pairs_at_most(c.n, c.tokens, c.heads_q / c.heads_kv) * c.heads_kv > INT32_MAX || !c.workspace ||
       (reinterpret_cast<uintptr_t>(c.workspace) & 15))
     return PREBA_ERR_INVALID_ARG;
@@ -752,9 +914,7 @@ extern "C" int preba_cross_attend(const preba_cross_attend_t* req, void* stream)
   const uint64_t rows = static_cast<uint64_t>(group) * p.max_q;
   if (rows > kFewRows)
     return finish(launch_packed_tiles(p, c.cu_k, c.seen, c.states, sms, static_cast<uint8_t*>(c.workspace) + kCounterBytes, s));
-  const cross_args a{p, c.cu_k, c.seen, c.states, group, static_cast<uint32_t>(std::min(sms, kMaxTileCtas))};
-  const uint32_t few = static_cast<uint32_t>(rows);
-  if (c.dtype == PREBA_F16)
-    return finish(c.head_dim <= 64 ? launch_cross<__half, 64>(a, few, s) : launch_cross<__half, 128>(a, few, s));
-  return finish(c.head_dim <= 64 ? launch_cross<__nv_bfloat16, 64>(a, few, s) : launch_cross<__nv_bfloat16, 128>(a, few, s));
+  cross_args a{p, c.cu_k, c.seen, c.states, group, static_cast<uint32_t>(std::min(sms, kMaxTileCtas)), p.max_q, 0};
+  return finish(c.dtype == PREBA_F16 ? launch_few<__half>(a, static_cast<uint32_t>(rows), s)
+                                     : launch_few<__nv_bfloat16>(a, static_cast<uint32_t>(rows), s));
 }
