@@ -158,7 +158,7 @@ int preba_beam_select(const preba_beam_select_t* req, void* stream);
  *   preba_beam_pages_query  bytes of workspace (host only), as for preba_beam_select.
  * Errors: PREBA_ERR_INVALID_ARG (NULL, n, beams or table_width 0, n * beams above PREBA_PAGES_MAX_REQUESTS, beams above
  * PREBA_BEAMS_MAX, page_size not a power of two in 8 .. PREBA_PAGES_MAX_PAGE, pages * page_size above 2^31 - 1, a stride
- * below table_width, table_width * page_size above 2^31 - 1, table_out == table, free_left == free_count, copies
+ * below table_width, table_width * page_size above 2^31 - 1, n * beams * table_width above 2^32 - 1, table_out == table, free_left == free_count, copies
  * or the workspace not 16-byte aligned), PREBA_ERR_BUFFER_TOO_SMALL (workspace), PREBA_ERR_CUDA.
  */
 typedef struct {

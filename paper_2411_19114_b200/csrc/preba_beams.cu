@@ -24,95 +24,169 @@ using attend::report;
 constexpr int kSegmentWords = 512;  // of 32 bits
 constexpr int kLaneWords = kSegmentWords / 32;
 constexpr int kScanThreads = 256, kChooseThreads = 512;
+constexpr int kScanBlocks = 4;      // on an SM
 constexpr int kChooseWarps = kChooseThreads / 32;
 
 template <typename T> constexpr int kPerWord = 4 / sizeof(T);
 template <typename T> constexpr int kSegment = kSegmentWords * kPerWord<T>;  // elements
 template <typename T> constexpr int kLane = kLaneWords * kPerWord<T>;        // elements of a lane
+constexpr float kFar = 65536.f;      // numbers beyond this have less exact exponents
+template <typename T> constexpr uint32_t kNothing = 0xff800000u;             // -inf in every element of a word
+template <> constexpr uint32_t kNothing<__half> = 0xfc00fc00u;
+template <> constexpr uint32_t kNothing<__nv_bfloat16> = 0xff80ff80u;
 
 struct select_args {
   preba_beam_select_t p;
   uint32_t segments;  // of a row
-  float2* parts;      // of every segment: maximum, sum of exponentials
+  float2* parts;      // of every segment: maximum, sum of the exponentials beside it
 };
 
-// The place in its segment of a lane's i-th element, ascending in i.  Vectors of 16 bytes where every row begins at a
+// The place in its segment of a lane's i-th element, ascending in i.  Vectors of 16 bytes (Vec) where every row begins at a
 // multiple of 16; else words, lane by lane.  All rows of a call are read alike, so that equal rows have equal sums.
 template <typename T, bool Vec> __device__ __forceinline__ uint32_t place(int i) {
   constexpr int per = kPerWord<T>;
   const uint32_t lane = threadIdx.x & 31, w = i / per;
-  const uint32_t word = Vec ? (w / 4) * 128 + lane * 4 + w % 4 : w * 32 + lane;
-  return word * per + i % per;
+  return (Vec ? w / 4 * 128 + lane * 4 + w % 4 : w * 32 + lane) * per + i % per;
 }
 
-__device__ __forceinline__ float number(float v) { return v; }
-__device__ __forceinline__ float number(__half v) { return __half2float(v); }
-__device__ __forceinline__ float number(__nv_bfloat16 v) { return __bfloat162float(v); }
-template <typename T> __device__ __forceinline__ void unpack(uint32_t w, float* x);
-template <> __device__ __forceinline__ void unpack<float>(uint32_t w, float* x) { x[0] = __uint_as_float(w); }
-template <> __device__ __forceinline__ void unpack<__half>(uint32_t w, float* x) {
-  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
-  x[0] = f.x, x[1] = f.y;
+template <typename T> __device__ __forceinline__ float element(uint32_t w, int i);
+template <> __device__ __forceinline__ float element<float>(uint32_t w, int) { return __uint_as_float(w); }
+template <> __device__ __forceinline__ float element<__half>(uint32_t w, int i) {
+  const __half2 h = *reinterpret_cast<const __half2*>(&w);
+  return i ? __high2float(h) : __low2float(h);
 }
-template <> __device__ __forceinline__ void unpack<__nv_bfloat16>(uint32_t w, float* x) {
-  x[0] = __uint_as_float(w << 16), x[1] = __uint_as_float(w & 0xffff0000u);
+template <> __device__ __forceinline__ float element<__nv_bfloat16>(uint32_t w, int i) {
+  return __uint_as_float(i ? w & 0xffff0000u : w << 16);
+}
+// The larger elements of two words; what is not a number is left out.
+template <typename T> __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b);
+template <> __device__ __forceinline__ uint32_t larger<float>(uint32_t a, uint32_t b) {
+  return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+}
+template <> __device__ __forceinline__ uint32_t larger<__half>(uint32_t a, uint32_t b) {
+  const __half2 m = __hmax2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&m);
+}
+template <> __device__ __forceinline__ uint32_t larger<__nv_bfloat16>(uint32_t a, uint32_t b) {
+  const __nv_bfloat162 m = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&m);
 }
 
-// A lane's elements of segment s of a row; what is behind the vocabulary or not allowed is -inf.
+// Puts -inf in the place of what is behind the vocabulary (from the `left`-th element on) or not allowed: a lane holds 32 of the
+// segment's bits, and the elements of a word, or of a vector, lie in the same ones.
 template <typename T, bool Vec>
-__device__ __forceinline__ void load_segment(const select_args& a, uint32_t row, uint32_t s, float (&x)[kLane<T>]) {
-  const preba_beam_select_t& p = a.p;
+__device__ __forceinline__ void drop(uint32_t (&w)[kLaneWords], uint32_t left, bool masked, uint32_t bits) {
   constexpr int per = kPerWord<T>;
-  const uint32_t first = s * kSegment<T>;
-  const T* from = static_cast<const T*>(p.logits) + row * p.row_stride + first;
-  const uint32_t left = p.vocab - first;  // at least 1
-  if (left >= kSegment<T>) {
-    if (Vec) {
+  if (left >= kSegment<T> && !masked) return;
 #pragma unroll
-      for (int w = 0; w < kLaneWords; w += 4) {
-        const uint4 v = __ldg(reinterpret_cast<const uint4*>(from + place<T, Vec>(w * per)));
-        unpack<T>(v.x, x + w * per), unpack<T>(v.y, x + (w + 1) * per);
-        unpack<T>(v.z, x + (w + 2) * per), unpack<T>(v.w, x + (w + 3) * per);
-      }
-    } else if (per == 1 || !(reinterpret_cast<uintptr_t>(from) & 2)) {
-#pragma unroll
-      for (int w = 0; w < kLaneWords; ++w)
-        unpack<T>(__ldg(reinterpret_cast<const uint32_t*>(from + place<T, Vec>(w * per))), x + w * per);
-    } else {
-#pragma unroll
-      for (int i = 0; i < kLane<T>; ++i) x[i] = number(from[place<T, Vec>(i)]);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < kLane<T>; ++i) {
-      const uint32_t e = place<T, Vec>(i);
-      x[i] = e < left ? number(from[e]) : -INFINITY;
-    }
-  }
-  if (p.allowed) {
-    // elements of a word lie in the same word of bits, and so do those of a vector
-    const uint32_t* bits = p.allowed + row * p.allowed_stride + first / 32;
-    constexpr int step = Vec ? 4 * per : per;
-#pragma unroll
-    for (int i = 0; i < kLane<T>; i += step) {
-      const uint32_t e = place<T, Vec>(i);
-      const uint32_t word = e < left ? __ldg(bits + e / 32) >> (e % 32) : 0;
-#pragma unroll
-      for (int k = 0; k < step; ++k)
-        if (!(word >> k & 1)) x[i + k] = -INFINITY;
-    }
+  for (int i = 0; i < kLaneWords; ++i) {
+    const uint32_t e = place<T, Vec>(i * per);
+    uint32_t keep = ~0u;
+    if (masked) keep = __shfl_sync(kFull, bits, e / 32) >> (e % 32);
+    if (!(keep & 1) || e >= left) w[i] = per == 1 ? kNothing<T> : (w[i] & 0xffff0000u) | (kNothing<T> & 0xffffu);
+    if (per == 2 && (!(keep & 2) || e + 1 >= left)) w[i] = (w[i] & 0xffffu) | (kNothing<T> & 0xffff0000u);
   }
 }
+// A lane's words of segment s of a row.  fetch() has the loads on the way, finish() makes of them what they stand for.
+template <typename T, bool Vec> struct segment_t {
+  uint32_t w[kLaneWords], extra, bits;
+  bool odd;  // words as they lie in memory, of a row of 16-bit elements that begins in the middle of one
 
-__device__ __forceinline__ float warp_max(float v) {
+  __device__ __forceinline__ void fetch(const select_args& a, uint32_t row, uint32_t s) {
+    const preba_beam_select_t& p = a.p;
+    constexpr int per = kPerWord<T>;
+    const uint32_t lane = threadIdx.x & 31, first = s * kSegment<T>, left = p.vocab - first;  // left: at least 1
+    const T* from = static_cast<const T*>(p.logits) + row * p.row_stride + first;
+    const bool middle = !Vec && per == 2 && (reinterpret_cast<uintptr_t>(from) & 2);
+    // such a row's first and last words have a neighbour's element in them, or nobody's
+    const bool edge = left < kSegment<T> || (middle && (s == 0 || left == kSegment<T>));
+    odd = middle && !edge;
+    if (edge) {
 #pragma unroll
-  for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(kFull, v, o));
-  return v;
+      for (int i = 0; i < kLaneWords; ++i) {
+        const uint32_t e = place<T, Vec>(i * per);
+        w[i] = 0;
+        if (per == 1) {
+          if (e < left) w[i] = __ldg(reinterpret_cast<const uint32_t*>(from) + e);
+        } else {
+          const uint16_t* half = reinterpret_cast<const uint16_t*>(from) + e;
+          if (e < left) w[i] = __ldg(half);
+          if (e + 1 < left) w[i] |= static_cast<uint32_t>(__ldg(half + 1)) << 16;
+        }
+      }
+    } else if (Vec) {
+#pragma unroll
+      for (int i = 0; i < kLaneWords; i += 4) {
+        const uint4 v = __ldg(reinterpret_cast<const uint4*>(from) + 8 * i + lane);
+        w[i] = v.x, w[i + 1] = v.y, w[i + 2] = v.z, w[i + 3] = v.w;
+      }
+    } else {
+      const uint32_t* words = reinterpret_cast<const uint32_t*>(from - (odd ? 1 : 0));
+#pragma unroll
+      for (int i = 0; i < kLaneWords; ++i) w[i] = __ldg(words + i * 32 + lane);
+      if (odd) extra = __ldg(words + kSegmentWords);
+    }
+    bits = bits_of(p, row, first);
+  }
+
+  // What of a row's bits belongs to a lane in the segment that begins with element `first`.
+  static __device__ __forceinline__ uint32_t bits_of(const preba_beam_select_t& p, uint32_t row, uint32_t first) {
+    const uint32_t lane = threadIdx.x & 31;
+    if (!p.allowed || lane >= kSegment<T> / 32 || first + lane * 32 >= p.vocab) return 0;
+    return __ldg(p.allowed + row * p.allowed_stride + first / 32 + lane);
+  }
+
+  __device__ __forceinline__ void finish(const select_args& a, uint32_t s) {
+    if (odd) {
+      // the second half of a word and the first half of the next, which is the next lane's
+      const uint32_t lane = threadIdx.x & 31;
+      uint32_t next = __shfl_sync(kFull, w[0], (lane + 1) & 31);
+#pragma unroll
+      for (int i = 0; i < kLaneWords; ++i) {
+        const uint32_t after = i + 1 < kLaneWords ? __shfl_sync(kFull, w[i + 1], (lane + 1) & 31) : extra;
+        w[i] = __funnelshift_r(w[i], lane == 31 ? after : next, 16);
+        next = after;
+      }
+    }
+    drop<T, Vec>(w, a.p.vocab - s * kSegment<T>, a.p.allowed, bits);
+  }
+};
+
+// The largest number of the warp; what is not a number is left out.
+__device__ __forceinline__ float warp_max(float v) {
+  float top;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(top) : "f"(v));
+  return top;
 }
 template <typename N> __device__ __forceinline__ N warp_sum(N v) {
 #pragma unroll
   for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
   return v;
+}
+// Arithmetic on two fp32 numbers at once.
+__device__ __forceinline__ uint64_t two(float a, float b) {
+  uint64_t v;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b));
+  return v;
+}
+__device__ __forceinline__ void apart(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t add_two(uint64_t a, uint64_t b) {
+  uint64_t v;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+  return v;
+}
+__device__ __forceinline__ uint64_t fma_two(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t v;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(a), "l"(b), "l"(c));
+  return v;
+}
+
+// What a word's elements are above a maximum: not above 0, so that its type holds it, rounded where that no longer matters.
+template <typename T> __device__ __forceinline__ uint32_t below(uint32_t w, float top) { return __float_as_uint(__uint_as_float(w) - top); }
+template <> __device__ __forceinline__ uint32_t below<__half>(uint32_t w, float) { return w; }  // never as large
+template <> __device__ __forceinline__ uint32_t below<__nv_bfloat16>(uint32_t w, float top) {
+  const __nv_bfloat162 d = __floats2bfloat162_rn(element<__nv_bfloat16>(w, 0) - top, element<__nv_bfloat16>(w, 1) - top);
+  return *reinterpret_cast<const uint32_t*>(&d);
 }
 
 // Whether a row offers what its logits say: it is there and has not ended.
@@ -120,73 +194,117 @@ __device__ __forceinline__ bool row_live(const preba_beam_select_t& p, uint32_t 
   return !(p.done && p.done[row]) && p.scores[row] != -INFINITY;
 }
 
+// The warps take segments in turn, so that together they read what lies together; the next one is on the way while one is looked
+// at.
 template <typename T, bool Vec>
-__global__ void __launch_bounds__(kScanThreads) scan_kernel(const select_args a) {
+__global__ void __launch_bounds__(kScanThreads, kScanBlocks) scan_kernel(const __grid_constant__ select_args a) {
   const preba_beam_select_t& p = a.p;
+  const uint32_t rows = p.n * p.beams, warps = gridDim.x * (kScanThreads / 32);
+  const uint32_t step_rows = warps / a.segments, step = warps - step_rows * a.segments;
+  const uint32_t unit = blockIdx.x * (kScanThreads / 32) + threadIdx.x / 32;
+  uint32_t row = unit / a.segments, s = unit - row * a.segments;
   chained_begin();
-  const uint32_t lane = threadIdx.x & 31;
-  const uint32_t total = p.n * p.beams * a.segments;
-  const uint32_t stride = gridDim.x * (kScanThreads / 32);
-  for (uint32_t unit = blockIdx.x * (kScanThreads / 32) + threadIdx.x / 32; unit < total; unit += stride) {
-    const uint32_t row = unit / a.segments, s = unit - row * a.segments;
-    if (!row_live(p, row)) continue;
-    float x[kLane<T>];
-    load_segment<T, Vec>(a, row, s, x);
-    float top = x[0];
+  segment_t<T, Vec> next;
+  bool live = row < rows && row_live(p, row);
+  if (live) next.fetch(a, row, s);
+#pragma unroll 1
+  while (row < rows) {
+    segment_t<T, Vec> seg = next;
+    const uint64_t at = static_cast<uint64_t>(row) * a.segments + s;
+    const uint32_t here = s;
+    const bool wanted = live;
+    row += step_rows;
+    s += step;
+    if (s >= a.segments) s -= a.segments, ++row;
+    live = row < rows && row_live(p, row);
+    if (live) next.fetch(a, row, s);
+    if (!wanted) continue;
+    seg.finish(a, here);
+    uint32_t most[4] = {seg.w[0], seg.w[1], seg.w[2], seg.w[3]};
 #pragma unroll
-    for (int i = 1; i < kLane<T>; ++i) top = fmaxf(top, x[i]);
+    for (int i = 4; i < kLaneWords; ++i) most[i % 4] = larger<T>(most[i % 4], seg.w[i]);
+    const uint32_t most1 = larger<T>(larger<T>(most[0], most[1]), larger<T>(most[2], most[3]));
+    float top = element<T>(most1, 0);
+    if (kPerWord<T> == 2) top = fmaxf(top, element<T>(most1, 1));
     top = warp_max(top);
-    const float from = top == -INFINITY ? 0.f : top;  // then all of it is -inf, or not a number
-    float sum = 0.f;
-    // the difference is rounded before it is scaled: what is near the maximum, and counts, is exact
+    // Exponents are x log2(e) - top log2(e), rounded once, beside a rounded product with the maximum whose error is the
+    // same for all and is taken out of the sum.  Where all is -inf, or not a number, beside 0; where that error would be more
+    // than 2^-7, (x - top) log2(e)
+    const bool far = fabsf(top) > kFar;
+    const float beside = far ? 0.f : top * kLog2e, off = far ? 0.f : fmaf(-top, kLog2e, beside);
+    if (far && top > -INFINITY) {
 #pragma unroll
-    for (int i = 0; i < kLane<T>; ++i) sum += exp2_approx((x[i] - from) * kLog2e);
-    sum = warp_sum(sum);
-    if (lane == 0) a.parts[unit] = make_float2(top, sum);
+      for (int i = 0; i < kLaneWords; ++i) seg.w[i] = below<T>(seg.w[i], top);
+    }
+    const uint64_t scale = two(kLog2e, kLog2e), less = two(-beside, -beside);
+    uint64_t sums[2] = {0, 0};
+    constexpr int kStep = 2 / kPerWord<T>;  // words of two elements
+#pragma unroll
+    for (int i = 0; i < kLaneWords; i += kStep) {
+      float z0, z1;
+      apart(fma_two(two(element<T>(seg.w[i], 0), element<T>(seg.w[i + kStep - 1], 1)), scale, less), z0, z1);
+      sums[i / kStep & 1] = add_two(sums[i / kStep & 1], two(exp2_approx(z0), exp2_approx(z1)));
+    }
+    float sum0, sum1;
+    apart(add_two(sums[0], sums[1]), sum0, sum1);
+    const float sum = warp_sum(sum0 + sum1) * exp2_approx(off);
+    if ((threadIdx.x & 31) == 0) a.parts[at] = make_float2(top, sum);
   }
 }
 
-// A candidate: a segment by its maximum, or a token.  `at` is the segment or the token.
+// Candidates: segments by their maxima, or tokens.  `at` is the segment or the token.
 struct candidate_t {
   double rank;
   float x;       // the logit (of a row that is done: 0)
   uint32_t row;  // the beam
   uint32_t at;
 };
-__device__ __forceinline__ bool before(const candidate_t& a, const candidate_t& b) {
-  if (a.rank != b.rank) return a.rank > b.rank;
-  if (a.row != b.row) return a.row < b.row;
-  if (a.x != b.x) return a.x > b.x;
-  return a.at < b.at;
-}
+constexpr uint32_t kCandidateBytes = 8 + 4 + 4 + 4;
+constexpr uint32_t kTeam = 8, kGroups = kChooseThreads / kTeam;  // threads in groups of eight
+static_assert(kGroups >= PREBA_BEAMS_MAX_WIDTH, "the width-th of them has to exist");
+
+// A list of them in shared memory, member by member: ranks decide, the others are looked at where two are equal.
+struct list_t {
+  double* rank;
+  float* x;
+  uint32_t* row;
+  uint32_t* at;
+  __device__ __forceinline__ list_t(uint8_t* base, uint32_t room)
+      : rank(reinterpret_cast<double*>(base)), x(reinterpret_cast<float*>(rank + room)),
+        row(reinterpret_cast<uint32_t*>(x + room)), at(row + room) {}
+  __device__ __forceinline__ void put(uint32_t i, const candidate_t& c) const { rank[i] = c.rank, x[i] = c.x, row[i] = c.row, at[i] = c.at; }
+  __device__ __forceinline__ candidate_t get(uint32_t i) const { return {rank[i], x[i], row[i], at[i]}; }
+  __device__ __forceinline__ bool before(uint32_t i, const candidate_t& c) const {
+    const double r = rank[i];
+    if (r != c.rank) return r > c.rank;
+    if (row[i] != c.row) return row[i] < c.row;
+    if (x[i] != c.x) return x[i] > c.x;
+    return at[i] < c.at;
+  }
+};
 
 struct choose_shared {
   double lse[PREBA_BEAMS_MAX], score[PREBA_BEAMS_MAX], weight[PREBA_BEAMS_MAX];
-  uint32_t live[PREBA_BEAMS_MAX];     // 0: offers nothing, 1: its logits, 2: its end token
-  uint32_t listed, chosen, found;
+  uint32_t live[PREBA_BEAMS_MAX];      // 0: offers nothing, 1: its logits, 2: its end token
+  uint32_t segments[PREBA_BEAMS_MAX];  // of the row's that are listed
+  uint32_t listed, found;
+  double groups[kGroups], floor;       // the best ranks of groups of threads, and the `width`-th of them
   candidate_t best[PREBA_BEAMS_MAX_WIDTH];  // segments
 };
 
-// Candidates of a request at most: segments, the first `width` of each row, or tokens, where the k-th segment can
-// give no more than width - k.
+// Candidates of a request at most: segments, as many as pass a threshold that is close to the `width`-th, or, where more do,
+// `width` of each row; then tokens, where the k-th segment can give no more than width - k.
 __host__ __device__ inline uint32_t candidates_of(uint32_t beams, uint32_t width) {
-  const uint32_t tokens = width * (width + 1) / 2;
-  return beams * width > tokens ? beams * width : tokens;
-}
-
-// One more candidate; their order in the list is that of whoever came first and means nothing.
-__device__ __forceinline__ void add(const preba_beam_select_t& p, candidate_t* list, uint32_t* count, uint32_t room,
-                                    const candidate_t& c) {
-  const uint32_t at = atomicAdd(count, 1);
-  if (PREBA_IN_RANGE(p.status, at < room)) list[at] = c;
+  const uint32_t tokens = width * (width + 1) / 2, rows = beams * width, passed = 16 * width;
+  const uint32_t segments = rows > passed ? rows : passed;
+  return segments > tokens ? segments : tokens;
 }
 
 __device__ __forceinline__ double value_of(const choose_shared& c, uint32_t row, float x) {
   return (static_cast<double>(x) - c.lse[row]) + c.score[row];
 }
 
-// The best candidate of the warp's lanes, `none` lanes taking no part; false if there is none.  In one row: by
-// logit, then place.
+// The best of the lanes' numbers, and where it is; of equals the lowest place.  False if there is none.
 __device__ __forceinline__ bool warp_best(float& x, uint32_t& at) {
   const float top = warp_max(x);
   if (top == -INFINITY) return false;
@@ -195,127 +313,224 @@ __device__ __forceinline__ bool warp_best(float& x, uint32_t& at) {
   return true;
 }
 
+// How many of a list come before one of its entries, by eight threads for each; `take` gets the entry and its place.
+template <typename Take> __device__ __forceinline__ void in_order(const list_t& list, uint32_t count, const Take& take) {
+  const uint32_t member = threadIdx.x % kTeam;
+  for (uint32_t i0 = 0; i0 < count; i0 += kChooseThreads / kTeam) {  // the same for the whole block
+    const uint32_t i = i0 + threadIdx.x / kTeam;
+    const candidate_t mine = list.get(min(i, count - 1));
+    uint32_t ahead = 0;
+#pragma unroll 4
+    for (uint32_t k = member; k < count; k += kTeam) ahead += list.before(k, mine);
+#pragma unroll
+    for (uint32_t o = 1; o < kTeam; o *= 2) ahead += __shfl_xor_sync(kFull, ahead, o);
+    if (member == 0 && i < count) take(mine, ahead);
+  }
+}
+
+constexpr uint32_t kHeld = 8;  // segments of a row that a lane keeps; rows of more are read again each time
+constexpr uint32_t kItems = 4;  // segments of all rows that a thread keeps, likewise
+
 template <typename T, bool Vec>
-__global__ void __launch_bounds__(kChooseThreads) choose_kernel(const select_args a) {
+__global__ void __launch_bounds__(kChooseThreads) choose_kernel(const __grid_constant__ select_args a) {
   extern __shared__ __align__(16) uint8_t choose_smem[];
-  candidate_t* list = reinterpret_cast<candidate_t*>(choose_smem);
   __shared__ choose_shared c;
   const preba_beam_select_t& p = a.p;
   const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint32_t r = blockIdx.x, row0 = r * p.beams, room = candidates_of(p.beams, p.width);
-  if (threadIdx.x == 0) c.listed = c.chosen = c.found = 0;
-  __syncthreads();
+  const list_t list(choose_smem, room);
+  if (threadIdx.x == 0) c.listed = c.found = 0;
   chained_begin();
 
-  // a warp per beam: the sum of its exponentials, then its best segments
+  // a warp per beam: the logarithm of its sum
+  const float2* all_parts = a.parts + static_cast<uint64_t>(row0) * a.segments;
   for (uint32_t b = warp; b < p.beams; b += kChooseWarps) {
     const uint32_t row = row0 + b;
-    const float score = p.scores[row], weight = p.weights ? p.weights[row] : 1.f;
+    const float2* parts = all_parts + b * a.segments;
+    float2 held[kHeld];
+#pragma unroll
+    for (uint32_t k = 0; k < kHeld; ++k)  // of a row that is not live they mean nothing
+      held[k] = lane + 32 * k < a.segments ? __ldcg(parts + lane + 32 * k) : make_float2(-INFINITY, 0.f);
     const bool done = p.done && p.done[row];
-    if (score == -INFINITY) {
-      if (lane == 0) c.live[b] = 0;
-      continue;
-    }
+    const float score = p.scores[row], weight = p.weights ? p.weights[row] : 1.f;
     bool good = score < INFINITY && weight > 0.f && weight < INFINITY;
-    const float2* parts = a.parts + static_cast<uint64_t>(row) * a.segments;
     float top = -INFINITY;
-    double sum = 0, lse = 0;
-    if (!done) {
-      for (uint32_t s = lane; s < a.segments; s += 32) top = fmaxf(top, parts[s].x);
+    double lse = 0;
+    if (!done && score != -INFINITY) {
+#pragma unroll
+      for (uint32_t k = 0; k < kHeld; ++k) top = fmaxf(top, held[k].x);
+      for (uint32_t s = lane + 32 * kHeld; s < a.segments; s += 32) top = fmaxf(top, __ldcg(parts + s).x);
       top = warp_max(top);
-      for (uint32_t s = lane; s < a.segments; s += 32) {
-        const float2 part = parts[s];
-        // a segment of nothing has the sum 0; one of -inf and NaN has a sum that is not a number
-        sum += part.x == -INFINITY ? static_cast<double>(part.y) : static_cast<double>(part.y) * exp(static_cast<double>(part.x) - top);
-      }
+      // a segment of nothing has the sum 0; one of -inf and NaN has a sum that is not a number
+      auto beside = [&](float2 v) {
+        return static_cast<double>(v.x == -INFINITY ? v.y : v.y * exp2_approx((v.x - top) * kLog2e));
+      };
+      double sum = 0;
+#pragma unroll
+      for (uint32_t k = 0; k < kHeld; ++k)
+        if (32 * k < a.segments) sum += beside(held[k]);
+      for (uint32_t s = lane + 32 * kHeld; s < a.segments; s += 32) sum += beside(__ldcg(parts + s));
       sum = warp_sum(sum);
       lse = top + log(sum);
       good = good && (top == -INFINITY ? sum == 0 : lse < INFINITY);  // not a number: false
     }
     if (lane == 0) {
       if (!good) report(p.status, PREBA_ERR_BAD_TABLE);
-      c.live[b] = !good ? 0 : done ? 2 : top > -INFINITY;
+      c.live[b] = !good || score == -INFINITY ? 0 : done ? 2 : top > -INFINITY;
       c.lse[b] = lse;
       c.score[b] = score;
       c.weight[b] = weight;
     }
-    __syncwarp();
-    if (!good) continue;
-    if (done) {
-      if (lane == 0) add(p, list, &c.listed, room, {static_cast<double>(weight) * score, 0.f, b, UINT32_MAX});
-      continue;
-    }
-    // the segments in order, one by one: what follows the one before
-    float last_x = INFINITY;
-    uint32_t last_s = 0;
-    for (uint32_t k = 0; k < p.width; ++k) {
-      float x = -INFINITY;
-      uint32_t at = UINT32_MAX;
-      for (uint32_t s = lane; s < a.segments; s += 32) {
-        const float m = parts[s].x;
-        const bool after = m < last_x || (m == last_x && s > last_s);
-        if (after && m > x) x = m, at = s;
-      }
-      if (!warp_best(x, at)) break;
-      last_x = x, last_s = at;
-      if (lane == 0) add(p, list, &c.listed, room, {c.weight[b] * value_of(c, b, x), x, b, at});
-    }
+  }
+  // the rows' segments, and behind them an end token for each, thread by thread
+  const uint32_t segments = p.beams * a.segments, items = segments + p.beams;
+  float kept[kItems];
+#pragma unroll
+  for (uint32_t k = 0; k < kItems; ++k) {
+    const uint32_t i = threadIdx.x + k * kChooseThreads;
+    kept[k] = i < segments ? __ldcg(&all_parts[i].x) : 0.f;
   }
   __syncthreads();
-
-  // the order of the segments: everyone counts who comes before
-  const uint32_t listed = min(c.listed, room);
-  for (uint32_t i = threadIdx.x; i < listed; i += kChooseThreads) {
-    const candidate_t mine = list[i];
+  auto item = [&](uint32_t i, float x) -> candidate_t {
+    const uint32_t b = i < segments ? i / a.segments : i - segments;
+    const bool there = i < segments ? c.live[b] == 1 && x > -INFINITY : i < items && c.live[b] == 2;
+    if (!there) return {-INFINITY, 0.f, 0, 0};
+    if (i >= segments) return {c.weight[b] * c.score[b], 0.f, b, UINT32_MAX};
+    return {c.weight[b] * value_of(c, b, x), x, b, i - b * a.segments};
+  };
+  auto every_item = [&](const auto& take) {
+#pragma unroll
+    for (uint32_t k = 0; k < kItems; ++k)
+      if (k * kChooseThreads < items) take(item(threadIdx.x + k * kChooseThreads, kept[k]));
+    for (uint32_t i = threadIdx.x + kItems * kChooseThreads; i < items; i += kChooseThreads)
+      take(item(i, i < segments ? __ldcg(&all_parts[i].x) : 0.f));
+  };
+  // As many groups of threads as are wanted have a candidate of the rank of the `width`-th best group, or a better one: the
+  // others need not be looked at
+  double best_rank = -INFINITY;
+  every_item([&](const candidate_t& x) { best_rank = fmax(best_rank, x.rank); });
+#pragma unroll
+  for (uint32_t o = 1; o < kTeam; o *= 2) best_rank = fmax(best_rank, __shfl_xor_sync(kFull, best_rank, o));
+  if (threadIdx.x % kTeam == 0) c.groups[threadIdx.x / kTeam] = best_rank;
+  __syncthreads();
+  {
+    const uint32_t g = threadIdx.x / kTeam;
     uint32_t ahead = 0;
-    for (uint32_t k = 0; k < listed; ++k) ahead += before(list[k], mine);
-    if (ahead < p.width) c.best[ahead] = mine;
+#pragma unroll
+    for (uint32_t k = threadIdx.x % kTeam; k < kGroups; k += kTeam) ahead += c.groups[k] > best_rank || (c.groups[k] == best_rank && k < g);
+#pragma unroll
+    for (uint32_t o = 1; o < kTeam; o *= 2) ahead += __shfl_xor_sync(kFull, ahead, o);
+    if (threadIdx.x % kTeam == 0 && ahead == p.width - 1) c.floor = best_rank;
   }
-  if (threadIdx.x == 0) c.chosen = min(listed, p.width);
   __syncthreads();
+  const double floor = c.floor;
+  every_item([&](const candidate_t& x) {
+    if (!(x.rank >= floor) || x.rank == -INFINITY) return;
+    const uint32_t at = atomicAdd(&c.listed, 1);
+    if (at < room) list.put(at, x);
+  });
+  __syncthreads();
+  uint32_t slots = c.listed;
+  if (slots > room) {
+    // Too many are equal to it.  A row's segments in order, one by one: what follows the one before
+    for (uint32_t b = warp; b < p.beams; b += kChooseWarps) {
+      float last_x = INFINITY;
+      uint32_t last_s = 0, n = 0;
+      for (; n < p.width && c.live[b] == 1; ++n) {
+        float x = -INFINITY;
+        uint32_t at = UINT32_MAX;
+        for (uint32_t s = lane; s < a.segments; s += 32) {
+          const float m = __ldcg(&all_parts[b * a.segments + s].x);
+          const bool after = m < last_x || (m == last_x && s > last_s);
+          if (after && m > x) x = m, at = s;
+        }
+        if (!warp_best(x, at)) break;
+        last_x = x, last_s = at;
+        if (lane == 0 && PREBA_IN_RANGE(p.status, b * p.width + n < room))
+          list.put(b * p.width + n, {c.weight[b] * value_of(c, b, x), x, b, at});
+      }
+      if (c.live[b] == 2) {
+        if (lane == 0) list.put(b * p.width, {c.weight[b] * c.score[b], 0.f, b, UINT32_MAX});
+        n = 1;
+      }
+      for (uint32_t k = n + lane; k < p.width; k += 32) list.put(b * p.width + k, {-INFINITY, 0.f, UINT32_MAX, b * p.width + k});
+    }
+    slots = p.beams * p.width;
+    __syncthreads();
+  }
+  in_order(list, slots, [&](const candidate_t& mine, uint32_t ahead) {
+    if (ahead < p.width) c.best[ahead] = mine;
+  });
+  __syncthreads();
+  const uint32_t listed = __syncthreads_count(threadIdx.x < min(slots, p.width) && c.best[threadIdx.x].rank > -INFINITY);
 
   // what the best segments hold, as far as it can be among the first: a warp per segment
-  const uint32_t chosen = c.chosen;
+  const uint32_t chosen = min(listed, p.width);
   const bool full = chosen == p.width;  // nothing after the last segment's maximum is among the first
+  auto add = [&](const candidate_t& x) {  // their order in the list is that of whoever came first and means nothing
+    const uint32_t at = atomicAdd(&c.found, 1);
+    if (PREBA_IN_RANGE(p.status, at < room)) list.put(at, x);
+  };
   for (uint32_t k = warp; k < chosen; k += kChooseWarps) {
     const candidate_t seg = c.best[k];
     if (seg.at == UINT32_MAX) {
-      if (lane == 0) add(p, list, &c.found, room, {seg.rank, 0.f, seg.row, static_cast<uint32_t>(p.end_token)});
+      if (lane == 0) add({seg.rank, 0.f, seg.row, static_cast<uint32_t>(p.end_token)});
       continue;
     }
-    float x[kLane<T>];
-    load_segment<T, Vec>(a, row0 + seg.row, seg.at, x);
-    const double floor = c.best[chosen - 1].rank;
+    segment_t<T, Vec> words;
+    words.fetch(a, row0 + seg.row, seg.at);
+    const double last = c.best[chosen - 1].rank, weight = c.weight[seg.row];
+    // the least logit that may do, less what it may be off by
+    const double level = last * (1.f / static_cast<float>(weight)), least = level - c.score[seg.row] + c.lse[seg.row];
+    const float least_x =
+        full ? static_cast<float>(least - 1e-6 * (1 + fabs(level) + fabs(c.score[seg.row]) + fabs(c.lse[seg.row]))) : -INFINITY;
+    words.finish(a, seg.at);
+    uint32_t enough = 0;  // a bit for each of the lane's elements
+#pragma unroll
+    for (int i = 0; i < kLane<T>; ++i)
+      if (element<T>(words.w[i / kPerWord<T>], i % kPerWord<T>) >= least_x) enough |= 1u << i;
+    if (__reduce_add_sync(kFull, __popc(enough)) <= p.width - k) {
+      // few enough to be listed as they are
+      for (; enough; enough &= enough - 1) {
+        const int which = __ffs(enough) - 1;
+        float x = 0.f;
+        uint32_t at = 0;
+#pragma unroll
+        for (int u = 0; u < kLane<T>; ++u)
+          if (u == which) x = element<T>(words.w[u / kPerWord<T>], u % kPerWord<T>), at = place<T, Vec>(u);
+        if (x > -INFINITY) add({weight * value_of(c, seg.row, x), x, seg.row, seg.at * kSegment<T> + at});
+      }
+      continue;
+    }
+    uint32_t taken = 0;  // a bit for each of the lane's elements
     for (uint32_t j = k; j < p.width; ++j) {
       float best = -INFINITY;
-      uint32_t at = UINT32_MAX;
+      uint32_t at = UINT32_MAX, which = 0;
 #pragma unroll
-      for (int i = 0; i < kLane<T>; ++i)
-        if (x[i] > best) best = x[i], at = place<T, Vec>(i);
+      for (int i = 0; i < kLane<T>; ++i) {
+        const float x = element<T>(words.w[i / kPerWord<T>], i % kPerWord<T>);
+        if (x > best && !(taken >> i & 1)) best = x, at = place<T, Vec>(i), which = i;
+      }
+      const uint32_t own = at;
       if (!warp_best(best, at)) break;
-      const double rank = c.weight[seg.row] * value_of(c, seg.row, best);
-      if (full && rank < floor) break;
-#pragma unroll
-      for (int i = 0; i < kLane<T>; ++i)
-        if (place<T, Vec>(i) == at) x[i] = -INFINITY;
-      if (lane == 0) add(p, list, &c.found, room, {rank, best, seg.row, seg.at * kSegment<T> + at});
+      const double rank = weight * value_of(c, seg.row, best);
+      if (full && rank < last) break;
+      if (own == at) taken |= 1u << which;
+      if (lane == 0) add({rank, best, seg.row, seg.at * kSegment<T> + at});
     }
   }
   __syncthreads();
 
   const uint32_t found = min(c.found, room);
   const uint64_t out = static_cast<uint64_t>(r) * p.width;
-  for (uint32_t i = threadIdx.x; i < found; i += kChooseThreads) {
-    const candidate_t mine = list[i];
-    uint32_t ahead = 0;
-    for (uint32_t k = 0; k < found; ++k) ahead += before(list[k], mine);
-    if (ahead >= p.width) continue;
+  in_order(list, found, [&](const candidate_t& mine, uint32_t ahead) {
+    if (ahead >= p.width) return;
     const bool done = c.live[mine.row] == 2;
     p.tokens[out + ahead] = static_cast<int32_t>(mine.at);
     p.parents[out + ahead] = static_cast<int32_t>(mine.row);
     p.scores_out[out + ahead] = static_cast<float>(done ? c.score[mine.row] : value_of(c, mine.row, mine.x));
     if (p.done_out) p.done_out[out + ahead] = done || static_cast<int32_t>(mine.at) == p.end_token;
-  }
+  });
   for (uint32_t i = found + threadIdx.x; i < p.width; i += kChooseThreads) {
     p.tokens[out + i] = p.parents[out + i] = -1;
     p.scores_out[out + i] = -INFINITY;
@@ -327,6 +542,13 @@ int finish(cudaError_t err) {
   if (err == cudaSuccess) return PREBA_OK;
   g_last_cuda_error = static_cast<int>(err);
   return PREBA_ERR_CUDA;
+}
+
+int device_sms(int* sms) {
+  int device = 0;
+  cudaError_t err = cudaGetDevice(&device);
+  if (err == cudaSuccess) err = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, device);
+  return finish(err);
 }
 
 bool aligned(const void* p, uintptr_t a) { return !(reinterpret_cast<uintptr_t>(p) & (a - 1)); }
@@ -343,14 +565,14 @@ uint32_t segments_of(uint32_t vocab, int32_t dtype) {
 
 template <typename T, bool Vec> cudaError_t launch_select(const select_args& a, int sms, cudaStream_t stream) {
   const preba_beam_select_t& p = a.p;
-  const uint64_t units = static_cast<uint64_t>(p.n) * p.beams * a.segments;
-  const uint32_t grid = static_cast<uint32_t>(std::min<uint64_t>((units + kScanThreads / 32 - 1) / (kScanThreads / 32), 8ull * sms));
-  cudaError_t err = launch_chained(scan_kernel<T, Vec>, grid, kScanThreads, 0, stream, a);
+  const uint64_t blocks = (static_cast<uint64_t>(p.n) * p.beams * a.segments + kScanThreads / 32 - 1) / (kScanThreads / 32);
+  cudaError_t err = launch_chained(scan_kernel<T, Vec>, static_cast<uint32_t>(std::min(blocks, static_cast<uint64_t>(kScanBlocks) * sms)),
+                                   kScanThreads, 0, stream, a);
   if (err != cudaSuccess) return err;
-  const size_t smem = candidates_of(p.beams, p.width) * sizeof(candidate_t);
+  const size_t smem = candidates_of(p.beams, p.width) * kCandidateBytes;
   if (smem > 40 * 1024) {  // beside 3 KB of its own
     err = cudaFuncSetAttribute(choose_kernel<T, Vec>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                               static_cast<int>(candidates_of(PREBA_BEAMS_MAX, PREBA_BEAMS_MAX_WIDTH) * sizeof(candidate_t)));
+                               static_cast<int>(candidates_of(PREBA_BEAMS_MAX, PREBA_BEAMS_MAX_WIDTH) * kCandidateBytes));
     if (err != cudaSuccess) return err;
   }
   return launch_chained(choose_kernel<T, Vec>, p.n, kChooseThreads, smem, stream, a);
@@ -362,19 +584,18 @@ template <typename T, bool Vec> cudaError_t launch_select(const select_args& a, 
 // Beams share pages only at the same place of their rows, so what is released shows column by column, without
 // counts of holders: a page of a beam that has no child, that no beam with a child has in that column, and that no
 // childless beam before it has.  A first kernel, a block per 256 columns of a request, writes the new rows and
-// lists what is released; a second, one block, numbers all of it and hands it out.
+// lists what is released.  In a second every block adds all requests' numbers up for itself (they are few and come from
+// L2), so that it knows where its own requests' copies and pages stand among all, and hands out without asking another.
 
 constexpr int kColumns = 256;
-constexpr int kHandThreads = 1024;
+constexpr int kHandThreads = 256;
+constexpr uint32_t kAtOnce = 8;  // beams whose entries of a column are on the way together
 
 struct pages_args {
   preba_beam_pages_t p;
   uint32_t page_shift, chunks;  // chunks of columns of a row
-  int32_t* need;      // n: copies of a request, or below 0: refused
-  uint32_t* copies_before;  // n
+  int32_t* need;      // n: copies of a request, or -1: it is at fault
   uint32_t* counts;   // n * chunks: pages released
-  int64_t* before;    // n * chunks: pages released before
-  int32_t* given;     // n * beams: the first released pages
   int32_t* lists;     // n * chunks lists of kColumns * beams pages
 };
 
@@ -391,6 +612,7 @@ __global__ void __launch_bounds__(kColumns) follow_kernel(const pages_args a) {
   const uint32_t c = chunk * kColumns + threadIdx.x;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   chained_begin();
+  const int64_t kept = p.kept ? p.kept[r] : 0;
   bool bad = false;
   if (threadIdx.x < p.beams) {
     const int32_t len = p.lengths[row0 + threadIdx.x], par = p.parents[row0 + threadIdx.x];
@@ -404,16 +626,22 @@ __global__ void __launch_bounds__(kColumns) follow_kernel(const pages_args a) {
   uint32_t parents = 0;  // a bit per beam that has a child
   for (uint32_t b = 0; b < p.beams; ++b)
     if (parent[b] >= 0 && !refused) parents |= 1u << parent[b];
-  for (uint32_t b = 0; b < p.beams; ++b)
-    if (c < held[b]) tile[b * kColumns + threadIdx.x] = p.table[(row0 + b) * p.table_stride + c];
-  // the new rows; every thread reads its own column only
+  // every thread has a column, and reads no other's
+  for (uint32_t b0 = 0; b0 < p.beams; b0 += kAtOnce) {
+    int32_t page[kAtOnce];
+#pragma unroll
+    for (uint32_t k = 0; k < kAtOnce; ++k)
+      page[k] = b0 + k < p.beams && c < held[b0 + k] ? p.table[(row0 + b0 + k) * p.table_stride + c] : 0;
+#pragma unroll
+    for (uint32_t k = 0; k < kAtOnce; ++k)
+      if (b0 + k < p.beams) tile[(b0 + k) * kColumns + threadIdx.x] = page[k];
+  }
   for (uint32_t i = 0; i < p.beams; ++i) {
     const int32_t from = refused ? static_cast<int32_t>(i) : parent[i];
     if (from >= 0 && c < held[from]) p.table_out[(row0 + i) * p.table_out_stride + c] = tile[from * kColumns + threadIdx.x];
   }
   // what this column releases, a bit per beam
   uint32_t gone = 0;
-  const int64_t kept = p.kept ? p.kept[r] : 0;
   if (!refused && c >= kept)
     for (uint32_t b = 0; b < p.beams; ++b) {
       if (parents >> b & 1 || c >= held[b]) continue;
@@ -435,6 +663,7 @@ __global__ void __launch_bounds__(kColumns) follow_kernel(const pages_args a) {
   if (lane == 31) warp_sums[warp] = incl;
   __syncthreads();
   uint32_t at = incl - mine, total = 0;
+#pragma unroll
   for (int w = 0; w < kColumns / 32; ++w) {
     if (w < warp) at += warp_sums[w];
     total += warp_sums[w];
@@ -444,37 +673,38 @@ __global__ void __launch_bounds__(kColumns) follow_kernel(const pages_args a) {
     if (PREBA_IN_RANGE(p.status, at < kColumns * p.beams)) to[at++] = tile[(__ffs(gone) - 1) * kColumns + threadIdx.x];
   if (threadIdx.x == 0) a.counts[blockIdx.x] = total;
 
-  if (chunk) return;
+  if (chunk || warp) return;
   // lengths, and which children need an open page: a row's number among those of its request in place of the page
-  uint32_t copied = 0;
+  bool needs = false;
   int4 copy = make_int4(0, 0, 0, 0);
-  if (warp == 0) {
-    bool needs = false;
-    if (lane < static_cast<int>(p.beams)) {
-      const int32_t from = parent[lane];
-      const bool there = !refused && from >= 0;
-      const uint32_t open = there ? length[from] & ((1u << a.page_shift) - 1) : 0;
-      p.lengths_out[row0 + lane] = there ? length[from] : 0;
-      bool first = true;
-      for (int i = 0; i < lane; ++i) first = first && parent[i] != from;
-      needs = there && open && !first;
-      if (needs) copy = make_int4(p.table[(row0 + from) * p.table_stride + held[from] - 1], 0, open, 0);
-    }
-    copied = __ballot_sync(kFull, needs);
-    copy.y = needs ? __popc(copied & ((1u << lane) - 1)) : 0;
-    if (lane < static_cast<int>(p.beams)) reinterpret_cast<int4*>(p.copies)[row0 + lane] = copy;
-    if (lane == 0) {
-      a.need[r] = refused ? -1 : __popc(copied);
-      if (refused) report(p.status, PREBA_ERR_BAD_TABLE);
-    }
+  if (lane < static_cast<int>(p.beams)) {
+    const int32_t from = parent[lane];
+    const bool there = !refused && from >= 0;
+    const uint32_t open = there ? length[from] & ((1u << a.page_shift) - 1) : 0;
+    p.lengths_out[row0 + lane] = there ? length[from] : 0;
+    bool first = true;
+    for (int i = 0; i < lane; ++i) first = first && parent[i] != from;
+    needs = there && open && !first;
+    if (needs) copy = make_int4(p.table[(row0 + from) * p.table_stride + held[from] - 1], 0, open, 0);
+  }
+  const uint32_t copied = __ballot_sync(kFull, needs);
+  copy.y = needs ? __popc(copied & ((1u << lane) - 1)) : 0;
+  if (lane < static_cast<int>(p.beams)) reinterpret_cast<int4*>(p.copies)[row0 + lane] = copy;
+  if (lane == 0) {
+    a.need[r] = refused ? -1 : __popc(copied);
+    if (refused) report(p.status, PREBA_ERR_BAD_TABLE);
   }
 }
 
 struct both_t {
   int64_t copies, released;
 };
+struct sums_t {  // 32 bits do: the table has no more entries
+  uint32_t copies, released;
+};
+constexpr uint32_t kHandBytes = sizeof(sums_t) + 1;  // shared, of a request
 __device__ __forceinline__ both_t hand_exclusive(both_t v, both_t* warp_sums, both_t& total) {
-  static_assert(kHandThreads == 1024, "a lane per warp");
+  constexpr int kWarps = kHandThreads / 32;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   both_t incl = v;
 #pragma unroll
@@ -485,104 +715,111 @@ __device__ __forceinline__ both_t hand_exclusive(both_t v, both_t* warp_sums, bo
   __syncthreads();  // what an earlier call left has been read
   if (lane == 31) warp_sums[warp] = incl;
   __syncthreads();
-  const both_t of = warp_sums[lane];
-  total = {warp_sum(of.copies), warp_sum(of.released)};
-  return {warp_sum(lane < warp ? of.copies : 0) + incl.copies - v.copies,
-          warp_sum(lane < warp ? of.released : 0) + incl.released - v.released};
+  total = {0, 0};
+  both_t before = {incl.copies - v.copies, incl.released - v.released};
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    const both_t of = warp_sums[w];
+    total.copies += of.copies, total.released += of.released;
+    if (w < warp) before.copies += of.copies, before.released += of.released;
+  }
+  return before;
 }
 
 __global__ void __launch_bounds__(kHandThreads) hand_out_kernel(const pages_args a) {
-  __shared__ both_t warp_sums[32];
+  extern __shared__ __align__(16) uint8_t hand_smem[];
   const preba_beam_pages_t& p = a.p;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  sums_t* sums = reinterpret_cast<sums_t*>(hand_smem);  // n: copies and pages, then those of the requests before
+  uint8_t* served = hand_smem + p.n * sizeof(sums_t);    // n
+  __shared__ both_t warp_sums[kHandThreads / 32];
   chained_begin();
   int64_t count = *p.free_count;
   if (count < 0 || count > p.free_capacity) {
-    if (threadIdx.x == 0) report(p.status, PREBA_ERR_BAD_TABLE);
+    if (blockIdx.x == 0 && threadIdx.x == 0) report(p.status, PREBA_ERR_BAD_TABLE);
     count = 0;
   }
+  // what every request asks for and releases
+  for (uint32_t r = threadIdx.x; r < p.n; r += kHandThreads) {
+    const int32_t need = a.need[r];
+    uint32_t released = 0;
+#pragma unroll 4
+    for (uint32_t k = 0; k < a.chunks; ++k) released += a.counts[r * a.chunks + k];
+    served[r] = need >= 0;
+    sums[r] = {static_cast<uint32_t>(max(need, 0)), released};  // one at fault releases nothing
+  }
+  __syncthreads();
   const uint32_t per = (p.n + kHandThreads - 1) / kHandThreads;
   const uint32_t r0 = min(threadIdx.x * per, p.n), r1 = min(r0 + per, p.n);
-  auto released_of = [&](uint32_t r) {
-    int64_t sum = 0;
-    for (uint32_t k = 0; k < a.chunks; ++k) sum += a.counts[r * a.chunks + k];
-    return sum;
-  };
-  both_t before, total;
-  bool any_refused = false;
-  for (int round = 0; round < 2; ++round) {
+  both_t total;
+  for (int round = 0;; ++round) {
     both_t mine{0, 0};
-    bool refused = false, short_of = false;
-    for (uint32_t r = r0; r < r1; ++r) {
-      const int32_t need = a.need[r];
-      refused |= need < 0;
-      if (need >= 0) mine.copies += need, mine.released += released_of(r);
-    }
-    before = hand_exclusive(mine, warp_sums, total);
+    for (uint32_t r = r0; r < r1; ++r)
+      if (served[r]) mine.copies += sums[r].copies, mine.released += sums[r].released;
+    const both_t before = hand_exclusive(mine, warp_sums, total);
     both_t at = before;
+    bool short_of = false;
     for (uint32_t r = r0; r < r1; ++r) {
-      if (a.need[r] < 0) continue;
-      at.copies += a.need[r], at.released += released_of(r);
+      if (!served[r]) continue;
+      at.copies += sums[r].copies, at.released += sums[r].released;
       short_of |= count + at.released < at.copies;
     }
-    any_refused = __syncthreads_or(refused);
-    if (!__syncthreads_or(short_of)) break;
-    // the pages do not suffice for all: one by one, in order.  The next round finds that they suffice
+    if (!__syncthreads_or(short_of)) {
+      at = before;
+      for (uint32_t r = r0; r < r1; ++r) {
+        const sums_t here = sums[r];
+        sums[r] = {static_cast<uint32_t>(at.copies), static_cast<uint32_t>(at.released)};
+        if (served[r]) at.copies += here.copies, at.released += here.released;
+      }
+      break;
+    }
+    // The pages do not suffice for all: one by one, in order.  The next round finds that they suffice
     if (threadIdx.x == 0) {
       int64_t left = count;
       for (uint32_t r = 0; r < p.n; ++r) {
-        if (a.need[r] < 0) continue;
-        const int64_t then = left + released_of(r) - a.need[r];
+        if (!served[r]) continue;
+        const int64_t then = left + sums[r].released - static_cast<int64_t>(sums[r].copies);
         if (then < 0) {
-          a.need[r] = -2;
-          report(p.status, PREBA_ERR_BUFFER_TOO_SMALL);
+          served[r] = 2;  // for a moment: refused
+          if (blockIdx.x == 0) report(p.status, PREBA_ERR_BUFFER_TOO_SMALL);
         } else {
           left = then;
         }
       }
     }
     __syncthreads();
-  }
-  both_t at = before;
-  for (uint32_t r = r0; r < r1; ++r) {
-    const bool served = a.need[r] >= 0;
-    a.copies_before[r] = static_cast<uint32_t>(at.copies);
-    if (served) at.copies += a.need[r];
-    for (uint32_t k = 0; k < a.chunks; ++k) {
-      const uint32_t unit = r * a.chunks + k;
-      a.before[unit] = at.released;
-      if (served) at.released += a.counts[unit];
-      else a.counts[unit] = 0;
-    }
+    for (uint32_t r = threadIdx.x; r < p.n; r += kHandThreads)
+      if (served[r] == 2) served[r] = 0;
+    __syncthreads();
   }
   __syncthreads();
-  // what is released: to the copies first, then onto the stack
-  for (uint32_t unit = warp; unit < p.n * a.chunks; unit += kHandThreads / 32) {
-    const uint32_t pages = a.counts[unit];
-    const int64_t first = a.before[unit];
-    const int32_t* from = a.lists + static_cast<uint64_t>(unit) * kColumns * p.beams;
-    for (uint32_t i = lane; i < pages; i += 32) {
-      const int64_t k = first + i;
-      if (k < total.copies) {
-        if (PREBA_IN_RANGE(p.status, k < static_cast<int64_t>(p.n) * p.beams)) a.given[k] = from[i];
-      } else if (count + k - total.copies < p.free_capacity) {
-        p.free_pages[count + k - total.copies] = from[i];
-      } else {
-        report(p.status, PREBA_ERR_BAD_TABLE);
-      }
-    }
-  }
-  __syncthreads();
-  for (uint32_t i = threadIdx.x; i < p.n * p.beams; i += kHandThreads) {
+
+  // this block's requests
+  const uint32_t each = (p.n + gridDim.x - 1) / gridDim.x;
+  const uint32_t b0 = min(blockIdx.x * each, p.n), b1 = min(b0 + each, p.n);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  // copies: a thread per row.  The k-th takes the k-th of the released pages, or one from the stack
+  for (uint32_t i = b0 * p.beams + threadIdx.x; i < b1 * p.beams; i += kHandThreads) {
     int4 copy = reinterpret_cast<const int4*>(p.copies)[i];
     if (copy.z == 0) continue;
     const uint32_t r = i / p.beams;
-    if (a.need[r] < 0) {
+    if (!served[r]) {
       reinterpret_cast<int4*>(p.copies)[i] = make_int4(0, 0, 0, 0);
       continue;
     }
-    const int64_t k = static_cast<int64_t>(a.copies_before[r]) + copy.y;
-    copy.y = k < total.released ? a.given[k] : p.free_pages[count - 1 - (k - total.released)];
+    int64_t k = static_cast<int64_t>(sums[r].copies) + copy.y;
+    if (k < total.released) {
+      uint32_t lo = 0, hi = p.n;  // the last request with no more released before it than k
+      while (hi - lo > 1) {
+        const uint32_t mid = (lo + hi) / 2;
+        if (sums[mid].released <= k) lo = mid; else hi = mid;
+      }
+      k -= sums[lo].released;
+      uint32_t unit = lo * a.chunks;
+      for (uint32_t n = a.counts[unit]; k >= n && unit + 1 < (lo + 1) * a.chunks; n = a.counts[unit]) k -= n, ++unit;
+      copy.y = PREBA_IN_RANGE(p.status, k < kColumns * p.beams) ? a.lists[static_cast<uint64_t>(unit) * kColumns * p.beams + k] : -1;
+    } else {
+      copy.y = p.free_pages[count - 1 - (k - total.released)];
+    }
     const uint32_t last = held_pages(a, p.lengths_out[i]) - 1;
     if (PREBA_IN_RANGE(p.status, last < p.table_width)) p.table_out[i * p.table_out_stride + last] = copy.y;
     if (copy.y < 0 || static_cast<uint32_t>(copy.y) >= p.pages) {
@@ -591,13 +828,29 @@ __global__ void __launch_bounds__(kHandThreads) hand_out_kernel(const pages_args
     }
     reinterpret_cast<int4*>(p.copies)[i] = copy;
   }
-  if (threadIdx.x == 0)
+  // what is released and not given to a copy goes onto the stack: a warp per request, or more of them where there are few
+  const uint32_t team = each == 1 ? kHandThreads : each == 2 ? kHandThreads / 2 : each <= 4 ? kHandThreads / 4 : 32;
+  const uint32_t member = threadIdx.x % team;
+  for (uint32_t r = b0 + threadIdx.x / team; r < b1; r += kHandThreads / team) {
+    if (!served[r]) continue;
+    int64_t first = static_cast<int64_t>(sums[r].released) - total.copies;  // its place above the old top
+    for (uint32_t k = 0; k < a.chunks; ++k) {
+      const uint32_t unit = r * a.chunks + k, pages = a.counts[unit];
+      const int32_t* from = a.lists + static_cast<uint64_t>(unit) * kColumns * p.beams;
+      for (uint32_t i = member; i < pages; i += team) {
+        if (first + i < 0) continue;
+        if (count + first + i < p.free_capacity) p.free_pages[count + first + i] = from[i];
+        else report(p.status, PREBA_ERR_BAD_TABLE);
+      }
+      first += pages;
+    }
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0)
     *p.free_left = static_cast<int32_t>(min(count + total.released - total.copies, static_cast<int64_t>(p.free_capacity)));
-  if (!any_refused) return;
   // requests that were refused for want of pages: their rows as they were
-  __syncthreads();
-  for (uint32_t i = warp; i < p.n * p.beams; i += kHandThreads / 32) {
-    if (a.need[i / p.beams] != -2) continue;
+  for (uint32_t i = b0 * p.beams + warp; i < b1 * p.beams; i += kHandThreads / 32) {
+    const uint32_t r = i / p.beams;
+    if (served[r] || a.need[r] < 0) continue;
     const uint32_t held = held_pages(a, p.lengths[i]);
     for (uint32_t c = lane; c < held; c += 32) p.table_out[i * p.table_out_stride + c] = p.table[i * p.table_stride + c];
     if (lane == 0) p.lengths_out[i] = 0;
@@ -608,11 +861,11 @@ uint64_t up16(uint64_t v) { return (v + 15) / 16 * 16; }
 
 bool beam_sizes_ok(uint32_t n, uint32_t beams, uint32_t table_width) {
   return n >= 1 && beams >= 1 && beams <= PREBA_BEAMS_MAX && static_cast<uint64_t>(n) * beams <= PREBA_PAGES_MAX_REQUESTS &&
-         table_width >= 1 && table_width <= INT32_MAX / 8;
+         table_width >= 1 && table_width <= INT32_MAX / 8 && static_cast<uint64_t>(n) * beams * table_width <= UINT32_MAX;
 }
 uint64_t pages_workspace(uint32_t n, uint32_t beams, uint32_t table_width) {
   const uint64_t units = static_cast<uint64_t>(n) * ((table_width + kColumns - 1) / kColumns);
-  return 2 * up16(4ull * n) + up16(4 * units) + up16(8 * units) + up16(4ull * n * beams) + 4 * units * kColumns * beams;
+  return up16(4ull * n) + up16(4 * units) + 4 * units * kColumns * beams;
 }
 
 // ---- preba_pages_copy -------------------------------------------------------------------------------
@@ -632,28 +885,43 @@ struct copy_args {
 
 __global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constant__ copy_args a) {
   __shared__ int4 jobs[kCopyRows];
-  __shared__ uint32_t n_jobs;
+  __shared__ uint32_t warp_jobs[kCopyThreads / 32];
   const preba_pages_copy_t& p = a.p;
   chained_begin();
   const uint32_t vectors = p.head_dim / 8;
   uint32_t turn = blockIdx.x;  // the block's next job, among all of them
   for (uint32_t row0 = 0; row0 < p.rows; row0 += kCopyRows) {
+    // in the order of the rows, for all blocks alike: four rows of a thread, 32 apart, 128 of a warp
+    constexpr int kEach = kCopyRows / kCopyThreads;
+    const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int4 c[kEach];
+    uint32_t masks[kEach], found = 0;
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      const uint32_t i = row0 + warp * 32 * kEach + 32 * k + lane;
+      c[k] = i < p.rows ? __ldg(reinterpret_cast<const int4*>(p.copies) + i) : make_int4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      const bool good = c[k].x >= 0 && static_cast<uint32_t>(c[k].x) < p.pages && c[k].y >= 0 &&
+                        static_cast<uint32_t>(c[k].y) < p.pages && c[k].z > 0 && static_cast<uint32_t>(c[k].z) <= p.page_size;
+      if (c[k].z != 0 && !good && blockIdx.x == 0) report(p.status, PREBA_ERR_BAD_TABLE);
+      masks[k] = __ballot_sync(kFull, good);
+      found += __popc(masks[k]);
+    }
     __syncthreads();  // the jobs before have been read
-    if (threadIdx.x < 32) {
-      // in the order of the rows, for all blocks alike
-      uint32_t found = 0;
-      for (uint32_t i = row0 + threadIdx.x; i - threadIdx.x < min(p.rows, row0 + kCopyRows); i += 32) {
-        int4 c = make_int4(0, 0, 0, 0);
-        if (i < p.rows) c = __ldg(reinterpret_cast<const int4*>(p.copies) + i);
-        const bool any = c.z != 0;
-        const bool good = any && c.x >= 0 && static_cast<uint32_t>(c.x) < p.pages && c.y >= 0 &&
-                          static_cast<uint32_t>(c.y) < p.pages && c.z > 0 && static_cast<uint32_t>(c.z) <= p.page_size;
-        if (any && !good && blockIdx.x == 0) report(p.status, PREBA_ERR_BAD_TABLE);
-        const uint32_t mask = __ballot_sync(kFull, good);
-        if (good) jobs[found + __popc(mask & ((1u << threadIdx.x) - 1))] = c;
-        found += __popc(mask);
-      }
-      if (threadIdx.x == 0) n_jobs = found;
+    if (lane == 0) warp_jobs[warp] = found;
+    __syncthreads();
+    uint32_t at = 0, n_jobs = 0;
+#pragma unroll
+    for (int w = 0; w < kCopyThreads / 32; ++w) {
+      if (w < static_cast<int>(warp)) at += warp_jobs[w];
+      n_jobs += warp_jobs[w];
+    }
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      if (masks[k] >> lane & 1) jobs[at + __popc(masks[k] & ((1u << lane) - 1))] = c[k];
+      at += __popc(masks[k]);
     }
     __syncthreads();
     const uint32_t caches = 2 * p.layers, all = n_jobs * caches;
@@ -687,13 +955,6 @@ __global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constan
   }
 }
 
-int device_sms(int* sms) {
-  int device = 0;
-  cudaError_t err = cudaGetDevice(&device);
-  if (err == cudaSuccess) err = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, device);
-  return finish(err);
-}
-
 }  // namespace
 }  // namespace preba
 
@@ -725,9 +986,9 @@ extern "C" int preba_beam_select(const preba_beam_select_t* req, void* stream) {
   int sms = 0;
   const int rc = device_sms(&sms);
   if (rc != PREBA_OK) return rc;
-  select_args a{p, segments_of(p.vocab, p.dtype), static_cast<float2*>(p.workspace)};
-  const bool vec = aligned(p.logits, 16) && (rows == 1 || p.row_stride * wide % 16 == 0);
+  const select_args a{p, segments_of(p.vocab, p.dtype), static_cast<float2*>(p.workspace)};
   cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const bool vec = aligned(p.logits, 16) && (rows == 1 || p.row_stride * wide % 16 == 0);
   if (p.dtype == PREBA_F32) return finish(vec ? launch_select<float, true>(a, sms, s) : launch_select<float, false>(a, sms, s));
   if (p.dtype == PREBA_F16) return finish(vec ? launch_select<__half, true>(a, sms, s) : launch_select<__half, false>(a, sms, s));
   return finish(vec ? launch_select<__nv_bfloat16, true>(a, sms, s) : launch_select<__nv_bfloat16, false>(a, sms, s));
@@ -754,6 +1015,9 @@ extern "C" int preba_beam_pages(const preba_beam_pages_t* req, void* stream) {
       static_cast<uint64_t>(p.n) * ((p.table_width + kColumns - 1) / kColumns) > INT32_MAX)
     return PREBA_ERR_INVALID_ARG;
   if (p.workspace_bytes < pages_workspace(p.n, p.beams, p.table_width)) return PREBA_ERR_BUFFER_TOO_SMALL;
+  int sms = 0;
+  const int rc = device_sms(&sms);
+  if (rc != PREBA_OK) return rc;
   pages_args a{};
   a.p = p;
   a.page_shift = 31 - __builtin_clz(p.page_size);
@@ -766,16 +1030,17 @@ extern "C" int preba_beam_pages(const preba_beam_pages_t* req, void* stream) {
     return got;
   };
   a.need = reinterpret_cast<int32_t*>(take(4ull * p.n));
-  a.copies_before = reinterpret_cast<uint32_t*>(take(4ull * p.n));
   a.counts = reinterpret_cast<uint32_t*>(take(4 * units));
-  a.before = reinterpret_cast<int64_t*>(take(8 * units));
-  a.given = reinterpret_cast<int32_t*>(take(4ull * p.n * p.beams));
   a.lists = reinterpret_cast<int32_t*>(at);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const cudaError_t err = launch_chained(follow_kernel, static_cast<uint32_t>(units), kColumns,
+  cudaError_t err = launch_chained(follow_kernel, static_cast<uint32_t>(units), kColumns,
                                          sizeof(int32_t) * kColumns * p.beams, s, a);
   if (err != cudaSuccess) return finish(err);
-  return finish(launch_chained(hand_out_kernel, 1, kHandThreads, 0, s, a));
+  const size_t smem = static_cast<size_t>(p.n) * kHandBytes;
+  if (smem > 40 * 1024)  // 48 KB need no leave
+    err = cudaFuncSetAttribute(hand_out_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, PREBA_PAGES_MAX_REQUESTS * kHandBytes);
+  if (err != cudaSuccess) return finish(err);
+  return finish(launch_chained(hand_out_kernel, std::min<uint32_t>(p.n, sms), kHandThreads, smem, s, a));
 }
 
 extern "C" int preba_pages_copy(const preba_pages_copy_t* req, void* stream) {

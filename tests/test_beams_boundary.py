@@ -94,7 +94,8 @@ PAGES = dict(workspace_bytes=1 << 40, table_stride=9, table_out_stride=9, table_
     dict(table=None), dict(table_out=None), dict(lengths_out=None), dict(copies=None), dict(copies=4104), dict(free_pages=None),
     dict(free_count=None), dict(free_left=None), dict(workspace=None), dict(workspace=4104), dict(table_out=4 * 4096),
     dict(free_left=9 * 4096), dict(lengths_out=2 * 4096), dict(free_capacity=1 << 31),
-    dict(table_width=1 << 27, table_stride=1 << 27, table_out_stride=1 << 27)])
+    dict(table_width=1 << 27, table_stride=1 << 27, table_out_stride=1 << 27),
+    dict(n=5000, table_width=1 << 19, table_stride=1 << 19, table_out_stride=1 << 19)])
 def test_tables_refuse(change):
     assert call("preba_beam_pages", filled(pb.PrebaBeamPages, **{**PAGES, **change})) == pb.ERR_INVALID_ARG
 

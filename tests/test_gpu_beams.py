@@ -325,3 +325,28 @@ def test_copies_at_fault_are_left_out():
         want = c.clone()
         want[3] = want[2]
         assert torch.equal(k, want) and torch.equal(v, want)
+
+
+@pytest.mark.parametrize("dtype,vocab,masked", [("bf16", 140001, False), ("fp16", 140000, True), ("fp32", 70003, True)])
+def test_selection_where_every_warp_has_many_segments(dtype, vocab, masked):
+    """More segments than the GPU has warps, several times over; rows of all kinds among them."""
+    n, beams, width = 32, 8, 8
+    rng = np.random.default_rng(vocab)
+    x, x64 = made(rng, n * beams, vocab, dtype)
+    scores = (-rng.random(n * beams) * 6).astype(np.float32)
+    scores[rng.random(n * beams) < 0.1] = -INF
+    done = rng.random(n * beams) < 0.2
+    allowed = rng.random((1, vocab)) < 0.5 if masked else None
+    check_select(run_select(x, scores, width, beams, 7, done, allowed), ob.select(x64, scores, width, beams, 7, done, allowed))
+
+
+@pytest.mark.parametrize("width", [1, 3, 20, 64])
+def test_equal_logits_in_many_segments(width):
+    """More segments of the same maximum than a request may list."""
+    vocab, beams = 180001, 3
+    x = torch.full((2 * beams, vocab), 1.25, dtype=torch.float16, device="cuda")
+    scores = np.array([-1, -1, -2, -3, -3, -3], dtype=np.float32)
+    done = np.array([False, True, False, True, True, True])
+    for ended in (None, done):
+        got = run_select(x, scores, width, beams, 9 if ended is not None else -1, ended)
+        check_select(got, ob.select(x.double().cpu().numpy(), scores, width, beams, 9 if ended is not None else -1, ended))
