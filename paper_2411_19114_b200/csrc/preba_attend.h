@@ -79,12 +79,24 @@ __device__ __forceinline__ bool load_packed(const preba_pages_attend_t& p, const
   return !(a < 0 || b < a || static_cast<uint32_t>(b) > p.tokens || static_cast<uint32_t>(b - a) > p.max_q || c < 0 || d < c ||
            static_cast<uint32_t>(d) > states);
 }
-// Rows j0 .. j1-1 of a request see its first states only, up to this many of them.
-__device__ __forceinline__ int32_t packed_seen(uint32_t tokens, const int32_t* seen, const request_t& q, int32_t j0, int32_t j1) {
+// Rows j0 .. j1-1 of a request see its first states only, up to this many of them.  Eight loads are on the way together; with
+// Warp all lanes ask for the same rows and share them.
+template <bool Warp = false>
+__device__ __forceinline__ int32_t packed_seen(const int32_t* seen, const request_t& q, int32_t j0, int32_t j1) {
   if (!seen) return q.keys;
   int32_t hi = 0;
-  for (int32_t j = j0; j < j1; ++j)
-    if (static_cast<uint32_t>(q.row + j) < tokens) hi = max(hi, seen[q.row + j]);
+  if (Warp) {
+    for (int32_t j = j0 + static_cast<int32_t>(threadIdx.x & 31); j < j1; j += 32) hi = max(hi, seen[q.row + j]);
+    hi = __reduce_max_sync(kFull, hi);
+  } else {
+    for (int32_t j = j0; j < j1; j += 8) {
+      int32_t v[8];
+#pragma unroll
+      for (int32_t k = 0; k < 8; ++k) v[k] = seen[q.row + min(j + k, j1 - 1)];
+#pragma unroll
+      for (int32_t k = 0; k < 8; ++k) hi = max(hi, v[k]);
+    }
+  }
   return min(hi, q.keys);
 }
 

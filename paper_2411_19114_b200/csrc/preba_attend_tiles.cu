@@ -66,8 +66,15 @@ template <int DP> struct layout {      // DP: head_dim rounded up to 64 or 128
   static constexpr uint32_t kItems = kBars + 512;
   static constexpr uint32_t kPlan = kItems + 256;      // own_plan_t
   static constexpr uint32_t kBytes = kPlan + 2048;
-  // tensor memory columns: S of A and B (P lies over them), O of A and B
-  static constexpr uint32_t kS = 0, kO = 256;
+  // Tensor memory columns: S (P lies over them), O of A and B.  Heads of up to 64 leave room for a third S, which A and B take
+  // in turn: their next scores are made while they are busy with the last ones, and the chain of a row tile is its softmax
+  // alone (16 prompts of up to 448 rows over up to 1500 states, 20 heads of 64: 88 -> THIRD us).
+  static constexpr uint32_t kBuffers = DP == 64 ? 3 : 2;
+  // Scores and probabilities of a tile may then be there before those of the last one have been waited for, but no further: two
+  // barriers of each kind take turns
+  static constexpr uint32_t kTurns = kBuffers - 1;
+  static constexpr uint32_t kS = 0, kO = kBuffers * kTile;
+  static_assert(kO + 2 * DP <= kTmemColumns, "tensor memory");
 };
 
 // Partial sums of a piece in groups of four floats: 256 rows of O, then a maximum and a sum for each.
@@ -134,12 +141,12 @@ __device__ __forceinline__ bool request_of(const tiles_args& a, uint32_t r, requ
   if (Packed) return load_packed(a.p, a.cu_k, a.states, r, q);
   return load_request(a.p, r, q);
 }
-template <bool Packed>
+template <bool Packed, bool Warp = false>
 __device__ __forceinline__ void seen_of(const tiles_args& a, const request_t& q, int32_t j0, int32_t j1, int32_t& lo,
                                         int32_t& hi) {
   if (Packed) {
     lo = 0;
-    hi = packed_seen(a.p.tokens, a.seen, q, j0, j1);
+    hi = packed_seen<Warp>(a.seen, q, j0, j1);
   } else {
     seen_by(a.p, q, j0, j1, lo, hi);
   }
@@ -150,7 +157,7 @@ struct pair_range {
   int32_t first[2], last[2];     // key tiles of A and B
   int32_t begin, end;            // of both
 };
-template <bool Packed>
+template <bool Packed, bool Warp = false>  // Warp: asked for by a whole warp together
 __device__ __forceinline__ pair_range range_of(const tiles_args& a, const request_t& q, uint32_t pair) {
   pair_range r;
   r.lo = r.hi = 0;
@@ -162,7 +169,7 @@ __device__ __forceinline__ pair_range range_of(const tiles_args& a, const reques
     r.first[x] = r.last[x] = 0;
     if (j0 >= j1) continue;  // only B
     int32_t lo, hi;
-    seen_of<Packed>(a, q, j0, j1, lo, hi);
+    seen_of<Packed, Warp>(a, q, j0, j1, lo, hi);
     lo = min(lo, max(0, q.keys - 1));  // rows behind all keys see nothing: one empty tile
     r.first[x] = lo / kTile;
     r.last[x] = max(r.first[x] + 1, (hi + kTile - 1) / kTile);
@@ -500,10 +507,10 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
   const uint32_t base = smem_addr(smem);
   const uint32_t kv_full = base + L::kBars, kv_empty = kv_full + 8 * L::kSlots;
   const uint32_t q_full = kv_empty + 8 * L::kSlots, q_empty = q_full + 8;
-  const uint32_t s_full = q_empty + 8, p_full = s_full + 16, o_full = p_full + 16;  // A, B each
+  const uint32_t s_full = q_empty + 8, p_full = s_full + 16 * L::kTurns, o_full = p_full + 16 * L::kTurns;  // A, B each
   const uint32_t item_full = o_full + 16, item_empty = item_full + 16;             // two slots each
   const uint32_t drained = item_empty + 16, h_full = drained + 8;
-  static_assert(8 * (2 * L::kSlots + 15) + 8 <= 504, "layout::kItems");
+  static_assert(8 * (2 * L::kSlots + 9 + 6 * L::kTurns) <= 504, "layout::kItems");
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + L::kBars + 504);
   item_t* items = reinterpret_cast<item_t*>(smem + L::kItems);
 
@@ -515,9 +522,11 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
     mbar_init(q_full, 1);
     mbar_init(q_empty, 1);
     for (int x = 0; x < 2; ++x) {
-      mbar_init(s_full + 8 * x, 1);
-      mbar_init(p_full + 8 * x, kSoftWarps / 2);
-      mbar_init(h_full + 8 * x, kSoftWarps / 2);
+      for (uint32_t k = 0; k < L::kTurns; ++k) {
+        mbar_init(s_full + 8 * (x + 2 * k), 1);
+        mbar_init(p_full + 8 * (x + 2 * k), kSoftWarps / 2);
+        mbar_init(h_full + 8 * (x + 2 * k), kSoftWarps / 2);
+      }
       mbar_init(o_full + 8 * x, 1);
       mbar_init(item_full + 8 * x, 1);
       mbar_init(item_empty + 8 * x, kSoftWarps + 1);
@@ -588,7 +597,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
             of.row = q.row;
             of.rows = q.rows;
             of.keys = q.keys;
-            const pair_range range = range_of<Packed>(a, q, of.pair);
+            const pair_range range = range_of<Packed, true>(a, q, of.pair);
             of.tiles = range.end - range.begin;
           } else {
             if (!PREBA_IN_RANGE(p.status, pair < plan.n_pairs)) pair = 0;
@@ -620,7 +629,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
         const bool done = item.count == 0;
         if (!done) {
           const request_t q{of.row, of.rows, of.keys};
-          const pair_range range = range_of<Packed>(a, q, of.pair);
+          const pair_range range = range_of<Packed, true>(a, q, of.pair);
           item.request = of.request;
           item.row = q.row;
           item.rows = q.rows;
@@ -698,8 +707,12 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
       // ---- matrix products: one lane issues, the warp clears values that nobody sees
       constexpr uint32_t kQkShape = shape<T>(kTile, false), kPvShape = shape<T>(DP, true);
       ring<L::kSlots> kv;  // next slot to be waited for
-      ring<1> q_ring, p_ring[2];
+      ring<1> q_ring;
+      ring<L::kTurns> p_ring[2];
       ring<2> in;
+      uint32_t made = 0;        // with three buffers: the one of the next scores
+      uint32_t where[2]{};      // and those of the last of A and of B
+      uint32_t s_turn[2]{};
       while (ok) {
         ok = wait(item_full + 8 * in.slot, in.phase);
         if (!ok) break;
@@ -716,21 +729,28 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
         auto qk = [&](int x) {
           const uint32_t q_op = __shfl_sync(kFull, operand(base + x * L::kQ, 16), 0);
           const uint32_t k_op = __shfl_sync(kFull, operand(base + L::kRing + k_slot * L::kSlot, 16), 0);
-          const uint32_t d = __shfl_sync(kFull, tmem + L::kS + x * kTile, 0);
+          uint32_t buffer = x;
+          if (L::kBuffers == 3) {
+            buffer = made;
+            made = made == 2 ? 0 : made + 1;
+            where[x] = buffer;
+          }
+          const uint32_t d = __shfl_sync(kFull, tmem + L::kS + buffer * kTile, 0);
           if (elected()) {
 #pragma unroll
             for (int ks = 0; ks < DP / 16; ++ks) {
               const uint32_t off = (ks / 4) * L::kHalf + (ks % 4) * 32;
               mma_ss(d, q_op + (off >> 4), k_op + (off >> 4), kQkShape, ks > 0);
             }
-            mma_commit(s_full + 8 * x);
+            mma_commit(s_full + 8 * (x + 2 * s_turn[x]));
           }
+          if (L::kTurns == 2) s_turn[x] ^= 1;
           __syncwarp();
         };
-        auto pv = [&](int x, bool add, int from, int to) {
+        auto pv = [&](int x, uint32_t buffer, bool add, int from, int to) {
           const uint32_t v_op = __shfl_sync(kFull, operand(base + L::kRing + v_slot * L::kSlot, L::kHalf), 0);
           const uint32_t d = __shfl_sync(kFull, tmem + L::kO + x * DP, 0);
-          const uint32_t a_op = __shfl_sync(kFull, tmem + L::kS + x * kTile, 0);
+          const uint32_t a_op = __shfl_sync(kFull, tmem + L::kS + buffer * kTile, 0);
           if (elected()) {
 #pragma unroll
             for (int ks = from; ks < to; ++ks)
@@ -772,31 +792,42 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
             __syncwarp();
           }
           bool k_waited = false;
+          auto next_scores = [&](int x) {
+            if (t + 1 < item.first[x] || t + 1 >= item.last[x]) return;
+            if (!k_waited) {
+              ok = ok && wait(kv_full + 8 * kv.slot, kv.phase);
+              if (!ok) return;
+              fence_after();
+              k_slot = kv.slot;
+              k_waited = true;
+            }
+            qk(x);
+          };
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
+            uint32_t buffer = x;
+            if (L::kBuffers == 3) {
+              // Of three buffers two at most hold what has no product yet: the next scores of A have the third, and those of B the
+              // one that A's product has just been issued from
+              buffer = where[x];
+              next_scores(x);
+            }
+            if (!ok) break;
             if (t >= item.first[x] && t < item.last[x]) {
               // the product with the first half of P while the second is being made
-              ok = ok && wait(h_full + 8 * x, p_ring[x].phase);
+              const uint32_t turn = 8 * (x + 2 * p_ring[x].slot);
+              ok = ok && wait(h_full + turn, p_ring[x].phase);
               if (!ok) break;
               fence_after();
-              pv(x, t > item.first[x], 0, kTile / 32);
-              ok = ok && wait(p_full + 8 * x, p_ring[x].phase);
+              pv(x, buffer, t > item.first[x], 0, kTile / 32);
+              ok = ok && wait(p_full + turn, p_ring[x].phase);
               if (!ok) break;
               p_ring[x].step();
               fence_after();
-              pv(x, true, kTile / 32, kTile / 16);
-              if (t + 1 == item.last[x] && elected()) mma_commit(o_full + 8 * x);
+              pv(x, buffer, true, kTile / 32, kTile / 16);
+              if ((L::kBuffers == 3 || t + 1 == item.last[x]) && elected()) mma_commit(o_full + 8 * x);
             }
-            if (t + 1 >= item.first[x] && t + 1 < item.last[x]) {
-              if (!k_waited) {
-                ok = ok && wait(kv_full + 8 * kv.slot, kv.phase);
-                if (!ok) break;
-                fence_after();
-                k_slot = kv.slot;
-                k_waited = true;
-              }
-              qk(x);
-            }
+            if (L::kBuffers == 2) next_scores(x);
           }
           if (!ok) break;
           if (elected()) mma_commit(kv_empty + 8 * v_slot);
@@ -828,7 +859,8 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
     // ---- softmax: group x has row tile x, a thread a row
     const int x = warp >> 2, r = threadIdx.x & (kTile - 1);
     const uint32_t lanes = static_cast<uint32_t>(warp & 3) << 21;  // 32 rows of tensor memory each
-    const uint32_t s_at = tmem + lanes + L::kS + x * kTile, o_at = tmem + lanes + L::kO + x * DP;
+    const uint32_t o_at = tmem + lanes + L::kO + x * DP;
+    uint32_t made = 0, products = 0;  // with three buffers: scores of A and B before (mod 3), and products of this one
     const float scale = p.scale * kLog2e;
     const int32_t j = r / static_cast<int32_t>(a.group), g = r - j * static_cast<int32_t>(a.group);
     ring<1> s_ring, o_ring;
@@ -838,6 +870,10 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
       if (!ok) break;
       const item_t item = items[in.slot];
       const int32_t first = items[in.slot].first[x], last = items[in.slot].last[x];
+      // the scores of the other tile, which are made in turn with these, A's first
+      const int32_t other_first = items[in.slot].first[1 - x], other_last = items[in.slot].last[1 - x] - x;
+      const uint32_t made_before = made;
+      if (L::kBuffers == 3) made = (made + (last - first) + (other_last + x - other_first)) % 3;
       __syncwarp();
       if (lane == 0) mbar_arrive(item_empty + 8 * in.slot);
       in.step();
@@ -859,10 +895,14 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
       }
       float m = -INFINITY, l = 0.f;
       for (int32_t t = first; t < last && ok; ++t) {
-        ok = wait(s_full + 8 * x, s_ring.phase);
+        const uint32_t buffer =
+            L::kBuffers == 3 ? (made_before + (t - first) + max(0, min(t, other_last) + x - other_first)) % 3 : x;
+        const uint32_t turn = 8 * (x + (L::kTurns == 2 ? 2 * (products & 1) : 0));
+        ok = wait(s_full + turn, L::kTurns == 2 ? products >> 1 & 1 : s_ring.phase);
         if (!ok) break;
         s_ring.step();
         fence_after();
+        const uint32_t s_at = tmem + lanes + L::kS + buffer * kTile;
         uint32_t s[kTile];
 #pragma unroll
         for (int c = 0; c < kTile; c += 32) tmem_load32(s + c, s_at + c);
@@ -895,7 +935,13 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
           const float keep = to == -INFINITY ? 0.f : exp2_approx(m - to);
           m = to;
           l *= keep;
-          if (t > first) {  // the product before has finished: S could not be there otherwise
+          if (t > first) {
+            // with two buffers the product before has finished: S could not be there otherwise
+            if (L::kBuffers == 3) {
+              ok = wait(o_full + 8 * x, products - 1 & 1);
+              if (!ok) break;
+              fence_after();
+            }
             for (int c = 0; c < DP; c += 32) {
               uint32_t o[32];
               tmem_load32(o, o_at + c);
@@ -906,6 +952,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
             }
           }
         }
+        ++products;
         const float shift = m == -INFINITY ? 0.f : m;
         const uint64_t scale2 = pair(scale, scale), shift2 = pair(-shift, -shift);
         uint64_t sums[2] = {0, 0};
@@ -926,7 +973,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
             tmem_stored();
             fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(h_full + 8 * x);
+            if (lane == 0) mbar_arrive(h_full + turn);
           }
         }
         float l0, l1;
@@ -935,12 +982,12 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
         tmem_stored();
         fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(p_full + 8 * x);
+        if (lane == 0) mbar_arrive(p_full + turn);
       }
       if (!ok) break;
       const bool any = first < last;
       if (any) {
-        ok = wait(o_full + 8 * x, o_ring.phase);
+        ok = wait(o_full + 8 * x, L::kBuffers == 3 ? products - 1 & 1 : o_ring.phase);
         if (!ok) break;
         o_ring.step();
         fence_after();

@@ -111,7 +111,7 @@ __device__ __forceinline__ bool load_entry(const cross_args& a, uint32_t r, entr
   e.tiles = 0;
   if (!load_packed(a.p, a.cu_k, a.states, r, e.q)) return false;
   e.state0 = a.cu_k[r];
-  e.hi = packed_seen(a.p.tokens, a.seen, e.q, 0, e.q.rows);
+  e.hi = packed_seen(a.seen, e.q, 0, e.q.rows);
   if (e.q.rows) e.tiles = max(1, (e.hi + kTile - 1) / kTile);  // one that sees nothing still has its zeros to write
   return true;
 }
@@ -501,7 +501,7 @@ cross_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
       const bool row_there = r < N && in_head < static_cast<uint32_t>(rows) && kv_head < p.heads_kv;
       const uint32_t j = in_head / a.group, h = kv_head * a.group + in_head - j * a.group;
       if (r < N) {
-        if (row_there) hi = packed_seen(p.tokens, a.seen, q, j, j + 1);
+        if (row_there) hi = packed_seen(a.seen, q, j, j + 1);
         row_hi[r] = hi;
         row_at[r] = row_there ? (q.row + j) * p.out_stride[0] + h * p.out_stride[1] : kNowhere;
         ref[r] = row_there ? 0.f : INFINITY;  // columns without a row hold whatever lay behind the queries: they outgrow nothing
