@@ -603,10 +603,11 @@ __device__ __forceinline__ uint32_t held_pages(const pages_args& a, int32_t leng
   return (static_cast<uint32_t>(length) + (1u << a.page_shift) - 1) >> a.page_shift;
 }
 
-__global__ void __launch_bounds__(kColumns) follow_kernel(const pages_args a) {
+// Few: at most kAtOnce beams, whose entries of a column a thread then keeps in registers; else they lie in shared memory.
+template <bool Few> __global__ void __launch_bounds__(kColumns) follow_kernel(const __grid_constant__ pages_args a) {
   extern __shared__ int32_t tile[];  // beams x kColumns
   __shared__ int32_t parent[PREBA_BEAMS_MAX], length[PREBA_BEAMS_MAX];
-  __shared__ uint32_t held[PREBA_BEAMS_MAX], warp_sums[kColumns / 32];
+  __shared__ uint32_t held[PREBA_BEAMS_MAX], warp_sums[kColumns / 32], parents_of;
   const preba_beam_pages_t& p = a.p;
   const uint32_t r = blockIdx.x / a.chunks, chunk = blockIdx.x - r * a.chunks, row0 = r * p.beams;
   const uint32_t c = chunk * kColumns + threadIdx.x;
@@ -614,21 +615,29 @@ __global__ void __launch_bounds__(kColumns) follow_kernel(const pages_args a) {
   chained_begin();
   const int64_t kept = p.kept ? p.kept[r] : 0;
   bool bad = false;
-  if (threadIdx.x < p.beams) {
-    const int32_t len = p.lengths[row0 + threadIdx.x], par = p.parents[row0 + threadIdx.x];
-    const uint32_t h = len < 0 ? 0 : held_pages(a, len);
-    bad = len < 0 || h > p.table_width || par >= static_cast<int32_t>(p.beams);
-    parent[threadIdx.x] = par < 0 ? -1 : par;
-    length[threadIdx.x] = len;
-    held[threadIdx.x] = min(h, p.table_width);
+  if (warp == 0) {
+    uint32_t child_of = 0;
+    if (lane < static_cast<int>(p.beams)) {
+      const int32_t len = p.lengths[row0 + lane], par = p.parents[row0 + lane];
+      const uint32_t h = len < 0 ? 0 : held_pages(a, len);
+      bad = len < 0 || h > p.table_width || par >= static_cast<int32_t>(p.beams);
+      parent[lane] = par < 0 ? -1 : par;
+      length[lane] = len;
+      held[lane] = min(h, p.table_width);
+      if (par >= 0 && !bad) child_of = 1u << par;
+    }
+    child_of = __reduce_or_sync(kFull, child_of);
+    if (lane == 0) parents_of = child_of;
   }
   const bool refused = __syncthreads_or(bad);
-  uint32_t parents = 0;  // a bit per beam that has a child
-  for (uint32_t b = 0; b < p.beams; ++b)
-    if (parent[b] >= 0 && !refused) parents |= 1u << parent[b];
+  const uint32_t parents = refused ? 0 : parents_of;  // a bit per beam that has a child
+  // the page that a row's copy comes from is looked up beside the columns
+  int32_t source = 0;
+  if (chunk == 0 && warp == 0 && lane < static_cast<int>(p.beams) && !refused && parent[lane] >= 0 && held[parent[lane]])
+    source = p.table[(row0 + parent[lane]) * p.table_stride + held[parent[lane]] - 1];
   // every thread has a column, and reads no other's
+  int32_t page[kAtOnce];
   for (uint32_t b0 = 0; b0 < p.beams; b0 += kAtOnce) {
-    int32_t page[kAtOnce];
 #pragma unroll
     for (uint32_t k = 0; k < kAtOnce; ++k)
       page[k] = b0 + k < p.beams && c < held[b0 + k] ? p.table[(row0 + b0 + k) * p.table_stride + c] : 0;
@@ -642,17 +651,36 @@ __global__ void __launch_bounds__(kColumns) follow_kernel(const pages_args a) {
   }
   // what this column releases, a bit per beam
   uint32_t gone = 0;
-  if (!refused && c >= kept)
-    for (uint32_t b = 0; b < p.beams; ++b) {
-      if (parents >> b & 1 || c >= held[b]) continue;
-      const int32_t page = tile[b * kColumns + threadIdx.x];
-      bool alone = true;
-      for (uint32_t o = 0; o < p.beams; ++o)
-        if ((parents >> o & 1 || o < b) && c < held[o] && tile[o * kColumns + threadIdx.x] == page) alone = false;
-      if (!alone) continue;
-      if (page < 0 || static_cast<uint32_t>(page) >= p.pages) report(p.status, PREBA_ERR_BAD_TABLE);
-      else gone |= 1u << b;
+  if (!refused && c >= kept) {
+    if (Few) {
+      uint32_t have = 0;  // beams with a page here
+#pragma unroll
+      for (uint32_t k = 0; k < kAtOnce; ++k)
+        if (k < p.beams && c < held[k]) have |= 1u << k;
+      gone = have & ~parents;
+#pragma unroll
+      for (uint32_t b = 0; b < kAtOnce; ++b)
+#pragma unroll
+        for (uint32_t o = 0; o < kAtOnce; ++o)
+          if (o != b && page[o] == page[b] && (have >> o & 1) && (o < b || (parents >> o & 1))) gone &= ~(1u << b);
+    } else {
+      for (uint32_t b = 0; b < p.beams; ++b) {
+        if (parents >> b & 1 || c >= held[b]) continue;
+        const int32_t mine = tile[b * kColumns + threadIdx.x];
+        bool alone = true;
+        for (uint32_t o = 0; o < p.beams; ++o)
+          if ((parents >> o & 1 || o < b) && c < held[o] && tile[o * kColumns + threadIdx.x] == mine) alone = false;
+        if (alone) gone |= 1u << b;
+      }
     }
+    for (uint32_t left = gone; left; left &= left - 1) {
+      const int b = __ffs(left) - 1;
+      const int32_t number = tile[b * kColumns + threadIdx.x];
+      if (number >= 0 && static_cast<uint32_t>(number) < p.pages) continue;
+      report(p.status, PREBA_ERR_BAD_TABLE);
+      gone &= ~(1u << b);
+    }
+  }
   const uint32_t mine = __popc(gone);
   uint32_t incl = mine;
 #pragma unroll
@@ -685,7 +713,7 @@ __global__ void __launch_bounds__(kColumns) follow_kernel(const pages_args a) {
     bool first = true;
     for (int i = 0; i < lane; ++i) first = first && parent[i] != from;
     needs = there && open && !first;
-    if (needs) copy = make_int4(p.table[(row0 + from) * p.table_stride + held[from] - 1], 0, open, 0);
+    if (needs) copy = make_int4(source, 0, open, 0);
   }
   const uint32_t copied = __ballot_sync(kFull, needs);
   copy.y = needs ? __popc(copied & ((1u << lane) - 1)) : 0;
@@ -726,7 +754,7 @@ __device__ __forceinline__ both_t hand_exclusive(both_t v, both_t* warp_sums, bo
   return before;
 }
 
-__global__ void __launch_bounds__(kHandThreads) hand_out_kernel(const pages_args a) {
+__global__ void __launch_bounds__(kHandThreads) hand_out_kernel(const __grid_constant__ pages_args a) {
   extern __shared__ __align__(16) uint8_t hand_smem[];
   const preba_beam_pages_t& p = a.p;
   sums_t* sums = reinterpret_cast<sums_t*>(hand_smem);  // n: copies and pages, then those of the requests before
@@ -797,52 +825,62 @@ __global__ void __launch_bounds__(kHandThreads) hand_out_kernel(const pages_args
   const uint32_t each = (p.n + gridDim.x - 1) / gridDim.x;
   const uint32_t b0 = min(blockIdx.x * each, p.n), b1 = min(b0 + each, p.n);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  // copies: a thread per row.  The k-th takes the k-th of the released pages, or one from the stack
-  for (uint32_t i = b0 * p.beams + threadIdx.x; i < b1 * p.beams; i += kHandThreads) {
-    int4 copy = reinterpret_cast<const int4*>(p.copies)[i];
-    if (copy.z == 0) continue;
-    const uint32_t r = i / p.beams;
-    if (!served[r]) {
-      reinterpret_cast<int4*>(p.copies)[i] = make_int4(0, 0, 0, 0);
-      continue;
-    }
-    int64_t k = static_cast<int64_t>(sums[r].copies) + copy.y;
-    if (k < total.released) {
-      uint32_t lo = 0, hi = p.n;  // the last request with no more released before it than k
-      while (hi - lo > 1) {
-        const uint32_t mid = (lo + hi) / 2;
-        if (sums[mid].released <= k) lo = mid; else hi = mid;
+  constexpr int kCopyWarps = 2;
+  if (warp < kCopyWarps) {
+    // copies: a thread per row.  The k-th takes the k-th of the released pages, or one from the stack
+    for (uint32_t i = b0 * p.beams + threadIdx.x; i < b1 * p.beams; i += 32 * kCopyWarps) {
+      int4 copy = reinterpret_cast<const int4*>(p.copies)[i];
+      const int32_t length = p.lengths_out[i];
+      if (copy.z == 0) continue;
+      const uint32_t r = i / p.beams;
+      if (!served[r]) {
+        reinterpret_cast<int4*>(p.copies)[i] = make_int4(0, 0, 0, 0);
+        continue;
       }
-      k -= sums[lo].released;
-      uint32_t unit = lo * a.chunks;
-      for (uint32_t n = a.counts[unit]; k >= n && unit + 1 < (lo + 1) * a.chunks; n = a.counts[unit]) k -= n, ++unit;
-      copy.y = PREBA_IN_RANGE(p.status, k < kColumns * p.beams) ? a.lists[static_cast<uint64_t>(unit) * kColumns * p.beams + k] : -1;
-    } else {
-      copy.y = p.free_pages[count - 1 - (k - total.released)];
-    }
-    const uint32_t last = held_pages(a, p.lengths_out[i]) - 1;
-    if (PREBA_IN_RANGE(p.status, last < p.table_width)) p.table_out[i * p.table_out_stride + last] = copy.y;
-    if (copy.y < 0 || static_cast<uint32_t>(copy.y) >= p.pages) {
-      report(p.status, PREBA_ERR_BAD_TABLE);
-      copy = make_int4(0, 0, 0, 0);
-    }
-    reinterpret_cast<int4*>(p.copies)[i] = copy;
-  }
-  // what is released and not given to a copy goes onto the stack: a warp per request, or more of them where there are few
-  const uint32_t team = each == 1 ? kHandThreads : each == 2 ? kHandThreads / 2 : each <= 4 ? kHandThreads / 4 : 32;
-  const uint32_t member = threadIdx.x % team;
-  for (uint32_t r = b0 + threadIdx.x / team; r < b1; r += kHandThreads / team) {
-    if (!served[r]) continue;
-    int64_t first = static_cast<int64_t>(sums[r].released) - total.copies;  // its place above the old top
-    for (uint32_t k = 0; k < a.chunks; ++k) {
-      const uint32_t unit = r * a.chunks + k, pages = a.counts[unit];
-      const int32_t* from = a.lists + static_cast<uint64_t>(unit) * kColumns * p.beams;
-      for (uint32_t i = member; i < pages; i += team) {
-        if (first + i < 0) continue;
-        if (count + first + i < p.free_capacity) p.free_pages[count + first + i] = from[i];
-        else report(p.status, PREBA_ERR_BAD_TABLE);
+      int64_t k = static_cast<int64_t>(sums[r].copies) + copy.y;
+      if (k < total.released) {
+        uint32_t lo = 0, hi = p.n;  // the last request with no more released before it than k
+        while (hi - lo > 1) {
+          const uint32_t mid = (lo + hi) / 2;
+          if (sums[mid].released <= k) lo = mid; else hi = mid;
+        }
+        k -= sums[lo].released;
+        uint32_t unit = lo * a.chunks;
+        for (const uint32_t last = unit + a.chunks - 1; unit < last; ++unit) {
+          const uint32_t pages = a.counts[unit];
+          if (k < pages) break;
+          k -= pages;
+        }
+        copy.y = PREBA_IN_RANGE(p.status, k < kColumns * p.beams) ? a.lists[static_cast<uint64_t>(unit) * kColumns * p.beams + k] : -1;
+      } else {
+        copy.y = p.free_pages[count - 1 - (k - total.released)];
       }
-      first += pages;
+      const uint32_t last = held_pages(a, length) - 1;
+      if (PREBA_IN_RANGE(p.status, last < p.table_width)) p.table_out[i * p.table_out_stride + last] = copy.y;
+      if (copy.y < 0 || static_cast<uint32_t>(copy.y) >= p.pages) {
+        report(p.status, PREBA_ERR_BAD_TABLE);
+        copy = make_int4(0, 0, 0, 0);
+      }
+      reinterpret_cast<int4*>(p.copies)[i] = copy;
+    }
+  } else {
+    // What is released and not given to a copy goes onto the stack: a warp per request, or all of these where there is one
+    const uint32_t threads = kHandThreads - 32 * kCopyWarps, team = each == 1 ? threads : 32;
+    const uint32_t place = threadIdx.x - 32 * kCopyWarps, member = place % team;
+    for (uint32_t r = b0 + place / team; r < b1; r += threads / team) {
+      if (!served[r]) continue;
+      int64_t first = static_cast<int64_t>(sums[r].released) - total.copies;  // its place above the old top
+      for (uint32_t k = 0; k < a.chunks; ++k) {
+        const uint32_t unit = r * a.chunks + k, pages = a.counts[unit];
+        const int32_t* from = a.lists + static_cast<uint64_t>(unit) * kColumns * p.beams;
+#pragma unroll 4
+        for (uint32_t i = member; i < pages; i += team) {
+          if (first + i < 0) continue;
+          if (count + first + i < p.free_capacity) p.free_pages[count + first + i] = from[i];
+          else report(p.status, PREBA_ERR_BAD_TABLE);
+        }
+        first += pages;
+      }
     }
   }
   if (blockIdx.x == 0 && threadIdx.x == 0)
@@ -1033,8 +1071,8 @@ extern "C" int preba_beam_pages(const preba_beam_pages_t* req, void* stream) {
   a.counts = reinterpret_cast<uint32_t*>(take(4 * units));
   a.lists = reinterpret_cast<int32_t*>(at);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  cudaError_t err = launch_chained(follow_kernel, static_cast<uint32_t>(units), kColumns,
-                                         sizeof(int32_t) * kColumns * p.beams, s, a);
+  cudaError_t err = launch_chained(p.beams <= kAtOnce ? follow_kernel<true> : follow_kernel<false>, static_cast<uint32_t>(units),
+                                   kColumns, sizeof(int32_t) * kColumns * p.beams, s, a);
   if (err != cudaSuccess) return finish(err);
   const size_t smem = static_cast<size_t>(p.n) * kHandBytes;
   if (smem > 40 * 1024)  // 48 KB need no leave
