@@ -720,6 +720,11 @@ cross_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
       soft_sync();  // what lies in shared memory has been read
     }
     if (!ok) report(p.status, PREBA_ERR_TIMEOUT);
+    if (pending) {  // the run ended with the beginning of a piece, but no tile of it
+      __threadfence();
+      soft_sync();
+      count_piece();
+    }
     if (first_counted) {
       counted(0);
       soft_sync();

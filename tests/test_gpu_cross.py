@@ -92,7 +92,9 @@ class Step:
     ([5] * 7, [1, 2, 127, 128, 129, 700, 31], 3, 3, 64), ([8] * 3, [300, 1, 640], 8, 2, 128), ([16], [513], 4, 1, 80),
     ([3, 0, 2, 3], [40, 50, 0, 256], 6, 2, 72), ([0, 0, 1], [9, 0, 3], 2, 2, 64), ([64], [5000], 1, 1, 64),
     ([2], [20000], 7, 1, 128), ([4] * 40, list(range(1, 161, 4)), 4, 4, 40), ([1] * 300, [7] * 300, 2, 1, 64),
-    ([1], [3], 64, 1, 64), ([13], [300], 5, 1, 128)])
+    ([1], [3], 64, 1, 64), ([13], [300], 5, 1, 128),
+    # runs that end with a piece's beginning but no tile of it
+    ([16, 2], [30000, 500], 2, 1, 128), ([2] * 5, [20000, 128 * 89, 128 * 90, 128 * 91, 40000], 3, 1, 64)])
 def test_few_rows_match_the_definition(rows, states, hq, hk, d, dtype):
     Step(rows, states, hq, hk, d, dtype, seed=len(rows) + d).check()
 
