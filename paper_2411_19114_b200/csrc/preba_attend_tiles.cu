@@ -68,10 +68,10 @@ template <int DP> struct layout {      // DP: head_dim rounded up to 64 or 128
   static constexpr uint32_t kBytes = kPlan + 2048;
   // Tensor memory columns: S (P lies over them), O of A and B.  Heads of up to 64 leave room for a third S, which A and B take
   // in turn: their next scores are made while they are busy with the last ones, and the chain of a row tile is its softmax
-  // alone (16 prompts of up to 448 rows over up to 1500 states, 20 heads of 64: 88 -> THIRD us).
+  // alone (16 prompts of up to 448 rows over up to 1500 states, 20 heads of 64: 88.6 -> 82.9 us).
   static constexpr uint32_t kBuffers = DP == 64 ? 3 : 2;
-  // Scores and probabilities of a tile may then be there before those of the last one have been waited for, but no further: two
-  // barriers of each kind take turns
+  // Scores and probabilities of a tile may then be there before those of the last one have been waited for, and a warp may be a
+  // tile ahead of the others, but no further: two barriers of each kind take turns, or their phases could be mistaken
   static constexpr uint32_t kTurns = kBuffers - 1;
   static constexpr uint32_t kS = 0, kO = kBuffers * kTile;
   static_assert(kO + 2 * DP <= kTmemColumns, "tensor memory");
@@ -536,9 +536,9 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
   const uint32_t kv_full = base + L::kBars, kv_empty = kv_full + 8 * L::kSlots;
   const uint32_t q_full = kv_empty + 8 * L::kSlots, q_empty = q_full + 8;
   const uint32_t s_full = q_empty + 8, p_full = s_full + 16 * L::kTurns, o_full = p_full + 16 * L::kTurns;  // A, B each
-  const uint32_t item_full = o_full + 16, item_empty = item_full + 16;             // two slots each
+  const uint32_t item_full = o_full + 16 * L::kTurns, item_empty = item_full + 16;             // two slots each
   const uint32_t drained = item_empty + 16, h_full = drained + 8;
-  static_assert(8 * (2 * L::kSlots + 9 + 6 * L::kTurns) <= 504, "layout::kItems");
+  static_assert(8 * (2 * L::kSlots + 7 + 8 * L::kTurns) <= 504, "layout::kItems");
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + L::kBars + 504);
   item_t* items = reinterpret_cast<item_t*>(smem + L::kItems);
 
@@ -552,10 +552,10 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
     for (int x = 0; x < 2; ++x) {
       for (uint32_t k = 0; k < L::kTurns; ++k) {
         mbar_init(s_full + 8 * (x + 2 * k), 1);
+        mbar_init(o_full + 8 * (x + 2 * k), 1);
         mbar_init(p_full + 8 * (x + 2 * k), kSoftWarps / 2);
         mbar_init(h_full + 8 * (x + 2 * k), kSoftWarps / 2);
       }
-      mbar_init(o_full + 8 * x, 1);
       mbar_init(item_full + 8 * x, 1);
       mbar_init(item_empty + 8 * x, kSoftWarps + 1);
     }
@@ -855,7 +855,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
               p_ring[x].step();
               fence_after();
               pv(x, buffer, true, kTile / 32, kTile / 16);
-              if ((L::kBuffers == 3 || t + 1 == item.last[x]) && elected()) mma_commit(o_full + 8 * x);
+              if ((L::kBuffers == 3 || t + 1 == item.last[x]) && elected()) mma_commit(o_full + turn);
             }
             if (L::kBuffers == 2) next_scores(x);
           }
@@ -968,7 +968,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
           if (t > first) {
             // with two buffers the product before has finished: S could not be there otherwise
             if (L::kBuffers == 3) {
-              ok = wait(o_full + 8 * x, products - 1 & 1);
+              ok = wait(o_full + 8 * (x + 2 * (products - 1 & 1)), products - 1 >> 1 & 1);
               if (!ok) break;
               fence_after();
             }
@@ -1017,7 +1017,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
       if (!ok) break;
       const bool any = first < last;
       if (any) {
-        ok = wait(o_full + 8 * x, L::kBuffers == 3 ? products - 1 & 1 : o_ring.phase);
+        ok = L::kBuffers == 3 ? wait(o_full + 8 * (x + 2 * (products - 1 & 1)), products - 1 >> 1 & 1) : wait(o_full + 8 * x, o_ring.phase);
         if (!ok) break;
         o_ring.step();
         fence_after();

@@ -257,3 +257,21 @@ def test_a_step_without_rows_and_calls_on_two_streams():
             c()
     for s, w in zip((a, b), want):
         assert torch.equal(s.out(), w)
+
+
+@pytest.mark.parametrize("rows,states,hq,hk,d", [([90, 200, 70], [400, 130, 1000], 4, 2, 64), ([60, 33], [400, 900], 4, 4, 64),
+                                                 ([12, 9, 16], [800, 500, 300], 4, 2, 64)])
+def test_rows_of_very_different_limits_give_the_same_bits_every_time(rows, states, hq, hk, d):
+    """Warps whose rows see little, or are not there, are done with a tile before the others."""
+    rng = np.random.default_rng(sum(rows))
+    most = np.repeat(states, rows)
+    for seed in range(40):
+        s = Step(rows, states, hq, hk, d, "bf16", seed=seed, seen=rng.integers(-2, most + 3))
+        s.call()
+        want = s.out().clone()
+        for _ in range(3):
+            s.whole.fill_(7)
+            s.call()
+            assert torch.equal(s.out(), want), seed
+        if seed == 0:
+            s.check()
