@@ -205,8 +205,8 @@ __global__ void __launch_bounds__(kScanThreads, kScanBlocks) scan_kernel(const _
   uint32_t row = unit / a.segments, s = unit - row * a.segments;
   chained_begin();
   segment_t<T, Vec> next;
+  if (row < rows) next.fetch(a, row, s);  // the first one before it is known whether it is wanted
   bool live = row < rows && row_live(p, row);
-  if (live) next.fetch(a, row, s);
 #pragma unroll 1
   while (row < rows) {
     segment_t<T, Vec> seg = next;

@@ -231,7 +231,8 @@ def both(parents, lengths, table, beams, page, free, count, capacity, total, kep
 
 @pytest.mark.parametrize("n,beams,page,longest,spread", [
     (1, 1, 16, 40, False), (1, 4, 16, 600, False), (3, 8, 8, 300, True), (2, 32, 16, 200, True), (5, 5, 32, 9000, False),
-    (1, 3, 8, 5000, True), (700, 4, 16, 60, False), (1100, 3, 16, 30, True), (512, 32, 64, 100, False), (2, 2, 256, 0, True)])
+    (1, 3, 8, 5000, True), (700, 4, 16, 60, False), (1100, 3, 16, 30, True), (512, 32, 64, 100, False), (2, 2, 256, 0, True),
+    (16384, 1, 16, 40, True), (5461, 3, 32, 40, False), (3, 9, 8, 2100, True)])
 def test_tables_match_the_definition(n, beams, page, longest, spread):
     rng = np.random.default_rng(n + beams)
     lengths, table, free, total = beam_state(rng, n, beams, page, longest, spread)
