@@ -606,8 +606,9 @@ __device__ __forceinline__ uint32_t held_pages(const pages_args& a, int32_t leng
 // Few: at most kAtOnce beams, whose entries of a column a thread then keeps in registers; else they lie in shared memory.
 template <bool Few> __global__ void __launch_bounds__(kColumns) follow_kernel(const __grid_constant__ pages_args a) {
   extern __shared__ int32_t tile[];  // beams x kColumns
-  __shared__ int32_t parent[PREBA_BEAMS_MAX], length[PREBA_BEAMS_MAX];
-  __shared__ uint32_t held[PREBA_BEAMS_MAX], warp_sums[kColumns / 32], parents_of;
+  __shared__ __align__(16) int32_t parent[PREBA_BEAMS_MAX], length[PREBA_BEAMS_MAX];
+  __shared__ __align__(16) uint32_t held[PREBA_BEAMS_MAX];
+  __shared__ uint32_t warp_sums[kColumns / 32], parents_of;
   const preba_beam_pages_t& p = a.p;
   const uint32_t r = blockIdx.x / a.chunks, chunk = blockIdx.x - r * a.chunks, row0 = r * p.beams;
   const uint32_t c = chunk * kColumns + threadIdx.x;
@@ -617,6 +618,7 @@ template <bool Few> __global__ void __launch_bounds__(kColumns) follow_kernel(co
   bool bad = false;
   if (warp == 0) {
     uint32_t child_of = 0;
+    parent[lane] = -1, held[lane] = 0;
     if (lane < static_cast<int>(p.beams)) {
       const int32_t len = p.lengths[row0 + lane], par = p.parents[row0 + lane];
       const uint32_t h = len < 0 ? 0 : held_pages(a, len);
@@ -637,32 +639,49 @@ template <bool Few> __global__ void __launch_bounds__(kColumns) follow_kernel(co
     source = p.table[(row0 + parent[lane]) * p.table_stride + held[parent[lane]] - 1];
   // every thread has a column, and reads no other's
   int32_t page[kAtOnce];
-  for (uint32_t b0 = 0; b0 < p.beams; b0 += kAtOnce) {
-#pragma unroll
-    for (uint32_t k = 0; k < kAtOnce; ++k)
-      page[k] = b0 + k < p.beams && c < held[b0 + k] ? p.table[(row0 + b0 + k) * p.table_stride + c] : 0;
-#pragma unroll
-    for (uint32_t k = 0; k < kAtOnce; ++k)
-      if (b0 + k < p.beams) tile[(b0 + k) * kColumns + threadIdx.x] = page[k];
-  }
-  for (uint32_t i = 0; i < p.beams; ++i) {
+  uint32_t have = 0;  // beams with a page here, of the first kAtOnce
+  auto follow = [&](uint32_t i) {
     const int32_t from = refused ? static_cast<int32_t>(i) : parent[i];
     if (from >= 0 && c < held[from]) p.table_out[(row0 + i) * p.table_out_stride + c] = tile[from * kColumns + threadIdx.x];
+  };
+  if (Few) {
+    const int32_t* from = p.table + row0 * p.table_stride + c;
+#pragma unroll
+    for (uint32_t k = 0; k < kAtOnce; ++k) have |= (c < held[k] ? 1u : 0u) << k;
+#pragma unroll
+    for (uint32_t k = 0; k < kAtOnce; ++k, from += p.table_stride) page[k] = have >> k & 1 ? *from : 0;
+#pragma unroll
+    for (uint32_t k = 0; k < kAtOnce; ++k)
+      if (have >> k & 1) tile[k * kColumns + threadIdx.x] = page[k];
+#pragma unroll
+    for (uint32_t i = 0; i < kAtOnce; ++i)
+      if (i < p.beams) follow(i);
+  } else {
+    for (uint32_t b0 = 0; b0 < p.beams; b0 += kAtOnce) {
+#pragma unroll
+      for (uint32_t k = 0; k < kAtOnce; ++k)
+        page[k] = b0 + k < p.beams && c < held[b0 + k] ? p.table[(row0 + b0 + k) * p.table_stride + c] : 0;
+#pragma unroll
+      for (uint32_t k = 0; k < kAtOnce; ++k)
+        if (b0 + k < p.beams) tile[(b0 + k) * kColumns + threadIdx.x] = page[k];
+    }
+    for (uint32_t i = 0; i < p.beams; ++i) follow(i);
   }
   // what this column releases, a bit per beam
   uint32_t gone = 0;
   if (!refused && c >= kept) {
     if (Few) {
-      uint32_t have = 0;  // beams with a page here
-#pragma unroll
-      for (uint32_t k = 0; k < kAtOnce; ++k)
-        if (k < p.beams && c < held[k]) have |= 1u << k;
       gone = have & ~parents;
+      if (gone) {
 #pragma unroll
-      for (uint32_t b = 0; b < kAtOnce; ++b)
+        for (uint32_t b = 0; b < kAtOnce; ++b) {
+          uint32_t same = 0;
 #pragma unroll
-        for (uint32_t o = 0; o < kAtOnce; ++o)
-          if (o != b && page[o] == page[b] && (have >> o & 1) && (o < b || (parents >> o & 1))) gone &= ~(1u << b);
+          for (uint32_t o = 0; o < kAtOnce; ++o)
+            if (o != b) same |= (page[o] == page[b] ? 1u : 0u) << o;
+          if (same & have & (parents | ((1u << b) - 1))) gone &= ~(1u << b);
+        }
+      }
     } else {
       for (uint32_t b = 0; b < p.beams; ++b) {
         if (parents >> b & 1 || c >= held[b]) continue;
