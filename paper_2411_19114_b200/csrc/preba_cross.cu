@@ -1,6 +1,6 @@
 // Attention of a decoder's rows to an encoder's packed states (preba_beams.h): preba_cross_attend.
 //
-// Where few rows share a key head (the beams of a request, times the query heads of a group, up to 64) the states have to
+// Where few rows share a key head (the beams of a request, times the query heads of a group) the states have to
 // be read once and bytes bound the call; rows are too few to fill the 128 of a matrix product, but states are
 // not.  So states take the rows' place:
 //   S^T = K Q^T        128 states x rows   (tcgen05, both operands in shared memory as they lie)
@@ -30,7 +30,13 @@ namespace {
 using namespace attend;
 
 constexpr int kTile = 128;            // states of a tile
-constexpr int kFewRows = 64;          // rows on a key head that this kernel takes
+constexpr int kColumns = 64;          // rows on a key head, or a pair of them, that this kernel takes
+
+// Rows on a key head that this kernel takes.  Measured, here and by the kernels for many rows: 48 requests of up to 2000 states on
+// 8 heads of 128, 16 rows 59 and 79 us, 64 rows 67 and 87; two of up to 400, 64 rows 11 and 15.  64 requests of up
+// to 1500 on 20 heads of 64, 32 rows 80 and 120 us; 4 of them, 16 rows 18.5 and 20, 32 rows 26 and 20.  More than 32 rows of
+// two heads do not fit the columns, and one such head at a time took 134 and 122 us.
+constexpr uint32_t few_rows(uint32_t head_dim) { return head_dim <= 64 ? kColumns / 2 : kColumns; }
 constexpr int kSoftWarps = 4, kSoftThreads = 32 * kSoftWarps;
 constexpr int kCopyWarp = 4, kMmaWarp = 5;
 constexpr int kThreads = 192;
@@ -43,18 +49,19 @@ constexpr uint64_t kCounterBytes = kMaxTileCtas * 4;  // at the workspace's star
 
 // D: head_dim rounded up to 64 or 128.  H: key heads of a piece.  Heads of up to 64 are taken in pairs, whose rows in memory
 // lie side by side more often than not: 64 requests of 5 beams over 1500 states of 20 heads of 64, single heads 76 us (61 if
-// each head's states lie together), pairs 60 us.  The product with the values then has the elements of both heads as its 128
+// each head's states lay together), pairs 68 to 70 either way, and 60 by what came after.  The product with the values then has the elements of both heads as its 128
 // rows, and of its columns each half belongs to one of them.  N: columns, R rows of each head.
 template <int D, int H, int R> struct layout {
   static constexpr int N = H * R;
-  static constexpr int kHalves = H * D / 64;                // of 64 elements: of one head, or of a pair
+  static_assert(H * D == 128, "a head of 128 or two of 64");
+  static constexpr int kHalves = 2;                         // of 64 elements: of one head, or of a pair
   static constexpr uint32_t kHalf = kTile * 128;            // 64 elements of 128 states
   static constexpr uint32_t kSlot = kHalves * kHalf;        // a tile of keys, or of values
-  static constexpr int kSlots = kHalves == 1 ? 10 : N <= 32 ? 6 : 5;
+  static constexpr int kSlots = N <= 32 ? 6 : 5;
   // Two tiles of P^T, 128 states of N rows each in lines of 128 bytes: side by side if they fit, else one after the other
   static constexpr uint32_t kP = kSlots * kSlot;
   static constexpr uint32_t kPNext = N <= 32 ? N * 2 : kTile * 128;
-  static constexpr uint32_t kQ = kP + (N <= 32 ? 1 : 2) * kTile * 128;  // two sets of queries: 64 elements of R rows, once or twice
+  static constexpr uint32_t kQ = kP + (N <= 32 ? 1 : 2) * kTile * 128;  // two sets of queries: 64 elements of R rows, twice
   static constexpr uint32_t kQSize = kHalves * R * 128;
   static constexpr uint32_t kStats = kQ + 2 * kQSize;
   static constexpr uint32_t kBars = kStats + 8 * N * 4 + N * 8;
@@ -62,14 +69,11 @@ template <int D, int H, int R> struct layout {
   static constexpr uint32_t kBytes = kControl + 256;
   // Tensor memory columns.
   static constexpr uint32_t kS = 0, kO = 2 * N;
-  static constexpr uint32_t kColumns = N == 64 ? 256 : N == 32 ? 128 : 64;
-  // One head of 64: the product has 128 rows all the same; what the upper 64 hold is read from behind the tile (there is
-  // always something of this CTA's there) and never looked at.
-  static constexpr uint32_t kLeading = kHalf;
+  static constexpr uint32_t kTmem = N == 64 ? 256 : N == 32 ? 128 : 64;
   static_assert(kBars % 8 == 0 && kBytes <= 227 * 1024 && kP >= kTile * 128, "shared memory");
 };
 // Floats of a partial sum: O^T column by column, then a maximum and a sum for each.
-template <int D> constexpr uint32_t kPartial = kFewRows * D + 2 * kFewRows;
+template <int D> constexpr uint32_t kPartial = kColumns * D + 2 * kColumns;
 constexpr uint32_t kDirect = 4;  // pieces of a (request, head) that the CTA with the first of them joins on the spot, at most
 
 // What a call is about beside the sizes it shares with the paged attention.
@@ -119,7 +123,7 @@ __device__ __forceinline__ bool load_entry(const cross_args& a, uint32_t r, entr
 // Where a CTA's run begins: the block adds up the units of all requests, each thread of a run of them.  The units of a (request,
 // key head) are one for its beginning and end, which cost about what a tile does, and one for each tile.  Where there is a CTA
 // for every (request, key head), and none of them is long, each takes one and nothing has to be joined (two
-// requests of up to 3 tiles on 8 heads: 8.1 us, in equal runs 11.3).
+// requests of up to 3 tiles on 8 heads: 7.9 us, in equal runs 11.3).
 __device__ __forceinline__ void find_run(const cross_args& a, control_t& ctl) {
   const preba_pages_attend_t& p = a.p;
   const uint32_t chunk = (p.n + kThreads - 1) / kThreads;
@@ -322,7 +326,7 @@ cross_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
   // would wait for this CTA as this CTA waits for it.
   if (warp == kMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&ctl.tmem)),
-                 "n"(L::kColumns)
+                 "n"(L::kTmem)
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -440,7 +444,7 @@ cross_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
         ok = wait(p_full + 8 * b, (n_p >> 1) & 1);
         if (!ok) break;
         fence_after();
-        const uint32_t v_op = __shfl_sync(kFull, operand(base + v_slot * L::kSlot, L::kLeading), 0);
+        const uint32_t v_op = __shfl_sync(kFull, operand(base + v_slot * L::kSlot, L::kHalf), 0);
         const uint32_t p_op = __shfl_sync(kFull, operand(base + L::kP + b * L::kPNext, 16), 0);
         const uint32_t d = __shfl_sync(kFull, tmem + L::kO, 0);
         if (elected()) {
@@ -644,7 +648,7 @@ cross_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
             stat[0] = make_float2(marked(m, sum), sum);
 #pragma unroll
             for (uint32_t k = 1; k < kDirect; ++k)
-              stat[k] = x.first + k <= x.last ? __ldcg(reinterpret_cast<const float2*>(partial_of<D>(a, x.first + k, 0) + kFewRows * D) + r)
+              stat[k] = x.first + k <= x.last ? __ldcg(reinterpret_cast<const float2*>(partial_of<D>(a, x.first + k, 0) + kColumns * D) + r)
                                               : make_float2(-INFINITY, 0.f);
             float top = -INFINITY;
 #pragma unroll
@@ -698,7 +702,7 @@ cross_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
         }
       } else {
         float* part = partial_of<D>(a, blockIdx.x, begins);
-        if (row_there) reinterpret_cast<float2*>(part + kFewRows * D)[r] = make_float2(marked(m, sum), sum);
+        if (row_there) reinterpret_cast<float2*>(part + kColumns * D)[r] = make_float2(marked(m, sum), sum);
         if (e < D) {
 #pragma unroll
           for (int c = 0; c < kMine; ++c)
@@ -752,7 +756,7 @@ cross_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
             float top = -INFINITY, sum = 0.f;
 #pragma unroll 8
             for (uint32_t k = 0; k < count; ++k) {
-              const float2 v = __ldcg(reinterpret_cast<const float2*>(partial_of<D>(a, x.first + k, k == 0) + kFewRows * D) + r);
+              const float2 v = __ldcg(reinterpret_cast<const float2*>(partial_of<D>(a, x.first + k, k == 0) + kColumns * D) + r);
               stat[k * N + r] = v;
               top = fmaxf(top, v.x);
             }
@@ -812,7 +816,7 @@ cross_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ 
   __syncthreads();
   fence_after();
   if (warp == kMmaWarp)
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(L::kColumns) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(L::kTmem) : "memory");
 }
 
 bool cross_sizes_ok(uint32_t n, uint32_t tokens, uint32_t heads_q, uint32_t heads_kv, uint32_t head_dim) {
@@ -844,9 +848,7 @@ template <typename T, int D, int H, int R> cudaError_t launch_cross(cross_args& 
   return launch_chained(cross_kernel<T, D, H, R>, a.grid, kThreads, L::kBytes, stream, map_q, map_k, map_v, a);
 }
 template <typename T> cudaError_t launch_few(cross_args& a, uint32_t rows, cudaStream_t stream) {
-  if (a.p.head_dim <= 64)
-    return rows <= 16 ? launch_cross<T, 64, 2, 16>(a, stream) : rows <= 32 ? launch_cross<T, 64, 2, 32>(a, stream)
-                                                                           : launch_cross<T, 64, 1, 64>(a, stream);
+  if (a.p.head_dim <= 64) return rows <= 16 ? launch_cross<T, 64, 2, 16>(a, stream) : launch_cross<T, 64, 2, 32>(a, stream);
   return rows <= 16 ? launch_cross<T, 128, 1, 16>(a, stream) : rows <= 32 ? launch_cross<T, 128, 1, 32>(a, stream)
                                                                           : launch_cross<T, 128, 1, 64>(a, stream);
 }
@@ -917,7 +919,7 @@ extern "C" int preba_cross_attend(const preba_cross_attend_t* req, void* stream)
   if (err != cudaSuccess) return finish(err);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const uint64_t rows = static_cast<uint64_t>(group) * p.max_q;
-  if (rows > kFewRows)
+  if (rows > few_rows(c.head_dim))
     return finish(launch_packed_tiles(p, c.cu_k, c.seen, c.states, sms, static_cast<uint8_t*>(c.workspace) + kCounterBytes, s));
   cross_args a{p, c.cu_k, c.seen, c.states, group, static_cast<uint32_t>(std::min(sms, kMaxTileCtas)), p.max_q, 0};
   return finish(c.dtype == PREBA_F16 ? launch_few<__half>(a, static_cast<uint32_t>(rows), s)

@@ -93,6 +93,8 @@ class Step:
     ([3, 0, 2, 3], [40, 50, 0, 256], 6, 2, 72), ([0, 0, 1], [9, 0, 3], 2, 2, 64), ([64], [5000], 1, 1, 64),
     ([2], [20000], 7, 1, 128), ([4] * 40, list(range(1, 161, 4)), 4, 4, 40), ([1] * 300, [7] * 300, 2, 1, 64),
     ([1], [3], 64, 1, 64), ([13], [300], 5, 1, 128),
+    # as many rows as the kernel takes, and one more
+    ([32, 5], [300, 1], 3, 3, 64), ([33, 5], [300, 1], 3, 3, 64), ([64], [300], 2, 2, 128), ([65], [300], 2, 2, 128),
     # runs that end with a piece's beginning but no tile of it
     ([16, 2], [30000, 500], 2, 1, 128), ([2] * 5, [20000, 128 * 89, 128 * 90, 128 * 91, 40000], 3, 1, 64)])
 def test_few_rows_match_the_definition(rows, states, hq, hk, d, dtype):
