@@ -480,10 +480,10 @@ __global__ void __launch_bounds__(kChooseThreads) choose_kernel(const __grid_con
     segment_t<T, Vec> words;
     words.fetch(a, row0 + seg.row, seg.at);
     const double last = c.best[chosen - 1].rank, weight = c.weight[seg.row];
-    // the least logit that may do, less what it may be off by
+    // the least logit that may do, less what it may be off by; where a weight has no reciprocal, all may
     const double level = last * (1.f / static_cast<float>(weight)), least = level - c.score[seg.row] + c.lse[seg.row];
     const float least_x =
-        full ? static_cast<float>(least - 1e-6 * (1 + fabs(level) + fabs(c.score[seg.row]) + fabs(c.lse[seg.row]))) : -INFINITY;
+        full && isfinite(level) ? static_cast<float>(least - 1e-6 * (1 + fabs(level) + fabs(c.score[seg.row]) + fabs(c.lse[seg.row]))) : -INFINITY;
     words.finish(a, seg.at);
     uint32_t enough = 0;  // a bit for each of the lane's elements
 #pragma unroll

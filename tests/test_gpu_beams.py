@@ -351,3 +351,14 @@ def test_equal_logits_in_many_segments(width):
     for ended in (None, done):
         got = run_select(x, scores, width, beams, 9 if ended is not None else -1, ended)
         check_select(got, ob.select(x.double().cpu().numpy(), scores, width, beams, 9 if ended is not None else -1, ended))
+
+
+@pytest.mark.parametrize("weights", [[1e-40, 1e-40, 2e-40], [1e-44, 1.0, 1e-44], [3e38, 1e38, 2e38]])
+@pytest.mark.parametrize("score", [300.0, -300.0])
+def test_weights_whose_reciprocals_leave_the_type(weights, score):
+    beams, width = 3, 5
+    rng = np.random.default_rng(4)
+    logits, x = made(rng, 2 * beams, 5000, "fp32")
+    scores = np.float32(score + 10 * rng.random(2 * beams))
+    w = np.float32(weights * 2)
+    check_select(run_select(logits, scores, width, beams, weights=w), ob.select(x, scores, width, beams, weights=w))
