@@ -140,7 +140,8 @@ int preba_beam_select(const preba_beam_select_t* req, void* stream);
  * preba_beam_pages — the block table of the next beams.  New row i of request r takes over the pages and the
  * length of row parents[i] of r (negative: the row is empty, its length 0).  Full pages are shared: beams of one
  * request may hold the same page at the same place of their rows, and only there.  The last page of a
- * length that does not fill it is open, the next token is written there: the first child of a beam keeps it,
+ * length that does not fill it is open, the next token is written there, so it belongs to one beam (a search that begins with
+ * one prompt begins with one beam that has it): the first child of a beam keeps it,
  * every other child gets a page of its own, and copies[i] = {from, to, tokens, 0} says what preba_pages_copy has to
  * bring there (all zeros where nothing has).  A page that no new row holds is released, unless it lies at one of the first
  * kept[r] places of its row (pages that the request shares with others).

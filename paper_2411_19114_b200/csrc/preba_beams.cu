@@ -20,6 +20,9 @@ using attend::report;
 // request lie in the `width` segments with the best maxima (in the order of rank, beam, segment), because
 // every other segment has `width` maxima before all that it holds.  The second kernel, a block per request, adds the
 // sums up in 64 bits, orders the maxima, reads those few segments again and orders what they hold.
+//
+// 64 requests of 8 beams, 128000 tokens in bf16: 31 to 32 us a call, of which 20 are the bytes at the measured copy rate; the scan
+// takes about 24 (exponentials 65 % of their rate, issue slots 59 %).  4 beams of 32000 tokens: 6.9 us, two launches.
 
 constexpr int kSegmentWords = 512;  // of 32 bits
 constexpr int kLaneWords = kSegmentWords / 32;
@@ -586,6 +589,7 @@ template <typename T, bool Vec> cudaError_t launch_select(const select_args& a, 
 // childless beam before it has.  A first kernel, a block per 256 columns of a request, writes the new rows and
 // lists what is released.  In a second every block adds all requests' numbers up for itself (they are few and come from
 // L2), so that it knows where its own requests' copies and pages stand among all, and hands out without asking another.
+// 128 requests of 8 beams over 8192 tokens: 10.6 us (one block that hands out for all: 35); 2 of 4: 6.5 us, two launches.
 
 constexpr int kColumns = 256;
 constexpr int kHandThreads = 256;
@@ -928,7 +932,8 @@ uint64_t pages_workspace(uint32_t n, uint32_t beams, uint32_t table_width) {
 // ---- preba_pages_copy -------------------------------------------------------------------------------
 //
 // Bytes bound it: what is copied, in and out once.  The rows that have a copy are found by every block for itself, a
-// job is a row's page in one cache, keys or values, and blocks take jobs in turn.
+// job is a row's page in one cache, keys or values, and blocks take jobs in turn.  64 requests of 8 beams, 12 layers, 304 MB in
+// and out: 49 to 50 us, 94 % of the measured copy rate; 4 requests of 4 beams: 3.0 us, a launch.
 
 constexpr int kCopyThreads = 256;
 constexpr uint32_t kCopyRows = 1024;  // looked at in one go
