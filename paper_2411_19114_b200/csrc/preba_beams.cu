@@ -589,7 +589,7 @@ template <typename T, bool Vec> cudaError_t launch_select(const select_args& a, 
 // childless beam before it has.  A first kernel, a block per 256 columns of a request, writes the new rows and
 // lists what is released.  In a second every block adds all requests' numbers up for itself (they are few and come from
 // L2), so that it knows where its own requests' copies and pages stand among all, and hands out without asking another.
-// 128 requests of 8 beams over 8192 tokens: 10.6 us (one block that hands out for all: 35); 2 of 4: 6.5 us, two launches.
+// 128 requests of 8 beams over 8192 tokens: 10.6 to 11.2 us (one block that hands out for all: 35); 2 of 4: 6.5 us, two launches.
 
 constexpr int kColumns = 256;
 constexpr int kHandThreads = 256;
@@ -933,7 +933,7 @@ uint64_t pages_workspace(uint32_t n, uint32_t beams, uint32_t table_width) {
 //
 // Bytes bound it: what is copied, in and out once.  The rows that have a copy are found by every block for itself, a
 // job is a row's page in one cache, keys or values, and blocks take jobs in turn.  64 requests of 8 beams, 12 layers, 304 MB in
-// and out: 49 to 50 us, 94 % of the measured copy rate; 4 requests of 4 beams: 3.0 us, a launch.
+// and out: 49 to 50 us, 94 % of the measured copy rate; 4 requests of 4 beams: 3.0 to 3.6 us, a launch.
 
 constexpr int kCopyThreads = 256;
 constexpr uint32_t kCopyRows = 1024;  // looked at in one go
