@@ -589,6 +589,9 @@ template <typename T, bool Vec> cudaError_t launch_select(const select_args& a, 
 // childless beam before it has.  A first kernel, a block per 256 columns of a request, writes the new rows and
 // lists what is released.  In a second every block adds all requests' numbers up for itself (they are few and come from
 // L2), so that it knows where its own requests' copies and pages stand among all, and hands out without asking another.
+// Only then it is known who is refused for want of pages, and a refused row keeps what lies behind its last page: so where the
+// stack may not suffice, the first kernel leaves the places of a row behind its own last page to the second (which then takes 0.2
+// to 0.4 us more).
 // 128 requests of 8 beams over 8192 tokens: 10.6 to 11.2 us (one block that hands out for all: 35); 2 of 4: 6.5 us, two launches.
 
 constexpr int kColumns = 256;
@@ -607,6 +610,16 @@ __device__ __forceinline__ uint32_t held_pages(const pages_args& a, int32_t leng
   return (static_cast<uint32_t>(length) + (1u << a.page_shift) - 1) >> a.page_shift;
 }
 
+// Pages on the stack; one whose count cannot be has none.
+__device__ __forceinline__ int64_t on_stack(const preba_beam_pages_t& p) {
+  const int64_t count = *p.free_count;
+  return count < 0 || count > p.free_capacity ? 0 : count;
+}
+// Whether the stack alone has a page for every row that can need one: then nobody is refused for want of pages.
+__device__ __forceinline__ bool plenty(const preba_beam_pages_t& p, int64_t count) {
+  return count >= static_cast<int64_t>(p.n) * (p.beams - 1);
+}
+
 // Few: at most kAtOnce beams, whose entries of a column a thread then keeps in registers; else they lie in shared memory.
 template <bool Few> __global__ void __launch_bounds__(kColumns) follow_kernel(const __grid_constant__ pages_args a) {
   extern __shared__ int32_t tile[];  // beams x kColumns
@@ -619,6 +632,7 @@ template <bool Few> __global__ void __launch_bounds__(kColumns) follow_kernel(co
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   chained_begin();
   const int64_t kept = p.kept ? p.kept[r] : 0;
+  const bool sure = plenty(p, on_stack(p));
   bool bad = false;
   if (warp == 0) {
     uint32_t child_of = 0;
@@ -646,7 +660,7 @@ template <bool Few> __global__ void __launch_bounds__(kColumns) follow_kernel(co
   uint32_t have = 0;  // beams with a page here, of the first kAtOnce
   auto follow = [&](uint32_t i) {
     const int32_t from = refused ? static_cast<int32_t>(i) : parent[i];
-    if (from >= 0 && c < held[from]) p.table_out[(row0 + i) * p.table_out_stride + c] = tile[from * kColumns + threadIdx.x];
+    if (from >= 0 && c < held[from] && (sure || c < held[i])) p.table_out[(row0 + i) * p.table_out_stride + c] = tile[from * kColumns + threadIdx.x];
   };
   if (Few) {
     const int32_t* from = p.table + row0 * p.table_stride + c;
@@ -784,11 +798,8 @@ __global__ void __launch_bounds__(kHandThreads) hand_out_kernel(const __grid_con
   uint8_t* served = hand_smem + p.n * sizeof(sums_t);    // n
   __shared__ both_t warp_sums[kHandThreads / 32];
   chained_begin();
-  int64_t count = *p.free_count;
-  if (count < 0 || count > p.free_capacity) {
-    if (blockIdx.x == 0 && threadIdx.x == 0) report(p.status, PREBA_ERR_BAD_TABLE);
-    count = 0;
-  }
+  const int64_t count = on_stack(p);
+  if (count != *p.free_count && blockIdx.x == 0 && threadIdx.x == 0) report(p.status, PREBA_ERR_BAD_TABLE);
   // what every request asks for and releases
   for (uint32_t r = threadIdx.x; r < p.n; r += kHandThreads) {
     const int32_t need = a.need[r];
@@ -908,13 +919,26 @@ __global__ void __launch_bounds__(kHandThreads) hand_out_kernel(const __grid_con
   }
   if (blockIdx.x == 0 && threadIdx.x == 0)
     *p.free_left = static_cast<int32_t>(min(count + total.released - total.copies, static_cast<int64_t>(p.free_capacity)));
-  // requests that were refused for want of pages: their rows as they were
+  if (plenty(p, count)) return;
+  // rows of requests that were refused for want of pages as they were; of the others, what was left to this kernel
   for (uint32_t i = b0 * p.beams + warp; i < b1 * p.beams; i += kHandThreads / 32) {
-    const uint32_t r = i / p.beams;
-    if (served[r] || a.need[r] < 0) continue;
-    const uint32_t held = held_pages(a, p.lengths[i]);
-    for (uint32_t c = lane; c < held; c += 32) p.table_out[i * p.table_out_stride + c] = p.table[i * p.table_stride + c];
-    if (lane == 0) p.lengths_out[i] = 0;
+    const uint32_t r = i / p.beams, row0 = r * p.beams;
+    if (a.need[r] < 0) continue;
+    const uint32_t own = held_pages(a, p.lengths[i]);
+    uint32_t from = i, first = 0, last = own;
+    if (served[r]) {
+      const int32_t parent = p.parents[i];
+      if (parent < 0) continue;
+      from = row0 + parent;
+      const int32_t length = p.lengths[from];
+      first = own, last = held_pages(a, length);
+      // the last page of all children but the first is another one, and written above
+      const bool again = __any_sync(kFull, lane < static_cast<int>(i - row0) && p.parents[row0 + min(lane, static_cast<int>(i - row0))] == parent);
+      if (again && (length & ((1u << a.page_shift) - 1))) --last;
+    } else if (lane == 0) {
+      p.lengths_out[i] = 0;
+    }
+    for (uint32_t c = first + lane; c < last; c += 32) p.table_out[i * p.table_out_stride + c] = p.table[from * p.table_stride + c];
   }
 }
 
