@@ -153,14 +153,16 @@ int preba_beam_select(const preba_beam_select_t* req, void* stream);
  * (PREBA_ERR_BAD_TABLE), or if the free pages, what the requests before it that were not refused left of them, and its
  * own released pages do not suffice (PREBA_ERR_BUFFER_TOO_SMALL): its rows of table_out are as in `table`, their lengths
  * 0, nothing is copied or released; a caller that takes lengths_out over leaves out the refused requests' zeros.
+ * Every request is refused if *free_count is negative or above free_capacity (PREBA_ERR_BAD_TABLE); the stack stays as it is, and
+ * *free_left is 0.
  * A released page that is not a page number is dropped, as is one for which the stack has no room (PREBA_ERR_BAD_TABLE);
  * a page from the stack that is not one is not copied to (the same).  Entries of table_out behind the last page
  * of a row are left as they were.
  *   preba_beam_pages_query  bytes of workspace (host only), as for preba_beam_select.
  * Errors: PREBA_ERR_INVALID_ARG (NULL, n, beams or table_width 0, n * beams above PREBA_PAGES_MAX_REQUESTS, beams above
  * PREBA_BEAMS_MAX, page_size not a power of two in 8 .. PREBA_PAGES_MAX_PAGE, pages * page_size above 2^31 - 1, a stride
- * below table_width, table_width * page_size above 2^31 - 1, n * beams * table_width above 2^32 - 1, table_out == table, free_left == free_count, copies
- * or the workspace not 16-byte aligned), PREBA_ERR_BUFFER_TOO_SMALL (workspace), PREBA_ERR_CUDA.
+ * below table_width, table_width * page_size above 2^31 - 1, n * beams * table_width above 2^32 - 1, table_out == table, lengths_out == lengths,
+ * free_left == free_count, free_capacity above 2^31 - 1, copies or the workspace not 16-byte aligned), PREBA_ERR_BUFFER_TOO_SMALL (workspace), PREBA_ERR_CUDA.
  */
 typedef struct {
   const int32_t* parents;     /* DEVICE, n * beams */

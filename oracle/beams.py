@@ -50,18 +50,19 @@ def select(logits, scores, width, beams, end=-1, done=None, allowed=None, weight
 
 def pages(parents, lengths, table, beams, page, free, count, capacity, total, kept=None):
     """The next block table and what belongs to it.  ``free``: the stack's memory (``capacity`` numbers), of which
-    ``count`` are on it; entries of the table that are not written are -7."""
+    ``count`` are on it, or it is no stack and every request is refused; entries of the table that are not written are -7."""
     table = np.asarray(table)
     rows, width = table.shape
     out, free = np.full((rows, width), -7), np.array(free)
     lengths_out, copies = np.zeros(rows, dtype=np.int64), np.zeros((rows, 4), dtype=np.int64)
-    bad = short = False
-    left = count
+    short = False
+    bad = no_stack = not 0 <= count <= capacity
+    left = count = 0 if no_stack else count
     served = []
     for r in range(rows // beams):
         mine = range(r * beams, (r + 1) * beams)
         held = [-(-int(lengths[i]) // page) for i in mine]
-        if any(lengths[i] < 0 or h > width or parents[i] >= beams for i, h in zip(mine, held)):
+        if no_stack or any(lengths[i] < 0 or h > width or parents[i] >= beams for i, h in zip(mine, held)):
             bad = True
             for i, h in zip(mine, held):
                 out[i, :max(0, min(h, width))] = table[i, :max(0, min(h, width))]

@@ -590,8 +590,8 @@ template <typename T, bool Vec> cudaError_t launch_select(const select_args& a, 
 // lists what is released.  In a second every block adds all requests' numbers up for itself (they are few and come from
 // L2), so that it knows where its own requests' copies and pages stand among all, and hands out without asking another.
 // Only then it is known who is refused for want of pages, and a refused row keeps what lies behind its last page: so where the
-// stack may not suffice, the first kernel leaves the places of a row behind its own last page to the second (which then takes 0.2
-// to 0.4 us more).
+// stack may not suffice, the first kernel leaves the places of a row behind its own last page to the second (which then takes 0.3
+// to 0.5 us more).
 // 128 requests of 8 beams over 8192 tokens: 10.6 to 11.2 us (one block that hands out for all: 35); 2 of 4: 6.5 us, two launches.
 
 constexpr int kColumns = 256;
@@ -610,10 +610,10 @@ __device__ __forceinline__ uint32_t held_pages(const pages_args& a, int32_t leng
   return (static_cast<uint32_t>(length) + (1u << a.page_shift) - 1) >> a.page_shift;
 }
 
-// Pages on the stack; one whose count cannot be has none.
+// Pages on the stack, or -1 where that cannot be: what lies there is then not known, and no request is served.
 __device__ __forceinline__ int64_t on_stack(const preba_beam_pages_t& p) {
   const int64_t count = *p.free_count;
-  return count < 0 || count > p.free_capacity ? 0 : count;
+  return count < 0 || count > p.free_capacity ? -1 : count;
 }
 // Whether the stack alone has a page for every row that can need one: then nobody is refused for want of pages.
 __device__ __forceinline__ bool plenty(const preba_beam_pages_t& p, int64_t count) {
@@ -798,15 +798,19 @@ __global__ void __launch_bounds__(kHandThreads) hand_out_kernel(const __grid_con
   uint8_t* served = hand_smem + p.n * sizeof(sums_t);    // n
   __shared__ both_t warp_sums[kHandThreads / 32];
   chained_begin();
-  const int64_t count = on_stack(p);
-  if (count != *p.free_count && blockIdx.x == 0 && threadIdx.x == 0) report(p.status, PREBA_ERR_BAD_TABLE);
+  int64_t count = on_stack(p);
+  const bool stack = count >= 0;
+  if (!stack) {
+    if (blockIdx.x == 0 && threadIdx.x == 0) report(p.status, PREBA_ERR_BAD_TABLE);
+    count = 0;
+  }
   // what every request asks for and releases
   for (uint32_t r = threadIdx.x; r < p.n; r += kHandThreads) {
     const int32_t need = a.need[r];
     uint32_t released = 0;
 #pragma unroll 4
     for (uint32_t k = 0; k < a.chunks; ++k) released += a.counts[r * a.chunks + k];
-    served[r] = need >= 0;
+    served[r] = need >= 0 && stack;
     sums[r] = {static_cast<uint32_t>(max(need, 0)), released};  // one at fault releases nothing
   }
   __syncthreads();
@@ -919,8 +923,8 @@ __global__ void __launch_bounds__(kHandThreads) hand_out_kernel(const __grid_con
   }
   if (blockIdx.x == 0 && threadIdx.x == 0)
     *p.free_left = static_cast<int32_t>(min(count + total.released - total.copies, static_cast<int64_t>(p.free_capacity)));
-  if (plenty(p, count)) return;
-  // rows of requests that were refused for want of pages as they were; of the others, what was left to this kernel
+  if (stack && plenty(p, count)) return;
+  // rows of requests that were refused for want of pages, or of a stack, as they were; of the others, what was left to this kernel
   for (uint32_t i = b0 * p.beams + warp; i < b1 * p.beams; i += kHandThreads / 32) {
     const uint32_t r = i / p.beams, row0 = r * p.beams;
     if (a.need[r] < 0) continue;
