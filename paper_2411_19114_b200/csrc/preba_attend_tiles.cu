@@ -420,6 +420,8 @@ __device__ __forceinline__ void plan_own(const tiles_args& a, own_plan_t& plan, 
     pair[k] = {lo, i - plan.pairs_before[lo], 0, seen_tiles, q.row, q.rows, q.keys, 0};
     tiles += pair[k].tiles + kSetUp<Packed>;
   }
+  // the limits lie where the copy warp's first keys and values go once this returns
+  if (limited) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   uint32_t total;
   uint32_t before = cta_exclusive<kThreads>(tiles, plan.sums, total);
   const uint32_t units = total * p.heads_kv;
