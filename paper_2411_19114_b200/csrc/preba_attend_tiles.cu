@@ -123,7 +123,7 @@ static_assert(sizeof(run_t) == 48, "three vector loads");
 struct tiles_args {
   preba_pages_attend_t p;
   uint32_t page_shift, group, tokens_per_tile, box_rows, box_shift, grid, max_pairs;
-  uint32_t own_plan;  // every CTA makes the plan for itself: it is small and sure to be a line
+  uint32_t own_plan;  // every CTA makes the plan for itself: it is small, and a line (plans_own())
   tiles_head* head;
   pair_t* pairs;
   run_t* runs;        // one per CTA
@@ -321,8 +321,8 @@ __global__ void __launch_bounds__(kPlanThreads) tiles_plan_kernel(const tiles_ar
 }
 static_assert(kBins == kPlanThreads, "one bin per thread in the sum");
 
-// The same by a CTA of the kernel itself, for itself: where there are few pairs, all of them are certain to
-// form one line, and a CTA needs its own run of it only.  One launch and 1.6 to 5 us less per call (4 chunks of 32
+// The same by a CTA of the kernel itself, for itself: where there are few pairs, all of them form one line (plans_own()), and a
+// CTA needs its own run of it only.  One launch and 1.6 to 5 us less per call (4 chunks of 32
 // tokens over 500 keys 16.5 -> 14.9 us, 512 tokens over 30000 keys 247 -> 241 us).
 static_assert(kOwnPairs == 3 * kMaxTileCtas, "fewer than this, and they cannot be claimed one by one");
 
@@ -1215,7 +1215,7 @@ cudaError_t launch_planned(tiles_args& a, int sms, uint64_t keys_at_most, void* 
   a.order = reinterpret_cast<uint32_t*>(at);
   at += up16(4 * pairs);
   a.partials = reinterpret_cast<float4*>(at);
-  a.own_plan = plans_own(pairs, p.heads_kv, a.grid, keys_at_most);
+  a.own_plan = plans_own(pairs, p.heads_kv, a.grid, keys_at_most, kSetUp<Packed>);
   const size_t smem = kPlanThreads * sizeof(pair_t) + 4 * (static_cast<size_t>(p.n) + 1);
   if (smem > 40 * 1024) {  // beside 5 KB of its own; 48 KB need no leave
     const cudaError_t err = cudaFuncSetAttribute(tiles_plan_kernel<Packed>, cudaFuncAttributeMaxDynamicSharedMemorySize,
