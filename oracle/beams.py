@@ -21,10 +21,10 @@ def select(logits, scores, width, beams, end=-1, done=None, allowed=None, weight
         for b in range(beams):
             i = r * beams + b
             score, weight = float(scores[i]), 1.0 if weights is None else float(weights[i])
-            if score == -math.inf:
-                continue
             if math.isnan(score) or score == math.inf or not 0 < weight < math.inf:
                 bad = True
+                continue
+            if score == -math.inf:
                 continue
             if done is not None and done[i]:
                 offers.append((-weight * score, b, 0.0, end, score, True))

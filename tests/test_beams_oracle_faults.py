@@ -1,10 +1,20 @@
-"""oracle/beams.py: a stack whose count cannot be."""
+"""oracle/beams.py: what is reported although nothing is offered, and a stack whose count cannot be."""
 from __future__ import annotations
+
+import math
 
 import numpy as np
 import pytest
 
 from oracle import beams as ob
+
+
+@pytest.mark.parametrize("score,done", [(-math.inf, False), (-math.inf, True), (-1.0, True), (-1.0, False)])
+@pytest.mark.parametrize("weight,fault", [(1.0, False), (0.0, True), (-2.0, True), (math.inf, True), (math.nan, True)])
+def test_a_weight_is_looked_at_in_every_row(score, done, weight, fault):
+    tokens, *_, bad = ob.select([[0, 1]], [score], 2, 1, end=1, done=[done], weights=[weight])
+    assert bad == fault
+    assert (tokens == -1).all() == (fault or score == -math.inf)
 
 
 @pytest.mark.parametrize("count", [-1, 5])
