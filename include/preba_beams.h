@@ -47,13 +47,15 @@ extern "C" {
  *                             the caller zeroes the workspace once, every call leaves its counters
  *                             zeroed again; calls that may overlap on the device need one each.
  * A request is skipped (its rows are not written) and PREBA_ERR_BAD_TABLE stored if its rows or states are out of range or
- * its rows more than max_q.
+ * its rows more than max_q.  Requests whose states or rows overlap (only with others skipped between them can they) may
+ * come to more work than n, tokens and states allow for: then PREBA_ERR_BAD_TABLE is stored and any rows may be left unwritten.
  * Every wait of the kernels has a limit.  If one runs out, PREBA_ERR_TIMEOUT is stored and the rows that the
  * call would have written hold anything; nothing else does, and the workspace is left as by any call.
  * Errors: PREBA_ERR_INVALID_ARG (NULL, sizes of 0, n above PREBA_PAGES_MAX_REQUESTS, tokens or states above
  * PREBA_PAGES_MAX_KEYS, a base that is not 16-byte aligned, a stride that is not a multiple of 8, heads_q not a multiple of
  * heads_kv, heads_q above 65535, more than 128 query heads on one key head, head_dim not a multiple of 8 in
- * 8 .. PREBA_PAGES_MAX_HEAD_DIM, a stride of 0 on an axis of q, k or v that has more than one entry, so many states that
+ * 8 .. PREBA_PAGES_MAX_HEAD_DIM, another dtype than the two, a scale that is not positive and finite, a stride of 2^38 or more,
+ * a stride of 0 on an axis of q, k or v that has more than one entry, so many states that
  * heads_kv * (2 * n + states / 128) passes 2e9, or so many rows that heads_kv * (n + tokens / (2 * g)) passes 2^31 - 1, where
  * g = 128 * heads_kv / heads_q rounded down), PREBA_ERR_BUFFER_TOO_SMALL (workspace), PREBA_ERR_CUDA.
  */
@@ -103,10 +105,11 @@ int preba_cross_attend(const preba_cross_attend_t* req, void* stream);
  * once.  Results do not depend on timing, and rows with equal logits have equal sums.
  *   preba_beam_select_query  bytes of workspace (host only); its contents mean nothing before and after a call;
  *                            calls that may overlap on the device need one each.
- * Outputs are distinct from inputs.  Two kernel launches.
+ * Outputs are distinct from inputs (scores_out == scores and done_out == done are refused).  Two kernel launches.
  * Errors: PREBA_ERR_INVALID_ARG (NULL, sizes of 0 or above the limits here, n * beams above
  * PREBA_PAGES_MAX_REQUESTS, a base that is not aligned to its elements, the workspace to 16 bytes, row_stride below vocab
- * with more than one row, end_token not a token where `done` is given, another dtype than the three),
+ * or allowed_stride not 0 and below a row's words with more than one row, either of 2^38 or more, end_token below -1 or not below
+ * vocab, or -1 where `done` is given, another dtype than the three),
  * PREBA_ERR_BUFFER_TOO_SMALL (workspace), PREBA_ERR_CUDA.
  */
 typedef struct {
@@ -161,8 +164,9 @@ int preba_beam_select(const preba_beam_select_t* req, void* stream);
  *   preba_beam_pages_query  bytes of workspace (host only), as for preba_beam_select.
  * Errors: PREBA_ERR_INVALID_ARG (NULL, n, beams or table_width 0, n * beams above PREBA_PAGES_MAX_REQUESTS, beams above
  * PREBA_BEAMS_MAX, page_size not a power of two in 8 .. PREBA_PAGES_MAX_PAGE, pages * page_size above 2^31 - 1, a stride
- * below table_width, table_width * page_size above 2^31 - 1, n * beams * table_width above 2^32 - 1, table_out == table, lengths_out == lengths,
- * free_left == free_count, free_capacity above 2^31 - 1, copies or the workspace not 16-byte aligned), PREBA_ERR_BUFFER_TOO_SMALL (workspace), PREBA_ERR_CUDA.
+ * below table_width, table_width * page_size above 2^31 - 1, n * beams * table_width above 2^32 - 1,
+ * table_out == table, lengths_out == lengths, free_left == free_count, free_capacity above 2^31 - 1, copies or the workspace not
+ * 16-byte aligned), PREBA_ERR_BUFFER_TOO_SMALL (workspace), PREBA_ERR_CUDA.
  */
 typedef struct {
   const int32_t* parents;     /* DEVICE, n * beams */
@@ -196,8 +200,9 @@ int preba_beam_pages(const preba_beam_pages_t* req, void* stream);
  * copies of preba_beam_pages are so).  An entry whose pages or tokens are out of range is left out (status
  * PREBA_ERR_BAD_TABLE).  One kernel launch for all layers.
  * Errors: PREBA_ERR_INVALID_ARG (NULL, layers of 0 or above PREBA_COPY_MAX_LAYERS, rows of 0 or above
- * PREBA_PAGES_MAX_REQUESTS, a cache or copies that is not 16-byte aligned, strides that are not multiples of 8, head_dim and
- * page_size as for preba_pages_attend, heads_kv of 0 or above 65535), PREBA_ERR_CUDA.
+ * PREBA_PAGES_MAX_REQUESTS, a cache or copies that is not 16-byte aligned, strides that are not multiples of 8
+ * or 2^38 or more, head_dim and page_size as for preba_pages_attend, pages * page_size above 2^31 - 1, another dtype than the two,
+ * heads_kv of 0 or above 65535), PREBA_ERR_CUDA.
  */
 typedef struct {
   const int32_t* copies;      /* DEVICE, [rows, 4] */
