@@ -22,7 +22,7 @@
 // The same kernels serve preba_cross_attend, whose keys are the states of an encoder and lie one after the other
 // (Packed): requests, what their rows see, the copies and the units of the line differ, and nothing else.
 // 16 prompts of up to 448 rows over up to 1500 states, 20 heads of 64: 71 to 73 us (exponentials 57 % of their rate); 6 prompts
-// over images, 14 heads of 80 on 2: 49 us.
+// over images, 14 heads of 80 on 2: 49 to 50 us.
 //
 // P is rounded to 16 bits because the matrix instructions take it so; its row sums are not.  With the one
 // rounding of the result the error against 64 bits is 1.3 to 1.4 times that of the one rounding alone.

@@ -22,7 +22,8 @@ using attend::report;
 // sums up in 64 bits, orders the maxima, reads those few segments again and orders what they hold.
 //
 // 64 requests of 8 beams, 128000 tokens in bf16: 31 to 32 us a call, of which 20 are the bytes at the measured copy rate; the scan
-// takes about 24 (exponentials 65 % of their rate, issue slots 59 %).  4 beams of 32000 tokens: 6.9 us, two launches.
+// takes 26 under the profiler (exponentials 65 % of their rate, issue slots 59 %), the choice 8.5.  4 beams of 32000 tokens: 6.6 to
+// 7.0 us, two launches.
 
 constexpr int kSegmentWords = 512;  // of 32 bits
 constexpr int kLaneWords = kSegmentWords / 32;
@@ -592,7 +593,7 @@ template <typename T, bool Vec> cudaError_t launch_select(const select_args& a, 
 // Only then it is known who is refused for want of pages, and a refused row keeps what lies behind its last page: so where the
 // stack may not suffice, the first kernel leaves the places of a row behind its own last page to the second (which then takes 0.3
 // to 0.5 us more).
-// 128 requests of 8 beams over 8192 tokens: 10.6 to 11.2 us (one block that hands out for all: 35); 2 of 4: 6.5 us, two launches.
+// 128 requests of 8 beams over 8192 tokens: 10.6 to 11.2 us (one block that hands out for all: 35); 2 of 4: 6.5 to 7.0 us, two launches.
 
 constexpr int kColumns = 256;
 constexpr int kHandThreads = 256;
@@ -961,7 +962,7 @@ uint64_t pages_workspace(uint32_t n, uint32_t beams, uint32_t table_width) {
 //
 // Bytes bound it: what is copied, in and out once.  The rows that have a copy are found by every block for itself, a
 // job is a row's page in one cache, keys or values, and blocks take jobs in turn.  64 requests of 8 beams, 12 layers, 304 MB in
-// and out: 49 to 50 us, 94 % of the measured copy rate; 4 requests of 4 beams: 3.0 to 3.6 us, a launch.
+// and out: 49 to 52 us, 90 to 94 % of the measured copy rate; 4 requests of 4 beams: 3.0 to 3.6 us, a launch.
 
 constexpr int kCopyThreads = 256;
 constexpr uint32_t kCopyRows = 1024;  // looked at in one go

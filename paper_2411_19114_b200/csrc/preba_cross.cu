@@ -18,7 +18,7 @@
 // P is rounded to the states' type because the matrix instructions take it so; its sums are not.
 //
 // Bound by bytes, less a start and an end: 64 requests of 5 beams over 1500 states of 20 heads of 64 59 to 60 us, 48 of 8 beams
-// over 2000 states of 8 heads of 128 52 to 53 us (floors 50 and 41; 6.1 TB/s while it streams); 2 requests of 4 beams over
+// over 2000 states of 8 heads of 128 51 to 53 us (floors 50 and 41; 6.1 TB/s while it streams); 2 requests of 4 beams over
 // 375 states 7.9 us, a chain of latencies.
 //
 // More rows go to the kernels for many rows (preba_attend_tiles.cu).
