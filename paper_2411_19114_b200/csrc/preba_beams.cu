@@ -592,7 +592,7 @@ template <typename T, bool Vec> cudaError_t launch_select(const select_args& a, 
 // L2), so that it knows where its own requests' copies and pages stand among all, and hands out without asking another.
 // Only then it is known who is refused for want of pages, and a refused row keeps what lies behind its last page: so where the
 // stack may not suffice, the first kernel leaves the places of a row behind its own last page to the second (which then takes 0.3
-// to 0.5 us more).
+// to 0.5 us more; where a search begins and all rows come from one of 8192 tokens, 10 us more for 128 requests, 3 for 4).
 // 128 requests of 8 beams over 8192 tokens: 10.6 to 11.2 us (one block that hands out for all: 35); 2 of 4: 6.5 to 7.0 us, two launches.
 
 constexpr int kColumns = 256;
@@ -938,7 +938,8 @@ __global__ void __launch_bounds__(kHandThreads) hand_out_kernel(const __grid_con
       const int32_t length = p.lengths[from];
       first = own, last = held_pages(a, length);
       // the last page of all children but the first is another one, and written above
-      const bool again = __any_sync(kFull, lane < static_cast<int>(i - row0) && p.parents[row0 + min(lane, static_cast<int>(i - row0))] == parent);
+      const bool before = lane < static_cast<int>(i - row0);
+      const bool again = __any_sync(kFull, before && p.parents[row0 + lane] == parent);
       if (again && (length & ((1u << a.page_shift) - 1))) --last;
     } else if (lane == 0) {
       p.lengths_out[i] = 0;
